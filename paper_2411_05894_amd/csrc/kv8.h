@@ -1,0 +1,174 @@
+// 8-bit KV cache: layout, codes and what its kernels share (private).
+//
+// A layer is [page][kv head] records of 64 * head_dim bytes -- the codes of a block of 32 positions, K and then V -- followed by the
+// scales, float2 {K, V} per [page][kv head].  Within a record both are in the order in which the matrix instructions take their operands
+// (16x16x32: lane l holds row l % 16, 8 k-slots from 8 * (l / 16)), two operand tiles side by side so that a lane's share of both is one
+// 16-byte load and a wave's 1 KiB in a row:
+//   K: for u (16 positions), p < head_dim/64: lane l's 16 bytes are position 16u + l%16, channels 32p + 8(l/16) .. +7, then the same ones
+//      plus head_dim/2 (pairs of a rotation by halves lie in one record: the writer needs no neighbour for them)
+//   V: for p < head_dim/32: lane l's 16 bytes are channel 32p + l%16 at positions 4(l/16) .. +3 and 16 + 4(l/16) .. +3, then channel
+//      32p + 16 + l%16: the positions whose scores that lane owns after the two score products, so probabilities are operands as they are
+// Integer codes are stored plus 128: a byte behind 0x64 is then the float16 1024 + code + 128.
+#pragma once
+#include "../../include/sssd_kv8.h"
+#include "common.h"
+
+typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
+
+constexpr int KV8_BLOCK = 32;   // positions of a page
+
+// Bits of the status word
+constexpr int KV8_RANGE = 1, KV8_NOT_FINITE = 2;
+
+struct Kv8Geom {
+    const int32_t *table;   // device [max_batch][blocks_per_seq], or nullptr: contiguous runs
+    int blocks_per_seq, n_pages, nkv, max_seq;
+};
+__device__ __forceinline__ int kv8_entry(const Kv8Geom &g, int b, int blk)
+{
+    const size_t at = (size_t)b * g.blocks_per_seq + blk;
+    return g.table ? g.table[at] : (int)at;
+}
+__device__ __forceinline__ int kv8_page(const Kv8Geom &g, int b, int blk) { return min(max(kv8_entry(g, b, blk), 0), g.n_pages - 1); }
+
+// Rows of heads as a kernel takes them (sssd_rows); `vec`: 16 bytes at a time.
+struct Rows8 {
+    char *p;
+    int64_t bs, rs, hs;   // elements
+    int bf16, vec;
+    __device__ __forceinline__ char *at(int b, int j, int h) const { return p + (b * bs + j * rs + h * hs) * (bf16 ? 2 : 4); }
+};
+__device__ __forceinline__ void unpack_bf16x8(const u32x4 &u, float (&x)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = bits_f32(u[i] << 16);
+        x[2 * i + 1] = bits_f32(u[i] & 0xFFFF0000u);
+    }
+}
+__device__ __forceinline__ float load1(const Rows8 &r, const char *row, int ch)
+{
+    return r.bf16 ? bf16_to_f32(reinterpret_cast<const uint16_t *>(row)[ch]) : reinterpret_cast<const float *>(row)[ch];
+}
+__device__ __forceinline__ void load8(const Rows8 &r, const char *row, int ch, float (&x)[8])
+{
+    if (!r.vec) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = load1(r, row, ch + i);
+    } else if (r.bf16) {
+        unpack_bf16x8(*reinterpret_cast<const u32x4 *>(row + ch * 2), x);
+    } else {
+        const f32x4 lo = *reinterpret_cast<const f32x4 *>(row + ch * 4), hi = *reinterpret_cast<const f32x4 *>(row + ch * 4 + 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[i] = lo[i];
+            x[4 + i] = hi[i];
+        }
+    }
+}
+// bf16: rounded once, to nearest even (what is no number stays none)
+__device__ __forceinline__ void store1(const Rows8 &r, char *row, int ch, float x)
+{
+    if (r.bf16) reinterpret_cast<uint16_t *>(row)[ch] = (uint16_t)pack_bf16x2(x, 0.f);
+    else reinterpret_cast<float *>(row)[ch] = x;
+}
+__device__ __forceinline__ void store8(const Rows8 &r, char *row, int ch, const float (&x)[8])
+{
+    if (!r.vec) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) store1(r, row, ch + i, x[i]);
+    } else if (r.bf16) {
+        *reinterpret_cast<u32x4 *>(row + ch * 2) = u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
+    } else {
+        *reinterpret_cast<f32x4 *>(row + ch * 4) = f32x4{x[0], x[1], x[2], x[3]};
+        *reinterpret_cast<f32x4 *>(row + ch * 4 + 16) = f32x4{x[4], x[5], x[6], x[7]};
+    }
+}
+
+// Rows of sequence b in a call of n; false: rejected.
+__device__ __forceinline__ bool kv8_rows(const int32_t *lens, const int32_t *counts, int b, int n, int max_seq, int &len, int &count)
+{
+    len = lens ? lens[b] : 0;
+    count = counts ? counts[b] : n;
+    return len >= 0 && count >= 0 && count <= n && (int64_t)len + count <= max_seq;
+}
+
+// The draft tree of one sequence, in lanes 0 .. n-1 of a wave (n <= 32): every lane's word of visible new rows, itself and its ancestors.
+// Five rounds of doubling: a lane adds what the row sees that it points to and points to where that one pointed.  bad: a parent
+// outside [0, lane), taken as lane - 1.
+__device__ __forceinline__ uint32_t kv8_tree_word(const int32_t *parents, int n, int lane, bool &bad)
+{
+    int up = lane > 0 && lane < n ? parents[lane] : 0;
+    bad = lane > 0 && lane < n && (up < 0 || up >= lane);
+    if (bad) up = lane - 1;
+    uint32_t word = 1u << (lane & 31);
+#pragma unroll
+    for (int i = 0; i < 5; ++i) {
+        word |= (uint32_t)__shfl((int)word, up);
+        up = __shfl(up, up);
+    }
+    return word;
+}
+__device__ __forceinline__ uint32_t kv8_chain_word(int j) { return (2u << j) - 1u; }
+
+struct Rope8 {
+    const double *turns;
+    int r, neighbours;
+    float magnitude;
+};
+// cos and sin of 2 pi frac(position * turns), times the magnitude.  The product in 64 bits: at position 10^6 a 32-bit angle is off by 0.06.
+__device__ __forceinline__ void rope_cos_sin(const Rope8 &rp, int position, double turns, float &c, float &s)
+{
+    const double t = (double)position * turns;
+    sincospif(2.f * (float)(t - __builtin_rint(t)), &s, &c);
+    c *= rp.magnitude;
+    s *= rp.magnitude;
+}
+
+// A rotation shared out over threads: an item is a unit (rope_unit) of a row, through `per` heads.
+struct RopeWork {
+    int d, heads, per, unit;      // unit: 8, 2 or 1
+    uint32_t n, units, items;     // units of a row; items: rows x units
+};
+RopeWork rope_work(int B, int n, int d, int heads, int r, bool neighbours, int threads);
+
+struct Kv8StoreArgs {
+    Kv8Geom g;
+    uint8_t *codes;      // the layer (commit: layer 0)
+    float2 *scales;
+    size_t layer_bytes;
+    int first, B, n, blocks;   // blocks: of a sequence that a call may touch at most
+    Rows8 k, v, q, q_out;      // q.p null: no queries
+    const int32_t *lens, *counts, *parents;
+    Rope8 rope;                // turns null: none
+    RopeWork work;             // of the queries
+    int32_t *status;
+};
+hipError_t launch_rope(const Rows8 &x, const Rows8 &out, const int32_t *positions, const Rope8 &rope, const RopeWork &w, hipStream_t s);
+hipError_t launch_kv8_append(const Kv8StoreArgs &a, int fmt, int d, hipStream_t s);
+hipError_t launch_kv8_read(const Kv8StoreArgs &a, int fmt, int d, hipStream_t s);
+hipError_t launch_kv8_commit(const Kv8StoreArgs &a, int fmt, int d, int layers, const int32_t *accepted, const int32_t *path, int32_t *lens, hipStream_t s);
+
+// How the attention's work is cut: `share` segments of a sequence at most, `passes` over the cache for the 16-row tiles of queries.
+struct Kv8Plan {
+    int passes, share;
+};
+constexpr int KV8_GROUPS = 512, KV8_MAX_TILES = 4;   // workgroups of a launch whose segments are merged, row tiles of a pass
+struct Kv8AttnArgs {
+    Kv8Geom g;
+    const uint8_t *codes;    // the layer
+    const float2 *scales;
+    int B, n, gq;            // gq: query heads of a kv head
+    Rows8 q, out;
+    const int32_t *lens, *counts, *parents;
+    int window, sinks;       // window 0: all positions
+    float *part_o;           // [sequence][kv head][segment][rows_pad][d] sums
+    float2 *part_ml;         // ... reference of the exponents (log2), sum of probabilities
+    int rows_pad;            // rows of a (sequence, kv head) in whole tiles
+    Kv8Plan plan;
+    int32_t *status;
+};
+Kv8Plan kv8_plan(int B, int n, int gq, int nkv);
+size_t kv8_attention_ws(int d);   // bytes behind the workspace that any call's partial results take
+hipError_t launch_kv8_attention(Kv8AttnArgs a, int fmt, int d, void *ws, hipStream_t s);

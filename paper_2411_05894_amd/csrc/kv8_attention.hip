@@ -1,0 +1,544 @@
+// Attention of a step's new rows over a KV cache in 8 bits.
+#include "kv8.h"
+
+namespace {
+
+__device__ __forceinline__ f32x4 mfma16(const half8_t &a, const half8_t &b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+constexpr float NEG_BIG = -1.0e30f;
+constexpr int NWAVE = 4;
+// Probabilities are kept below 2^15 (the largest float16 is 65504): the reference of the exponents is put 2^7 below a row's maximum and
+// follows once the maximum has outgrown it by 2^15.  So they lose no bits to float16's small numbers until they are 2^-21 of the largest.
+constexpr float REF_BELOW = 7.f, REF_MOST = 15.f;
+
+// max / sum over the four lanes 16 apart that share a query row
+__device__ __forceinline__ float rows_max(float x)
+{
+    auto h = __builtin_amdgcn_permlane32_swap(f32_bits(x), f32_bits(x), false, false);
+    x = fmaxf(bits_f32(h[0]), bits_f32(h[1]));
+    h = __builtin_amdgcn_permlane16_swap(f32_bits(x), f32_bits(x), false, false);
+    return fmaxf(bits_f32(h[0]), bits_f32(h[1]));
+}
+__device__ __forceinline__ float rows_sum(float x)
+{
+    auto h = __builtin_amdgcn_permlane32_swap(f32_bits(x), f32_bits(x), false, false);
+    x = bits_f32(h[0]) + bits_f32(h[1]);
+    h = __builtin_amdgcn_permlane16_swap(f32_bits(x), f32_bits(x), false, false);
+    return bits_f32(h[0]) + bits_f32(h[1]);
+}
+
+__device__ __forceinline__ uint32_t half2_bits(half2_t x) { return __builtin_bit_cast(uint32_t, x); }
+__device__ __forceinline__ uint32_t pack_half2(float a, float b)   // to nearest even
+{
+    const f32x2_t v = {a, b};
+    return half2_bits(__builtin_convertvector(v, half2_t));
+}
+__device__ __forceinline__ void split_half2(float a, float b, uint32_t &hi, uint32_t &lo)   // x ~= hi + lo, 22 bits
+{
+    hi = pack_half2(a, b);
+    const half2_t h = __builtin_bit_cast(half2_t, hi);
+    lo = pack_half2(a - (float)h[0], b - (float)h[1]);
+}
+
+// Eight codes as float16, times `ratio` (a power of two).
+template <int FMT> __device__ __forceinline__ half8_t codes_half8(uint32_t w0, uint32_t w1, float ratio)
+{
+    u32x4 r;
+    if (FMT == SSSD_KV8_E4M3) {
+        r[0] = half2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w0, ratio, false));
+        r[1] = half2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w0, ratio, true));
+        r[2] = half2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w1, ratio, false));
+        r[3] = half2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w1, ratio, true));
+    } else {   // 0x64xx is 1024 + xx, and xx the code + 128
+        const _Float16 f = (_Float16)ratio, off = (_Float16)(-1152.f * ratio);
+        const half2_t m = {f, f}, o = {off, off};
+        auto two = [&](uint32_t w, uint32_t sel) {
+            return half2_bits(__builtin_elementwise_fma(__builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, w, sel)), m, o));
+        };
+        r[0] = two(w0, 0x04010400u);
+        r[1] = two(w0, 0x04030402u);
+        r[2] = two(w1, 0x04010400u);
+        r[3] = two(w1, 0x04030402u);
+    }
+    return __builtin_bit_cast(half8_t, r);
+}
+
+// The blocks of a sequence that some row of the call can see: `sink` at its front, then those from `from` on.
+struct Span {
+    int sink, from, n;
+    __device__ __forceinline__ int block(int i) const { return i < sink ? i : i - sink + from; }
+};
+__device__ __forceinline__ Span span_of(int len, int count, int window, int sinks)
+{
+    const int end = (len + count + 31) >> 5;
+    Span s{0, 0, end};
+    if (window > 0 && len >= window) {
+        s.from = (len - window + 1) >> 5;            // the root row sees farthest back
+        s.sink = min((int)(((unsigned)sinks + 31u) >> 5), s.from);
+        s.n = s.sink + end - s.from;
+    }
+    return s;
+}
+struct Cut {
+    int each, n;   // blocks per segment (the last may have fewer), segments
+};
+// By the sequence's own blocks and the call's plan alone: what the others hold changes no bit.  At least four blocks a segment, one for each wave;
+// up to eight are one segment.
+__device__ __forceinline__ Cut cut_of(int blocks, int share)
+{
+    auto up = [](int x, int y) { return (int)(((unsigned)x + (unsigned)y - 1u) / (unsigned)y); };
+    if (blocks <= 0) return Cut{1, 1};
+    const int fair = up(blocks, share), least = blocks <= 8 ? 8 : 4;
+    Cut c;
+    c.each = up(blocks, up(blocks, max(fair, least)));
+    if (c.each >= 16) c.each = (c.each + 3) & ~3;
+    c.n = up(blocks, c.each);
+    return c;
+}
+
+struct RowOut {   // where query row r of (sequence, kv head) goes
+    int j, head;
+    __device__ __forceinline__ RowOut(int r, int gq, int kvh) : j((int)((unsigned)r / (unsigned)gq)), head(kvh * gq + r - j * gq) {}
+};
+__device__ __forceinline__ void store4(const Rows8 &o, char *row, int ch, const f32x4 &y)
+{
+    if (!o.vec) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) store1(o, row, ch + i, y[i]);
+    } else if (o.bf16) {
+        *reinterpret_cast<uint2 *>(row + ch * 2) = uint2{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
+    } else {
+        *reinterpret_cast<f32x4 *>(row + ch * 4) = y;
+    }
+}
+
+// PARTS: the query operand is float16 (1: bf16 queries) or float16 hi + lo (2: float32 queries), and so are the probabilities.
+template <int HD, int FMT, int RT, int PARTS>
+__global__ __launch_bounds__(NWAVE * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void kv8_attn_kernel(Kv8AttnArgs a)
+{
+    constexpr int KS = HD / 32, DT = HD / 16, QT = DT / 4, TR = RT <= 2 ? RT : 2;
+    constexpr int QREC = RT * KS * PARTS * 64, RRED = NWAVE * (NWAVE - 1) * TR * QT * 64;
+    __shared__ u32x4 lds[QREC > RRED ? QREC : RRED];
+    __shared__ float row_scale_s[RT * 16];
+    __shared__ uint32_t word_s[RT * 16];
+    __shared__ int low_s[RT * 16], depth_s[32];
+    __shared__ float2 ml_s[NWAVE][RT * 16];
+    __shared__ float vref_s[NWAVE];
+
+    const int passes = a.plan.passes, share = a.plan.share, nkv = a.g.nkv;
+    uint32_t id = blockIdx.x;
+    const int pass = (int)(id % (uint32_t)passes);
+    id /= (uint32_t)passes;
+    const int segment = (int)(id % (uint32_t)share);
+    id /= (uint32_t)share;
+    const int b = (int)(id / (uint32_t)nkv), kvh = (int)id - b * nkv;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int q = lane >> 4, c = lane & 15;
+    int len, count;
+    const bool ok = kv8_rows(a.lens, a.counts, b, a.n, a.g.max_seq, len, count);
+    const int rt0 = pass * RT;
+    if (!ok) {   // zeros
+        if (segment == 0) {
+            if (kvh == 0 && pass == 0 && threadIdx.x == 0) atomicOr(a.status, KV8_RANGE);
+            for (int i = threadIdx.x; i < RT * 16 * (HD / 4); i += NWAVE * 64) {
+                const int r = rt0 * 16 + i / (HD / 4);
+                const RowOut o(r, a.gq, kvh);
+                if (o.j < a.n) store4(a.out, a.out.at(b, o.j, o.head), i % (HD / 4) * 4, f32x4{0.f, 0.f, 0.f, 0.f});
+            }
+        }
+        return;
+    }
+    const int rows = count * a.gq;
+    if (rt0 * 16 >= rows) return;
+    const Span span = span_of(len, count, a.window, a.sinks);
+    const Cut cut = cut_of(span.n, share);
+    if (segment >= cut.n) return;
+    const int first = segment * cut.each, n_blk = min(cut.each, span.n - first);
+    const int n_it = n_blk > wave ? (n_blk - wave + NWAVE - 1) / NWAVE : 0;
+
+    // Pages and scales of this wave's blocks: lane l keeps those of its block number 64 * chunk + l, one chunk ahead.
+    struct Ahead {
+        int page;
+        float2 scale;
+    };
+    auto look = [&](int chunk) {
+        const int i = min(first + wave + NWAVE * (64 * chunk + lane), span.n - 1);
+        Ahead x;
+        const int entry = kv8_entry(a.g, b, span.block(i));
+        x.page = min(max(entry, 0), a.g.n_pages - 1);
+        if (entry != x.page && kvh == 0 && pass == 0) atomicOr(a.status, KV8_RANGE);
+        x.scale = a.scales[(size_t)x.page * nkv + kvh];
+        return x;
+    };
+    int chunk = 0;
+    Ahead now = look(0), next = look(1);
+
+    constexpr int KR = HD / 32, VR = HD / 32;   // 16-byte records of a lane
+    u32x4 k[KR], v[VR];
+    auto block = [&](int i) {
+        const int at = i < n_it ? i : 0;
+        const int page = __builtin_amdgcn_readlane(at >> 6 == chunk ? now.page : next.page, at & 63);
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(a.codes) + ((size_t)page * nkv + kvh) * (64 * HD), 0, i < n_it ? 64 * HD : 0, 0x00027000);
+    };
+    auto load_k = [&](int i) {
+        const auto p = block(i);
+#pragma unroll
+        for (int x = 0; x < KR; ++x) k[x] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(p, lane * 16, x * 1024, 0));
+    };
+    auto load_v = [&](int i) {
+        const auto p = block(i);
+#pragma unroll
+        for (int x = 0; x < VR; ++x) v[x] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(p, lane * 16, 32 * HD + x * 1024, 0));
+    };
+    load_k(0);
+    load_v(0);
+
+    // Query operands: a row's channels times a power of two that brings its largest below 2^15, as float16.
+    {
+        constexpr int TPR = HD / 8, RPP = NWAVE * 64 / TPR;   // threads of a row, rows at a time
+        const int part = threadIdx.x % TPR;
+#pragma unroll
+        for (int r0 = 0; r0 < RT * 16; r0 += RPP) {
+            const int r = r0 + (int)threadIdx.x / TPR;
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = 0.f;
+            if (rt0 * 16 + r < rows) {
+                const RowOut o(rt0 * 16 + r, a.gq, kvh);
+                load8(a.q, a.q.at(b, o.j, o.head), part * 8, x);
+            }
+            float most = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(x[i]));
+#pragma unroll
+            for (int i = TPR / 2; i > 0; i >>= 1) most = fmaxf(most, __shfl_xor(most, i));
+            const int e = (int)(f32_bits(most) >> 23);   // 2^(e-127) <= most < 2^(e-126)
+            const int up = e == 0 || e == 255 ? 127 : min(268 - e, 253);   // biased exponent of the factor, 2^(141-e)
+            const float f = bits_f32((uint32_t)up << 23);
+            u32x4 hi, lo;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint32_t h, l;
+                if (PARTS == 2) split_half2(x[2 * i] * f, x[2 * i + 1] * f, h, l);
+                else h = pack_half2(x[2 * i] * f, x[2 * i + 1] * f), l = 0;
+                hi[i] = h;
+                lo[i] = l;
+            }
+            if (r >= RT * 16) continue;   // an odd tile of 64 channels
+            const int rec = (((r >> 4) * KS + (part >> 2)) * PARTS) * 64 + (part & 3) * 16 + (r & 15);
+            lds[rec] = hi;
+            if (PARTS == 2) lds[rec + 64] = lo;
+            if (part == 0) row_scale_s[r] = bits_f32((uint32_t)(254 - up) << 23);
+        }
+    }
+    // What the rows see of the new ones, and where their windows begin.
+    {
+        bool bad = false;
+        uint32_t word = a.parents ? kv8_tree_word(a.parents + (size_t)b * a.n, count, lane, bad) : kv8_chain_word(lane & 31);
+        if (segment == 0 && kvh == 0 && pass == 0 && wave == 0 && __any(bad) && lane == 0) atomicOr(a.status, KV8_RANGE);
+        const int depth = __popc(word) - 1;
+        if (wave == 0 && lane < 32) depth_s[lane] = depth;
+        if (a.window > 0 && a.window < count) {   // ancestors farther than the window go, but for those among the first positions
+            uint32_t near = 0;
+            for (int i = 0; i < count; ++i) {
+                const int d = __shfl(depth, i);
+                if (depth - d < a.window || len + d < a.sinks) near |= 1u << i;
+            }
+            word &= near;
+        }
+#pragma unroll
+        for (int t = 0; t < (RT * 16 + 63) / 64; ++t) {
+            const int r = t * 64 + lane, j = min(RowOut(rt0 * 16 + r, a.gq, kvh).j, 31);
+            const uint32_t w = (uint32_t)__shfl((int)word, j);
+            const int d = __shfl(depth, j);
+            if (wave == 0 && r < RT * 16) {
+                word_s[r] = w;
+                low_s[r] = a.window > 0 ? len + d - a.window + 1 : 0;
+            }
+        }
+    }
+    __syncthreads();
+    float row_scale[RT];
+    const float soft = 1.4426950408889634f * rsqrtf((float)HD);   // log2(e) / sqrt(d)
+#pragma unroll
+    for (int t = 0; t < RT; ++t) row_scale[t] = row_scale_s[t * 16 + c] * soft;
+
+    f32x4 o[RT][DT];
+    float m_run[RT], l_run[RT], v_ref = 0.f;
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[t][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        m_run[t] = NEG_BIG;
+        l_run[t] = 0.f;
+    }
+    const int all_from = a.window > 0 ? len + count - a.window : 0;   // every row sees the old positions from here on
+
+    for (int i = 0; i < n_it; ++i) {
+        if (i >> 6 != chunk) {
+            chunk = i >> 6;
+            now = next;
+            next = look(chunk + 1);
+        }
+        const int t0 = span.block(first + wave + NWAVE * i) * 32;
+        const float k_scale = bits_f32((uint32_t)__builtin_amdgcn_readlane((int)f32_bits(now.scale.x), i & 63));
+        const float v_scale = bits_f32((uint32_t)__builtin_amdgcn_readlane((int)f32_bits(now.scale.y), i & 63));
+        f32x4 s[RT][2];   // s[t][u][r]: position t0 + 16u + 4q + r for query row c of tile t
+#pragma unroll
+        for (int t = 0; t < RT; ++t) s[t][0] = s[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            half8_t kk[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const u32x4 &w = k[u * (KS / 2) + ks % (KS / 2)];
+                kk[u] = ks < KS / 2 ? codes_half8<FMT>(w[0], w[1], 1.f) : codes_half8<FMT>(w[2], w[3], 1.f);
+            }
+#pragma unroll
+            for (int t = 0; t < RT; ++t)
+#pragma unroll
+                for (int part = 0; part < PARTS; ++part) {
+                    const half8_t qq = __builtin_bit_cast(half8_t, lds[((t * KS + ks) * PARTS + part) * 64 + lane]);
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) s[t][u] = mfma16(kk[u], qq, s[t][u]);
+                }
+        }
+        load_k(i + 1);
+        if (t0 + 32 > len || (t0 < all_from && t0 + 32 > a.sinks)) {   // not all of the block is seen by all rows
+#pragma unroll
+            for (int t = 0; t < RT; ++t) {
+                const uint32_t word = word_s[t * 16 + c];
+                const int low = low_s[t * 16 + c];
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int p = t0 + 16 * u + 4 * q + r, x = p - len;
+                        const bool sees = x < 0 ? p >= low || p < a.sinks : x < 32 && (word >> (x & 31) & 1u);
+                        if (!sees) s[t][u][r] = -INFINITY;
+                    }
+            }
+        }
+        float sc[RT], mx[RT];
+        bool grow = false;
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            sc[t] = row_scale[t] * k_scale;
+            float m = fmaxf(fmaxf(fmaxf(s[t][0][0], s[t][0][1]), fmaxf(s[t][0][2], s[t][0][3])), fmaxf(fmaxf(s[t][1][0], s[t][1][1]), fmaxf(s[t][1][2], s[t][1][3])));
+            mx[t] = rows_max(m) * sc[t];
+            grow = grow || mx[t] > m_run[t] + REF_MOST;
+        }
+        if (__any(grow)) {
+#pragma unroll
+            for (int t = 0; t < RT; ++t) {
+                const float m_new = mx[t] > m_run[t] + REF_MOST ? mx[t] - REF_BELOW : m_run[t], alpha = __builtin_amdgcn_exp2f(m_run[t] - m_new);
+                m_run[t] = m_new;
+                if (i == 0) continue;
+                l_run[t] *= alpha;
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) o[t][dt] *= alpha;
+            }
+        }
+        // The sums are in units of v_ref, a V scale: they move to a larger one only when a block's outgrows it by 2^4.
+        if (v_scale > 16.f * v_ref) {
+            const float down = v_ref / v_scale;   // powers of two
+            if (i > 0) {
+#pragma unroll
+                for (int t = 0; t < RT; ++t)
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt) o[t][dt] *= down;
+            }
+            v_ref = v_scale;
+        }
+        const float ratio = v_scale / v_ref;
+        u32x4 pk[RT][PARTS];
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e >> 1][2 * (e & 1)], sc[t], -m_run[t]));
+                const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e >> 1][2 * (e & 1) + 1], sc[t], -m_run[t]));
+                l_run[t] += p0;
+                l_run[t] += p1;
+                uint32_t hi, lo;
+                if (PARTS == 2) {
+                    split_half2(p0, p1, hi, lo);
+                    pk[t][PARTS - 1][e] = lo;
+                } else {
+                    hi = pack_half2(p0, p1);
+                }
+                pk[t][0][e] = hi;
+            }
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+            const u32x4 &w = v[dt >> 1];
+            const half8_t vv = dt & 1 ? codes_half8<FMT>(w[2], w[3], ratio) : codes_half8<FMT>(w[0], w[1], ratio);
+#pragma unroll
+            for (int t = 0; t < RT; ++t)
+#pragma unroll
+                for (int part = 0; part < PARTS; ++part) o[t][dt] = mfma16(vv, __builtin_bit_cast(half8_t, pk[t][part]), o[t][dt]);
+        }
+        load_v(i + 1);
+    }
+
+    // The waves' sums on one reference per row, each wave ending with a quarter of the channels.
+    f32x4 *red = reinterpret_cast<f32x4 *>(lds);
+    const int dt0 = wave * QT;
+    f32x4 own[RT][QT];
+    __syncthreads();   // the query operands have been read
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        l_run[t] = rows_sum(l_run[t]);
+        if (q == 0) ml_s[wave][t * 16 + c] = float2{m_run[t], l_run[t]};
+    }
+    if (lane == 0) vref_s[wave] = v_ref;
+#pragma unroll
+    for (int w = 0; w < NWAVE; ++w)
+        if (w == wave)
+#pragma unroll
+            for (int t = 0; t < RT; ++t)
+#pragma unroll
+                for (int x = 0; x < QT; ++x) own[t][x] = o[t][w * QT + x];
+    auto part = [&](int quarter, int from, int t, int x) -> f32x4 & {
+        return red[(((quarter * (NWAVE - 1) + from - (from > quarter ? 1 : 0)) * TR + t % TR) * QT + x) * 64 + lane];
+    };
+#pragma unroll
+    for (int tt = 0; tt < RT; tt += TR) {
+        if (tt > 0) __syncthreads();
+#pragma unroll
+        for (int w = 0; w < NWAVE; ++w)
+            if (w != wave)
+#pragma unroll
+                for (int t = tt; t < tt + TR && t < RT; ++t)
+#pragma unroll
+                    for (int x = 0; x < QT; ++x) part(w, wave, t, x) = o[t][w * QT + x];
+        __syncthreads();
+#pragma unroll
+        for (int t = tt; t < tt + TR && t < RT; ++t) {
+            const int row = (rt0 + t) * 16 + c;
+            float2 s4[NWAVE];
+            float m_all = NEG_BIG;
+#pragma unroll
+            for (int i = 0; i < NWAVE; ++i) {
+                s4[i] = ml_s[(wave + i) & (NWAVE - 1)][t * 16 + c];
+                m_all = fmaxf(m_all, s4[i].x);
+            }
+            float l_all = 0.f;
+            f32x4 y[QT];
+#pragma unroll
+            for (int x = 0; x < QT; ++x) y[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < NWAVE; ++i) {
+                const int w = (wave + i) & (NWAVE - 1);
+                const float f = __builtin_amdgcn_exp2f(s4[i].x - m_all), fv = f * vref_s[w];
+                l_all += s4[i].y * f;
+#pragma unroll
+                for (int x = 0; x < QT; ++x) y[x] += (i ? part(wave, w, t, x) : own[t][x]) * fv;
+            }
+            if (row >= rows) continue;
+            if (cut.n == 1) {
+                const RowOut ro(row, a.gq, kvh);
+                const float inv = l_all != 0.f ? 1.f / l_all : 0.f;   // a row that sees nothing: 0
+                char *to = a.out.at(b, ro.j, ro.head);
+#pragma unroll
+                for (int x = 0; x < QT; ++x) store4(a.out, to, (dt0 + x) * 16 + 4 * q, y[x] * inv);
+            } else {
+                const size_t at = (((size_t)b * nkv + kvh) * share + segment) * a.rows_pad + row;
+#pragma unroll
+                for (int x = 0; x < QT; ++x) *reinterpret_cast<f32x4 *>(a.part_o + at * HD + (dt0 + x) * 16 + 4 * q) = y[x];
+                if (wave == 0 && q == 0) a.part_ml[at] = float2{m_all, l_all};
+            }
+        }
+    }
+}
+
+// One wave per query row: lanes 16s .. 16s+15 take segments s, s+4, ...
+template <int HD> __global__ __launch_bounds__(256) void kv8_merge_kernel(Kv8AttnArgs a, int R)
+{
+    const uint32_t task = blockIdx.x * 4 + (threadIdx.x >> 6), nkv = a.g.nkv;
+    if (task >= (uint32_t)a.B * nkv * R) return;
+    const int r = (int)(task % (uint32_t)R), kvh = (int)(task / (uint32_t)R % nkv), b = (int)(task / ((uint32_t)R * nkv));
+    int len, count;
+    if (!kv8_rows(a.lens, a.counts, b, a.n, a.g.max_seq, len, count) || r >= count * a.gq) return;
+    const Cut cut = cut_of(span_of(len, count, a.window, a.sinks).n, a.plan.share);
+    if (cut.n == 1) return;
+    const int lane = threadIdx.x & 63, sg = lane >> 4, cl = lane & 15;
+    constexpr int E = HD / 16;   // channels of a lane
+    const size_t slot = ((size_t)b * nkv + kvh) * a.plan.share * a.rows_pad + r;
+    float m = NEG_BIG;
+    for (int s = sg; s < cut.n; s += 4) m = fmaxf(m, a.part_ml[slot + (size_t)s * a.rows_pad].x);
+    m = rows_max(m);
+    float den = 0.f, num[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) num[e] = 0.f;
+    for (int s = sg; s < cut.n; s += 4) {
+        const size_t at = slot + (size_t)s * a.rows_pad;
+        const float2 ml = a.part_ml[at];
+        const float w = __builtin_amdgcn_exp2f(ml.x - m);
+        den += w * ml.y;
+#pragma unroll
+        for (int e = 0; e < E; e += 4) {
+            const f32x4 x = *reinterpret_cast<const f32x4 *>(a.part_o + at * HD + cl * E + e);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) num[e + i] += w * x[i];
+        }
+    }
+    den = rows_sum(den);
+    const float inv = den != 0.f ? 1.f / den : 0.f;
+    const RowOut o(r, a.gq, kvh);
+    char *to = a.out.at(b, o.j, o.head);
+#pragma unroll
+    for (int e = 0; e < E; e += 4) {
+        f32x4 y;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = rows_sum(num[e + i]) * inv;
+        if (sg == e / 4) store4(a.out, to, cl * E + e, y);
+    }
+}
+
+template <int HD, int FMT, int PARTS> hipError_t launch_parts(const Kv8AttnArgs &a, int rt, hipStream_t s)
+{
+    const dim3 grid((uint32_t)a.B * a.g.nkv * a.plan.share * a.plan.passes), block(NWAVE * 64);
+    switch (rt) {
+    case 1: hipLaunchKernelGGL((kv8_attn_kernel<HD, FMT, 1, PARTS>), grid, block, 0, s, a); break;
+    case 2: hipLaunchKernelGGL((kv8_attn_kernel<HD, FMT, 2, PARTS>), grid, block, 0, s, a); break;
+    case 3: hipLaunchKernelGGL((kv8_attn_kernel<HD, FMT, 3, PARTS>), grid, block, 0, s, a); break;
+    default: hipLaunchKernelGGL((kv8_attn_kernel<HD, FMT, 4, PARTS>), grid, block, 0, s, a); break;
+    }
+    return hipGetLastError();
+}
+template <int HD> hipError_t launch_hd(const Kv8AttnArgs &a, int fmt, int rt, hipStream_t s)
+{
+    hipError_t e;
+    if (fmt == SSSD_KV8_E4M3) e = a.q.bf16 ? launch_parts<HD, SSSD_KV8_E4M3, 1>(a, rt, s) : launch_parts<HD, SSSD_KV8_E4M3, 2>(a, rt, s);
+    else e = a.q.bf16 ? launch_parts<HD, SSSD_KV8_INT8, 1>(a, rt, s) : launch_parts<HD, SSSD_KV8_INT8, 2>(a, rt, s);
+    if (e != hipSuccess || a.plan.share == 1) return e;
+    const int R = a.n * a.gq;
+    hipLaunchKernelGGL(kv8_merge_kernel<HD>, dim3(((uint32_t)a.B * a.g.nkv * R + 3) / 4), dim3(256), 0, s, a, R);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+Kv8Plan kv8_plan(int B, int n, int gq, int nkv)
+{
+    const int tiles = (n * gq + 15) / 16;
+    Kv8Plan p;
+    p.passes = (tiles + KV8_MAX_TILES - 1) / KV8_MAX_TILES;
+    const int64_t units = (int64_t)B * nkv * p.passes, share = 256 / units;
+    p.share = share < 1 ? 1 : share > 64 ? 64 : (int)share;
+    return p;
+}
+
+size_t kv8_attention_ws(int d) { return (size_t)KV8_GROUPS * KV8_MAX_TILES * 16 * (d * sizeof(float) + sizeof(float2)); }
+
+hipError_t launch_kv8_attention(Kv8AttnArgs a, int fmt, int d, void *ws, hipStream_t s)
+{
+    const int tiles = (a.n * a.gq + 15) / 16;
+    a.plan = kv8_plan(a.B, a.n, a.gq, a.g.nkv);
+    const int rt = (tiles + a.plan.passes - 1) / a.plan.passes;
+    a.rows_pad = tiles * 16;
+    a.part_o = reinterpret_cast<float *>(ws);
+    a.part_ml = reinterpret_cast<float2 *>(a.part_o + (size_t)KV8_GROUPS * KV8_MAX_TILES * 16 * d);
+    return d == 128 ? launch_hd<128>(a, fmt, rt, s) : launch_hd<64>(a, fmt, rt, s);
+}

@@ -1,0 +1,564 @@
+// Rotary positions, and writing, reading back and committing rows of a KV cache in 8 bits.
+//
+// All of it is bound by memory for prompts and by a launch and two or three dependent round trips for a step's few rows.
+#include "kv8.h"
+
+namespace {
+
+// ------------------------------------------------------------------------------------------------ codes ----
+// The scale of a block of largest finite magnitude `most`: the smallest power of two with most <= 448 s or 127 s, at least 2^-126; 1 for
+// none.  From the bits: most = 1.m * 2^(E-127), and 448 = 1.75 * 2^8, 127 = 1.984375 * 2^6.
+template <int FMT> __device__ __forceinline__ float block_scale(float most)
+{
+    const int bits = (int)f32_bits(most), e = bits >> 23, m = bits & 0x7FFFFF;
+    const int x = FMT == SSSD_KV8_E4M3 ? e - 8 + (m > 0x600000) : e - 6 + (m > 0x7E0000);   // biased exponent of the scale
+    return bits == 0 ? 1.f : bits_f32((uint32_t)max(x, 1) << 23);
+}
+
+// Magnitudes above 2^127 are taken as infinite: rounded up, they would stand for 2^128.
+__device__ __forceinline__ bool finite(float x) { return fabsf(x) <= 0x1p127f; }
+
+// Four codes of values already divided by the scale.
+template <int FMT> __device__ __forceinline__ uint32_t to_codes(float a, float b, float c, float d)
+{
+    if (FMT == SSSD_KV8_E4M3) {
+        int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+        return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+    }
+    auto code = [](float x) { return (uint32_t)((int)__builtin_rintf(x) + 128); };
+    return code(a) | code(b) << 8 | code(c) << 16 | code(d) << 24;
+}
+template <int FMT> __device__ __forceinline__ void from_codes(uint32_t w, float s, float *x)
+{
+    if (FMT == SSSD_KV8_E4M3) {
+        const f32x2_t lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+        x[0] = lo[0] * s;
+        x[1] = lo[1] * s;
+        x[2] = hi[0] * s;
+        x[3] = hi[1] * s;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = (float)((int)(w >> (8 * i) & 0xFFu) - 128) * s;
+    }
+}
+// Both runs of a thread (Place) over the scale, as codes.
+template <int FMT> __device__ __forceinline__ u32x4 row_codes(const float (&x)[8], const float (&y)[8], float inv)
+{
+    return u32x4{to_codes<FMT>(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv), to_codes<FMT>(x[4] * inv, x[5] * inv, x[6] * inv, x[7] * inv),
+                 to_codes<FMT>(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv), to_codes<FMT>(y[4] * inv, y[5] * inv, y[6] * inv, y[7] * inv)};
+}
+template <int FMT> constexpr float largest_code() { return FMT == SSSD_KV8_E4M3 ? 448.f : 127.f; }
+
+// Largest magnitude over a workgroup of 2 * HD threads.
+template <int HD> __device__ __forceinline__ float group_max(float x, float *most_s)
+{
+#pragma unroll
+    for (int i = 32; i > 0; i >>= 1) x = fmaxf(x, __shfl_xor(x, i));
+    if ((threadIdx.x & 63) == 0) most_s[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = most_s[0];
+#pragma unroll
+    for (int w = 1; w < HD / 32; ++w) x = fmaxf(x, most_s[w]);
+    return x;
+}
+
+// A thread of a workgroup on a block: two runs of eight channels of one row, `c` and `c + HD/2`; for K that is record threadIdx.x.
+template <int HD> struct Place {
+    int row, c;
+    __device__ __forceinline__ Place()
+    {
+        const int rec = threadIdx.x, l = rec & 63, p = (rec >> 6) % (HD / 64), u = (rec >> 6) / (HD / 64);
+        row = 16 * u + (l & 15);
+        c = 32 * p + 8 * (l >> 4);
+    }
+};
+
+// V records pass through LDS, [row][channel] with rows HD + 4 bytes apart (a wave's byte accesses then spread over the banks).
+template <int HD> struct Turn {
+    static constexpr int PITCH = HD + 4;
+    static __device__ __forceinline__ void place(int e, int &row, int &ch)   // byte e of record threadIdx.x
+    {
+        const int l = threadIdx.x & 63, p = threadIdx.x >> 6, q = l >> 4, i = e & 7;
+        row = (i < 4 ? 0 : 12) + 4 * q + i;
+        ch = 32 * p + 16 * (e >> 3) + (l & 15);
+    }
+    // record -> the thread's row
+    static __device__ __forceinline__ u32x4 rows(const u32x4 &rec, uint8_t *lds, const Place<HD> &at)
+    {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            int row, ch;
+            place(e, row, ch);
+            lds[row * PITCH + ch] = (uint8_t)(rec[e >> 2] >> (8 * (e & 3)));
+        }
+        __syncthreads();
+        const uint8_t *a = lds + at.row * PITCH + at.c;
+        auto word = [](const uint8_t *x) { return *reinterpret_cast<const uint32_t *>(x); };
+        return u32x4{word(a), word(a + 4), word(a + HD / 2), word(a + HD / 2 + 4)};
+    }
+    // the thread's row -> record
+    static __device__ __forceinline__ u32x4 record(const u32x4 &mine, uint8_t *lds, const Place<HD> &at)
+    {
+        uint8_t *a = lds + at.row * PITCH + at.c;
+        auto put = [](uint8_t *x, uint32_t w) { *reinterpret_cast<uint32_t *>(x) = w; };
+        put(a, mine[0]);
+        put(a + 4, mine[1]);
+        put(a + HD / 2, mine[2]);
+        put(a + HD / 2 + 4, mine[3]);
+        __syncthreads();
+        u32x4 rec = u32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            int row, ch;
+            place(e, row, ch);
+            rec[e >> 2] |= (uint32_t)lds[row * PITCH + ch] << (8 * (e & 3));
+        }
+        return rec;
+    }
+};
+
+template <int HD> __device__ __forceinline__ u32x4 *block_record(uint8_t *codes, int page, int nkv, int h, int is_v)
+{
+    return reinterpret_cast<u32x4 *>(codes + ((size_t)page * nkv + h) * (64 * HD) + is_v * (32 * HD)) + threadIdx.x;
+}
+
+// ------------------------------------------------------------------------------------------------- rope ----
+// Channels ch .. ch+7 of a row, rotated.  `x` holds them as they are.
+__device__ __forceinline__ void rotate8(const Rope8 &rp, const Rows8 &r, const char *row, int ch, int position, float (&x)[8])
+{
+    const int half = rp.r >> 1;
+    if (rp.neighbours) {
+#pragma unroll
+        for (int i = 0; i < 8; i += 2)
+            if (ch + i < rp.r) {
+                float c, s;
+                rope_cos_sin(rp, position, rp.turns[(ch + i) >> 1], c, s);
+                const float a = x[i], b = x[i + 1];
+                x[i] = a * c - b * s;
+                x[i + 1] = b * c + a * s;
+            }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (ch + i < rp.r) {
+            const bool low = ch + i < half;
+            float c, s;
+            rope_cos_sin(rp, position, rp.turns[low ? ch + i : ch + i - half], c, s);
+            const float other = load1(r, row, low ? ch + i + half : ch + i - half);
+            x[i] = low ? x[i] * c - other * s : x[i] * c + other * s;
+        }
+}
+// ... of both runs of a Place, which are each other's pairs where the whole head is rotated by halves.
+template <int HD>
+__device__ __forceinline__ void rotate_place(const Rope8 &rp, const Rows8 &r, const char *row, int c0, int position, float (&x)[8], float (&y)[8])
+{
+    if (!rp.neighbours && rp.r == HD) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float c, s;
+            rope_cos_sin(rp, position, rp.turns[c0 + i], c, s);
+            const float a = x[i], b = y[i];
+            x[i] = a * c - b * s;
+            y[i] = b * c + a * s;
+        }
+    } else {
+        rotate8(rp, r, row, c0, position, x);
+        rotate8(rp, r, row, c0 + HD / 2, position, y);
+    }
+}
+
+// One row's units of the rotation: by halves U pairs (i .. i+U-1 with their partners), as neighbours U/2 pairs that lie in a row, and U
+// channels that pass.  A thread takes its unit through heads h0 .. h1-1: the angles are worked out once.
+template <int U> __device__ __forceinline__ void rope_unit(const Rope8 &rp, const Rows8 &x, const Rows8 &out, int b, int j, int position, int unit, int d, int h0, int h1)
+{
+    const int half = rp.r >> 1;
+    const bool halves = !rp.neighbours;
+    const int turning = halves ? half / U : rp.r / U;      // U divides them
+    const bool pass = unit >= turning;
+    const int ch = pass ? rp.r + (unit - turning) * U : unit * U;
+    auto get = [&](const char *row, int at, float (&v)[U]) {
+        if constexpr (U == 8) load8(x, row, at, v);
+        else
+#pragma unroll
+            for (int i = 0; i < U; ++i) v[i] = load1(x, row, at + i);
+    };
+    auto put = [&](char *row, int at, const float (&v)[U]) {
+        if constexpr (U == 8) store8(out, row, at, v);
+        else
+#pragma unroll
+            for (int i = 0; i < U; ++i) store1(out, row, at + i, v[i]);
+    };
+    if (pass) {
+        if (x.p == out.p) return;
+        for (int h = h0; h < h1; ++h) {
+            const char *row = x.at(b, j, h);
+            char *to = out.at(b, j, h);
+            if constexpr (U == 8) {
+                float v[U];
+                get(row, ch, v);
+                put(to, ch, v);
+            } else {
+                for (int i = 0; i < U && ch + i < d; ++i) store1(out, to, ch + i, load1(x, row, ch + i));
+            }
+        }
+        return;
+    }
+    float c[U], s[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+        if (halves) rope_cos_sin(rp, position, rp.turns[ch + i], c[i], s[i]);
+        else if (i % 2 == 0) rope_cos_sin(rp, position, rp.turns[(ch + i) >> 1], c[i], s[i]);
+    for (int h = h0; h < h1; ++h) {
+        const char *row = x.at(b, j, h);
+        char *to = out.at(b, j, h);
+        float v[U];
+        get(row, ch, v);
+        if (halves) {
+            float w[U], a[U];
+            get(row, ch + half, w);
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                a[i] = v[i] * c[i] - w[i] * s[i];
+                w[i] = w[i] * c[i] + v[i] * s[i];
+            }
+            put(to, ch, a);
+            put(to, ch + half, w);
+        } else {
+#pragma unroll
+            for (int i = 0; i + 1 < U; i += 2) {
+                const float a = v[i];
+                v[i] = a * c[i] - v[i + 1] * s[i];
+                v[i + 1] = v[i + 1] * c[i] + a * s[i];
+            }
+            put(to, ch, v);
+        }
+    }
+}
+
+struct RopeArgs {
+    Rows8 x, out;
+    const int32_t *positions;
+    Rope8 rope;
+    RopeWork w;
+};
+
+template <int U> __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a)
+{
+    const uint32_t item = blockIdx.x * 256u + threadIdx.x;
+    if (item >= a.w.items) return;
+    const uint32_t row = item / a.w.units, unit = item - row * a.w.units, b = row / a.w.n, j = row - b * a.w.n;
+    const int h0 = blockIdx.y * a.w.per;
+    rope_unit<U>(a.rope, a.x, a.out, b, j, a.positions[row], unit, a.w.d, h0, min(h0 + a.w.per, a.w.heads));
+}
+
+// The page of block `step` of the rows that a call moves for sequence b, or -1: a block past them, or the sequence is rejected, which one of
+// its workgroups (`tell`) reports.  Every workgroup looks at all pages of the sequence, so that its blocks agree.
+template <int T> __device__ __forceinline__ int touched_page(const Kv8StoreArgs &a, int b, int step, bool tell, int &len, int &count)
+{
+    const bool fits = kv8_rows(a.lens, a.counts, b, a.n, a.g.max_seq, len, count);
+    if (!fits) {
+        if (tell && step == 0 && threadIdx.x == 0) atomicOr(a.status, KV8_RANGE);
+        return -1;
+    }
+    const int blk0 = len >> 5, last = (len + count - 1) >> 5;
+    if (count == 0 || blk0 + step > last) return -1;
+    if (a.g.table) {
+        bool bad = false;
+        for (int i = blk0 + (int)threadIdx.x; i <= last; i += T) {
+            const int page = kv8_entry(a.g, a.first + b, i);
+            bad |= page < 0 || page >= a.g.n_pages;
+        }
+        if (__syncthreads_or(bad)) {
+            if (tell && step == 0 && threadIdx.x == 0) atomicOr(a.status, KV8_RANGE);
+            return -1;
+        }
+    }
+    return kv8_entry(a.g, a.first + b, blk0 + step);
+}
+
+// ----------------------------------------------------------------------------------------------- append ----
+// Workgroup = (sequence, touched block, kv head, K or V); behind them the workgroups that rotate queries.
+template <int HD, int FMT> __global__ __launch_bounds__(2 * HD) void append_kernel(Kv8StoreArgs a, int store_groups)
+{
+    constexpr int T = 2 * HD;
+    __shared__ float most_s[HD / 32];
+    __shared__ __align__(16) uint8_t turn_s[32 * Turn<HD>::PITCH];
+    __shared__ int32_t up_s[128];   // at most 33 rows and the rest of two trees
+    const int lane = threadIdx.x & 63;
+    int id = blockIdx.x;
+    int len, count;
+    if (id >= store_groups) {
+        id -= store_groups;
+        const RopeWork &w = a.work;
+        const int groups = (int)((w.items + T - 1) / T), chunk = id / groups;
+        const uint32_t first = (uint32_t)(id - chunk * groups) * T, item = min(first + threadIdx.x, w.items - 1);
+        const uint32_t row = item / w.units, unit = item - row * w.units;
+        const int b = (int)(row / w.n), j = (int)row - b * a.n;
+        int dep = j;
+        if (a.parents) {   // a workgroup's rows, 33 at most, may be of several sequences: their trees in LDS, where a thread walks up
+            const int b0 = (int)(first / w.units / w.n), b1 = (int)(min(first + T - 1, w.items - 1) / w.units / w.n);
+            for (int i = threadIdx.x; i < (b1 - b0 + 1) * a.n; i += T) up_s[i] = a.parents[(size_t)b0 * a.n + i];
+            __syncthreads();
+            const int32_t *up = up_s + (b - b0) * a.n;
+            dep = 0;
+            for (int x = j; x > 0; ++dep) {
+                const int y = up[x];
+                x = y < 0 || y >= x ? x - 1 : y;
+            }
+        }
+        const int h0 = chunk * w.per, h1 = min(h0 + w.per, w.heads);
+        if (first + threadIdx.x >= w.items || !kv8_rows(a.lens, a.counts, b, a.n, a.g.max_seq, len, count) || j >= count) return;
+        if (w.unit == 8) rope_unit<8>(a.rope, a.q, a.q_out, b, j, len + dep, unit, HD, h0, h1);
+        else if (w.unit == 2) rope_unit<2>(a.rope, a.q, a.q_out, b, j, len + dep, unit, HD, h0, h1);
+        else rope_unit<1>(a.rope, a.q, a.q_out, b, j, len + dep, unit, HD, h0, h1);
+        return;
+    }
+    const int is_v = id & 1;
+    id >>= 1;
+    const int x0 = (uint32_t)id / (uint32_t)a.g.nkv, h = id - x0 * a.g.nkv, b = (uint32_t)x0 / (uint32_t)a.blocks, step = x0 - b * a.blocks;
+    const int page = touched_page<T>(a, b, step, h == 0 && !is_v, len, count);
+    if (page < 0) return;
+    const int blk = (len >> 5) + step;
+    const Place<HD> at;
+    const int t = blk * 32 + at.row, j = t - len;
+    const Rows8 &in = is_v ? a.v : a.k;
+    float x[8], y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = y[i] = 0.f;
+    float *scale = reinterpret_cast<float *>(a.scales + (size_t)page * a.g.nkv + h) + is_v;
+    u32x4 *record = block_record<HD>(a.codes, page, a.g.nkv, h, is_v);
+    const bool is_new = j >= 0 && j < count;
+    const char *row = in.at(b, is_new ? j : 0, h);
+    if (is_new) {
+        load8(in, row, at.c, x);
+        load8(in, row, at.c + HD / 2, y);
+    }
+    if (blk * 32 < len) {   // the block holds older rows
+        u32x4 old = *record;
+        const float s = *scale;
+        if (is_v) {
+            old = Turn<HD>::rows(old, turn_s, at);
+            __syncthreads();   // turn_s is used again
+        }
+        if (j < 0) {
+            from_codes<FMT>(old[0], s, x);
+            from_codes<FMT>(old[1], s, x + 4);
+            from_codes<FMT>(old[2], s, y);
+            from_codes<FMT>(old[3], s, y + 4);
+        }
+    }
+    if (!is_v && a.rope.turns) {
+        int dep = j;
+        if (a.parents) {
+            bool bad;
+            const uint32_t word = kv8_tree_word(a.parents + (size_t)b * a.n, count, lane, bad);
+            if (step == 0 && h == 0 && threadIdx.x < 64 && __any(bad) && lane == 0) atomicOr(a.status, KV8_RANGE);
+            dep = __popc((uint32_t)__shfl((int)word, j & 31)) - 1;
+        }
+        if (is_new) rotate_place<HD>(a.rope, in, row, at.c, len + dep, x, y);
+    }
+    float most = 0.f;
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        most = fmaxf(most, fmaxf(finite(x[i]) ? fabsf(x[i]) : 0.f, finite(y[i]) ? fabsf(y[i]) : 0.f));
+        odd |= !finite(x[i]) || !finite(y[i]);
+    }
+    const float s = block_scale<FMT>(group_max<HD>(most, most_s)), inv = bits_f32((254u << 23) - f32_bits(s));
+    if (__any(odd)) {
+        if (lane == 0) atomicOr(a.status, KV8_NOT_FINITE);
+        const float top = largest_code<FMT>() * s;
+        auto mend = [&](float z) { return finite(z) ? z : z != z ? 0.f : copysignf(top, z); };
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            x[i] = mend(x[i]);
+            y[i] = mend(y[i]);
+        }
+    }
+    const u32x4 mine = row_codes<FMT>(x, y, inv);
+    *record = is_v ? Turn<HD>::record(mine, turn_s, at) : mine;
+    if (threadIdx.x == 0) *scale = s;
+}
+
+// ------------------------------------------------------------------------------------------------- read ----
+template <int HD, int FMT> __global__ __launch_bounds__(2 * HD) void read_kernel(Kv8StoreArgs a)
+{
+    __shared__ __align__(16) uint8_t turn_s[32 * Turn<HD>::PITCH];
+    int id = blockIdx.x;
+    const int is_v = id & 1;
+    id >>= 1;
+    const int x0 = (uint32_t)id / (uint32_t)a.g.nkv, h = id - x0 * a.g.nkv, b = (uint32_t)x0 / (uint32_t)a.blocks, step = x0 - b * a.blocks;
+    int start, count;
+    const int page = touched_page<2 * HD>(a, b, step, h == 0 && !is_v, start, count);
+    if (page < 0) return;
+    const int blk = (start >> 5) + step;
+    const Place<HD> at;
+    u32x4 rec = *block_record<HD>(a.codes, page, a.g.nkv, h, is_v);
+    const float2 both = a.scales[(size_t)page * a.g.nkv + h];
+    const float s = is_v ? both.y : both.x;
+    if (is_v) rec = Turn<HD>::rows(rec, turn_s, at);
+    const int j = blk * 32 + at.row - start;
+    if (j < 0 || j >= count) return;
+    float x[8], y[8];
+    from_codes<FMT>(rec[0], s, x);
+    from_codes<FMT>(rec[1], s, x + 4);
+    from_codes<FMT>(rec[2], s, y);
+    from_codes<FMT>(rec[3], s, y + 4);
+    const Rows8 &out = is_v ? a.v : a.k;
+    char *row = out.at(b, j, h);
+    store8(out, row, at.c, x);
+    store8(out, row, at.c + HD / 2, y);
+}
+
+// ----------------------------------------------------------------------------------------------- commit ----
+// Whether a sequence's step is committed; acc: accepted drafts, node: in lanes 1..acc of every wave, what lies there.
+__device__ __forceinline__ bool commit_ok(const Kv8StoreArgs &g, const int32_t *accepted, const int32_t *path, int b, int &len, int &acc, int &node)
+{
+    const int lane = threadIdx.x & 63;
+    len = g.lens[b];
+    acc = accepted[b];
+    node = lane;
+    if (len < 0 || (int64_t)len + g.n > g.g.max_seq || acc < 0 || acc >= g.n) return false;
+    bool ok = true;
+    if (path) {
+        if (lane > 0 && lane <= acc) node = path[(size_t)b * g.n + lane];
+        const int before = __shfl_up(node, 1);
+        ok = lane == 0 || lane > acc || (node > before && node < g.n);
+    }
+    const int blk = (len >> 5) + lane;
+    if (blk <= (len + g.n - 1) >> 5) {
+        const int page = kv8_entry(g.g, b, blk);
+        ok = ok && page >= 0 && page < g.g.n_pages;
+    }
+    return __all(ok);
+}
+
+// Workgroup = (layer, sequence, kv head, K or V): the one or two blocks that a step's rows lie in are taken apart, their live rows put in
+// place and both blocks written anew, each with the scale of what it holds then.  Paths that move nothing are left alone.
+template <int HD, int FMT>
+__global__ __launch_bounds__(2 * HD) void commit_kernel(Kv8StoreArgs a, const int32_t *accepted, const int32_t *path)
+{
+    __shared__ float most_s[HD / 32];
+    __shared__ __align__(16) uint8_t rows_s[2][32 * HD], turn_s[32 * Turn<HD>::PITCH];
+    int id = blockIdx.x;
+    const int is_v = id & 1;
+    id >>= 1;
+    const int x0 = (uint32_t)id / (uint32_t)a.g.nkv, h = id - x0 * a.g.nkv, layer = (uint32_t)x0 / (uint32_t)a.B, b = x0 - layer * a.B;
+    int len, acc, node;
+    if (!commit_ok(a, accepted, path, b, len, acc, node)) return;   // the launch that advances lens reports it
+    const int farthest = __shfl(node, acc);
+    if (farthest == acc) return;                                    // strictly increasing from 1: nothing moves
+    const Place<HD> at;
+    uint8_t *codes = a.codes + layer * a.layer_bytes;
+    float2 *scales = reinterpret_cast<float2 *>(reinterpret_cast<char *>(a.scales) + layer * a.layer_bytes);
+    const int blk0 = len >> 5, from_last = (len + farthest) >> 5, to_last = (len + acc) >> 5;
+    float s_old[2] = {1.f, 1.f};
+    for (int x = 0; x <= from_last - blk0; ++x) {   // at most two
+        const int page = kv8_entry(a.g, b, blk0 + x);
+        u32x4 rec = *block_record<HD>(codes, page, a.g.nkv, h, is_v);
+        const float2 both = scales[(size_t)page * a.g.nkv + h];
+        s_old[x] = is_v ? both.y : both.x;
+        if (is_v) {
+            rec = Turn<HD>::rows(rec, turn_s, at);
+            __syncthreads();
+        }
+        uint32_t *to = reinterpret_cast<uint32_t *>(rows_s[x] + at.row * HD + at.c);
+        to[0] = rec[0];
+        to[1] = rec[1];
+        to[HD / 8] = rec[2];
+        to[HD / 8 + 1] = rec[3];
+    }
+    __syncthreads();
+    for (int x = 0; x <= to_last - blk0; ++x) {
+        const int page = kv8_entry(a.g, b, blk0 + x), t = (blk0 + x) * 32 + at.row, i = t - len;
+        float v[8], w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = w[e] = 0.f;
+        const int from_node = __shfl(node, max(min(i, acc), 0));
+        if (i <= acc) {
+            const int src = (i <= 0 ? t : len + from_node) - blk0 * 32;
+            const uint32_t *from = reinterpret_cast<const uint32_t *>(rows_s[src >> 5] + (src & 31) * HD + at.c);
+            const float s = src < 32 ? s_old[0] : s_old[1];
+            from_codes<FMT>(from[0], s, v);
+            from_codes<FMT>(from[1], s, v + 4);
+            from_codes<FMT>(from[HD / 8], s, w);
+            from_codes<FMT>(from[HD / 8 + 1], s, w + 4);
+        }
+        float most = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) most = fmaxf(most, fmaxf(fabsf(v[e]), fabsf(w[e])));
+        const float s = block_scale<FMT>(group_max<HD>(most, most_s)), inv = bits_f32((254u << 23) - f32_bits(s));
+        u32x4 mine = row_codes<FMT>(v, w, inv);
+        if (is_v) mine = Turn<HD>::record(mine, turn_s, at);
+        *block_record<HD>(codes, page, a.g.nkv, h, is_v) = mine;
+        if (threadIdx.x == 0) (is_v ? scales[(size_t)page * a.g.nkv + h].y : scales[(size_t)page * a.g.nkv + h].x) = s;
+        __syncthreads();   // most_s and turn_s are used again
+    }
+}
+
+__global__ __launch_bounds__(64) void advance_kernel(Kv8StoreArgs a, const int32_t *accepted, const int32_t *path, int32_t *lens)
+{
+    const int b = blockIdx.x;
+    int len, acc, node;
+    const bool ok = commit_ok(a, accepted, path, b, len, acc, node);
+    if (threadIdx.x != 0) return;
+    if (ok) lens[b] = len + acc + 1;
+    else atomicOr(a.status, KV8_RANGE);
+}
+
+}  // namespace
+
+// Units of eight channels where pairs and the channels that pass divide into them, else single pairs.  A thread works its unit's angles out
+// once (some thirty instructions a pair) for `per` heads: as many as leave eight workgroups to every compute unit, up to eight.
+RopeWork rope_work(int B, int n, int d, int heads, int r, bool neighbours, int threads)
+{
+    RopeWork w;
+    const int turning = neighbours ? r : r / 2;
+    w.unit = turning % 8 == 0 && (d - r) % 8 == 0 ? 8 : (neighbours ? 2 : 1);
+    const int units = turning / w.unit + (d - r + w.unit - 1) / w.unit;
+    w.n = n; w.d = d; w.heads = heads; w.units = units;
+    w.items = (uint32_t)B * n * units;
+    const int64_t groups = ((int64_t)w.items + threads - 1) / threads * heads;
+    w.per = (int)(groups / 2048 < 1 ? 1 : groups / 2048 > 8 ? 8 : groups / 2048);
+    return w;
+}
+
+hipError_t launch_rope(const Rows8 &x, const Rows8 &out, const int32_t *positions, const Rope8 &rope, const RopeWork &w, hipStream_t s)
+{
+    const RopeArgs a{x, out, positions, rope, w};
+    const dim3 grid((w.items + 255) / 256, (w.heads + w.per - 1) / w.per);
+    if (w.unit == 8) hipLaunchKernelGGL(rope_kernel<8>, grid, dim3(256), 0, s, a);
+    else if (w.unit == 2) hipLaunchKernelGGL(rope_kernel<2>, grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL(rope_kernel<1>, grid, dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
+#define KV8_LAUNCH(kernel, grid, ...)                                                                                                \
+    do {                                                                                                                             \
+        if (d == 128 && fmt == SSSD_KV8_E4M3) hipLaunchKernelGGL((kernel<128, SSSD_KV8_E4M3>), dim3(grid), dim3(256), 0, s, __VA_ARGS__); \
+        else if (d == 128) hipLaunchKernelGGL((kernel<128, SSSD_KV8_INT8>), dim3(grid), dim3(256), 0, s, __VA_ARGS__);               \
+        else if (fmt == SSSD_KV8_E4M3) hipLaunchKernelGGL((kernel<64, SSSD_KV8_E4M3>), dim3(grid), dim3(128), 0, s, __VA_ARGS__);    \
+        else hipLaunchKernelGGL((kernel<64, SSSD_KV8_INT8>), dim3(grid), dim3(128), 0, s, __VA_ARGS__);                              \
+    } while (0)
+
+hipError_t launch_kv8_append(const Kv8StoreArgs &a, int fmt, int d, hipStream_t s)
+{
+    const int store = a.B * a.blocks * a.g.nkv * 2, T = 2 * d;
+    const int turn = a.q.p ? (int)((a.work.items + T - 1) / T) * ((a.work.heads + a.work.per - 1) / a.work.per) : 0;
+    KV8_LAUNCH(append_kernel, store + turn, a, store);
+    return hipGetLastError();
+}
+
+hipError_t launch_kv8_read(const Kv8StoreArgs &a, int fmt, int d, hipStream_t s)
+{
+    KV8_LAUNCH(read_kernel, a.B * a.blocks * a.g.nkv * 2, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_kv8_commit(const Kv8StoreArgs &a, int fmt, int d, int layers, const int32_t *accepted, const int32_t *path, int32_t *lens, hipStream_t s)
+{
+    if (path) KV8_LAUNCH(commit_kernel, layers * a.B * a.g.nkv * 2, a, accepted, path);
+    hipLaunchKernelGGL(advance_kernel, dim3(a.B), dim3(64), 0, s, a, accepted, path, lens);
+    return hipGetLastError();
+}

@@ -1,0 +1,368 @@
+"""Writing, reading back and committing rows of the 8-bit cache, against tests/kv8_reference.py in 64 bits.  Without a rotation what is
+held is the same value for value; with one a held value is within half a step of the rotated row, whose own rounding (|a| + |b|) * 8 * 2^-24
+may carry it past a border."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+from kv8_reference import BLOCK, LIMIT, Cache, code_steps, frequencies, held, lines, rotate, scale_of
+from paper_2411_05894_amd import kv8
+from paper_2411_05894_amd.binding import SSSD_EINVAL, SSSD_ENOSPACE, SSSD_OK
+
+DEV = "cuda:0"
+
+
+def ints(v):
+    return torch.tensor(v, dtype=torch.int32, device=DEV)
+
+
+def table(cache, seed=5):
+    t = torch.randperm(cache.n_pages, generator=torch.Generator().manual_seed(seed)).to(torch.int32)
+    return t[:cache.cfg.max_batch * cache.blocks_per_seq].view(cache.cfg.max_batch, -1).to(DEV)
+
+
+def rows(g, *shape, dtype=torch.float32, outliers=True):
+    x = torch.randn(*shape, generator=g, device=DEV)
+    if outliers:
+        x[..., ::13] *= 9
+        x *= torch.exp2(torch.randint(-3, 4, x.shape[:-2] + (1, 1), generator=g, device=DEV).float())   # rows of several sizes
+    return x.to(dtype)
+
+
+def read_all(cache, layer, lens, n, dtype=torch.bfloat16):
+    B = len(lens)
+    out = [torch.full((B, n, cache.cfg.n_kv_heads, cache.cfg.head_dim), 7.25, dtype=dtype, device=DEV) for _ in range(2)]
+    cache.sssd_kv8_read(layer, None, ints(lens), *out)
+    return out
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("nkv,d,paged", [(2, 64, False), (8, 128, True), (1, 128, False), (3, 64, True)])
+def test_steps_of_a_batch(fmt, dtype, nkv, d, paged):
+    """Rows come in pieces of uneven size, some sequences with none, some rolled back to before what was written; two layers."""
+    g = torch.Generator(device=DEV).manual_seed(nkv * d)
+    B, max_seq = 5, 210
+    cache = kv8.Kv8Cache(2, 2 * nkv, nkv, d, B, max_seq, fmt, n_pages=40 if paged else 0, device=DEV)
+    if paged:
+        cache.sssd_kv8_set_block_table(table(cache))
+    want = [[[Cache(nkv, d, fmt, DEV) for _ in range(2)] for _ in range(B)] for _ in range(2)]
+    lens = [0] * B
+    pieces = [(70, [70, 1, 33, 0, 64]), (1, [1] * 5), (9, [9, 9, 3, 9, 0]), (32, [32, 31, 32, 1, 32]), (5, [5, 5, 5, 5, 5]), (9, [9, 9, 9, 9, 2])]
+    for turn, (n, counts) in enumerate(pieces):
+        print(f"kv8 append {fmt} {dtype} {nkv}x{d} piece {turn}", flush=True)
+        for layer in range(2):
+            k, v = rows(g, B, n, nkv, d, dtype=dtype), rows(g, B, n, nkv, d, dtype=dtype)
+            cache.sssd_kv8_append(layer, k, v, ints(lens), counts=None if turn in (1, 4) else ints(counts))
+            for b in range(B):
+                for c, x in zip(want[layer][b], (k, v)):
+                    if counts[b]:
+                        c.append(lens[b], x[b, :counts[b]])
+        # what is kept of the step: all, or as after rejected drafts
+        lens = [a + (c if turn in (0, 3) else (c + 1) // 2) for a, c in zip(lens, counts)]
+        assert cache.sssd_kv8_sync() == SSSD_OK
+        for layer in range(2):
+            for dt in (torch.bfloat16, torch.float32):
+                got = read_all(cache, layer, lens, max(lens) + 3, dt)
+                for b in range(B):
+                    for x, c in zip(got, want[layer][b]):
+                        assert torch.equal(x[b, :lens[b]].double(), c.x[:lens[b]]), (layer, b, turn)
+                        assert (x[b, lens[b]:] == 7.25).all()
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_every_code_and_border(fmt):
+    """Values at and beside the borders between codes, at several scales: the largest decides the scale, the others round to nearest even."""
+    d = 128
+    codes = torch.arange(256, dtype=torch.uint8).view(torch.float8_e4m3fn).float() if fmt == "e4m3" else torch.arange(-127, 128).float()
+    codes = codes[codes.isfinite() & (codes >= 0)].unique()
+    mid = (codes[1:] + codes[:-1]) / 2
+    x = torch.cat([codes, mid, mid * (1 + 2.0 ** -20), mid * (1 - 2.0 ** -20)])
+    x = torch.cat([x, -x, torch.zeros(-2 * len(x) % d)]).view(-1, d)[:32]
+    x[0, 0] = LIMIT[fmt]
+    scaled = torch.stack([x * 2.0 ** e for e in (0, -20, 60, -118)], 1).to(DEV)       # [rows][heads][d]: one scale per head
+    cache = kv8.Kv8Cache(1, 4, 4, d, 1, 64, fmt, device=DEV)
+    cache.sssd_kv8_append(0, scaled[None], scaled.flip(2)[None].contiguous(), ints([0]))
+    n = len(x)
+    k, v = read_all(cache, 0, [n], n, torch.float32)
+    assert torch.equal(k[0].double(), held(scaled, fmt)[0])
+    assert torch.equal(v[0].double(), held(scaled.flip(2), fmt)[0])
+    assert cache.sssd_kv8_sync() == SSSD_OK
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_scales_at_the_ends_of_the_range(fmt):
+    d, heads = 64, 12
+    tops = [0.0, 1e-45, 2.0 ** -149, 2.0 ** -127, 2.0 ** -126, 2.0 ** -120, 448.0, 448.0 * (1 + 2.0 ** -23), 127.0, 127.0 * (1 + 2.0 ** -23), 3.4e38, 3.3895314e38]
+    x = torch.zeros(3, heads, d, device=DEV)
+    x[1, :, 5] = torch.tensor(tops, device=DEV)
+    x[2, :, 6] = -0.3 * torch.tensor(tops, device=DEV)
+    cache = kv8.Kv8Cache(1, heads, heads, d, 1, 32, fmt, device=DEV)
+    cache.sssd_kv8_append(0, x[None], x[None], ints([0]))
+    k, v = read_all(cache, 0, [3], 3, torch.float32)
+    want, s = held(x, fmt)
+    assert torch.equal(k[0].double(), want) and torch.equal(v, k)
+    big = x.double().abs()
+    assert s.tolist() == [scale_of(float(t), fmt) for t in torch.where(big <= 2.0 ** 127, big, 0.0).amax((0, 2))]
+    assert k.isfinite().all()
+    assert cache.sssd_kv8_sync() == SSSD_EINVAL       # the last two are above 2^127
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_values_that_are_no_finite_numbers(fmt):
+    """They count for no scale, are held as 0 and as the largest code, and are reported; their block's other values are as without them."""
+    d = 64
+    x = torch.randn(20, 2, d, device=DEV)
+    x[3, 0, 7], x[4, 0, 8], x[5, 1, 9] = float("nan"), float("inf"), -float("inf")
+    cache = kv8.Kv8Cache(1, 2, 2, d, 1, 32, fmt, device=DEV)
+    cache.sssd_kv8_append(0, x[None], torch.ones_like(x)[None], ints([0]))
+    assert cache.sssd_kv8_sync() == SSSD_EINVAL and cache.sssd_kv8_sync() == SSSD_OK
+    k, _ = read_all(cache, 0, [20], 20, torch.float32)
+    want, s = held(x, fmt)
+    assert torch.equal(k[0].double(), want)
+    assert k[0, 3, 0, 7] == 0 and k[0, 4, 0, 8] == LIMIT[fmt] * s[0] and k[0, 5, 1, 9] == -LIMIT[fmt] * s[1]
+    x = torch.where(x.isfinite(), x, 0.0)
+    x[7, 0, 0] = float("nan")                       # of a row that the sequence does not have
+    cache.sssd_kv8_append(0, x[None], x[None], ints([0]), counts=ints([7]))
+    assert cache.sssd_kv8_sync() == SSSD_OK
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_rejected_drafts_leave_no_trace(fmt):
+    """Huge rows that are rejected, over and over, against a cache that never saw them: e4m3 the same values, int8 within one step of the
+    largest scale that the rows were held at (half of it, and of each smaller one on the way), however often."""
+    g = torch.Generator(device=DEV).manual_seed(11)
+    d = 128
+    a, b = (kv8.Kv8Cache(1, 2, 1, d, 1, 96, fmt, device=DEV) for _ in range(2))
+    kept = 0
+    for turn in range(12):
+        good, wild = rows(g, 1, 3, 1, d, outliers=False), rows(g, 1, 6, 1, d, outliers=False) * 4.0
+        both = torch.cat([good, wild], 1)
+        a.sssd_kv8_append(0, both, both, ints([kept]))
+        b.sssd_kv8_append(0, good, good, ints([kept]))
+        kept += 3
+    last = rows(g, 1, 1, 1, d, outliers=False)
+    for c in (a, b):
+        c.sssd_kv8_append(0, last, last, ints([kept]))
+    (ka, va), (kb, vb) = (read_all(c, 0, [kept + 1], kept + 1, torch.float32) for c in (a, b))
+    if fmt == "e4m3":      # 448 * 2^-6 / 4: values below 2^-6 of the larger scale may lose bits
+        fine = kb.abs() >= 2.0 ** -4
+        assert torch.equal(ka[fine], kb[fine]) and torch.equal(va[fine], vb[fine])
+        assert ((ka - kb).abs() <= 2.0 ** -9).all()
+    else:                  # |wild| < 4 * 6: a scale of at most 2^-2, and |good| < 6: 2^-4
+        assert ((ka - kb).abs() <= 2.0 ** -2 + 2.0 ** -4 / 2).all() and torch.equal(ka, va)
+
+
+@pytest.mark.parametrize("fmt,d", [("e4m3", 128), ("int8", 64)])
+@pytest.mark.parametrize("rotary,interleaved", [(None, False), (None, True), (32, False), (10, False), (22, True)])
+@pytest.mark.parametrize("tree", [False, True])
+def test_rotation_on_the_way(fmt, d, rotary, interleaved, tree):
+    g = torch.Generator(device=DEV).manual_seed(21)
+    rotary = rotary or d
+    B, n, nq, nkv, max_seq = 3, 13, 6, 2, 300
+    lens, counts = [0, 40, 250], [13, 13, 9]
+    cache = kv8.Kv8Cache(1, nq, nkv, d, B, max_seq, fmt, device=DEV)
+    rope = kv8.Rope(rotary, 10000.0, interleaved=interleaved, magnitude=0.75, device=DEV)
+    qkv = rows(g, B, n, nq + 2 * nkv, d, dtype=torch.bfloat16)
+    q, k, v = qkv[:, :, :nq], qkv[:, :, nq:nq + nkv], qkv[:, :, nq + nkv:]
+    parents = [[0] + [int(x) for x in (torch.rand(n - 1, generator=torch.Generator().manual_seed(b)) * torch.arange(1, n))] for b in range(B)]
+    old = rows(g, B, max_seq, nkv, d, dtype=torch.bfloat16)
+    cache.sssd_kv8_append(0, old, old, ints([0] * B), counts=ints(lens))
+    q_out = torch.full((B, n, nq, d), 3.5, dtype=torch.bfloat16, device=DEV)
+    cache.sssd_kv8_append(0, k, v, ints(lens), counts=ints(counts), rope=rope, parents=ints(parents) if tree else None, q=q, q_out=q_out)
+    assert cache.sssd_kv8_sync() == SSSD_OK
+    freq = frequencies(rotary, 10000.0)
+    got = read_all(cache, 0, [a + c for a, c in zip(lens, counts)], max_seq, torch.float32)
+    for b in range(B):
+        c = counts[b]
+        depth = torch.tensor([len(x) - 1 for x in lines(parents[b] if tree else None, n)][:c], device=DEV)
+        pos = lens[b] + depth
+        exact_k, exact_q = rotate(k[b, :c], pos, freq, interleaved, 0.75), rotate(q[b, :c], pos, freq, interleaved, 0.75)
+        size_q, size_k = (rotate_sizes(x[b, :c], rotary, interleaved) * 0.75 * 8 * 2.0 ** -24 for x in (q, k))
+        assert ((q_out[b, :c].double() - exact_q).abs() <= size_q + (exact_q.abs() + size_q) * torch.finfo(torch.bfloat16).eps / 2).all()
+        assert (q_out[b, c:] == 3.5).all()
+        K, V = Cache(nkv, d, fmt, DEV), Cache(nkv, d, fmt, DEV)
+        K.append(0, old[b, :lens[b]])
+        V.append(0, old[b, :lens[b]])
+        V.append(lens[b], v[b, :c])
+        assert torch.equal(got[1][b, :lens[b] + c].double(), V.x)
+        # K: half a step of the block's scale, which is that of the exact rows (their largest is no border case here)
+        x = torch.cat([K.x[lens[b] // BLOCK * BLOCK:], exact_k])
+        for a in range(0, len(x), BLOCK):
+            s = held(x[a:a + BLOCK], fmt)[1][:, None]
+            at = got[0][b, lens[b] // BLOCK * BLOCK + a:][:len(x[a:a + BLOCK])].double()
+            new = slice(max(0, lens[b] % BLOCK - a), None)
+            err = (at - x[a:a + BLOCK])[new].abs()
+            slack = torch.zeros_like(x[a:a + BLOCK])
+            first = max(0, a - lens[b] % BLOCK)
+            slack[new] = size_k[first:first + len(slack[new])]
+            assert (err <= (code_steps(x[a:a + BLOCK] / s, fmt) * s / 2 + slack)[new]).all()
+    if not tree:      # in place
+        again = q.clone()
+        cache.sssd_kv8_append(0, k, v, ints(lens), rope=rope, q=again, q_out=again)
+        whole = torch.zeros_like(q_out)
+        cache.sssd_kv8_append(0, k, v, ints(lens), rope=rope, q=q, q_out=whole)
+        assert torch.equal(again, whole)
+
+
+def rotate_sizes(x, rotary, interleaved):
+    """|a| + |b| of each rotated channel's pair."""
+    a = x.double().abs()
+    out = torch.zeros_like(a)
+    if interleaved:
+        out[..., 0:rotary:2] = out[..., 1:rotary:2] = a[..., 0:rotary:2] + a[..., 1:rotary:2]
+    else:
+        out[..., :rotary // 2] = out[..., rotary // 2:rotary] = a[..., :rotary // 2] + a[..., rotary // 2:rotary]
+    return out
+
+
+def test_one_slot_of_a_live_batch_and_a_long_prompt():
+    """A prompt of 2011 rows into slot 2 in one call, read back from the middle; the other slots keep their bits."""
+    g = torch.Generator(device=DEV).manual_seed(8)
+    cache = kv8.Kv8Cache(1, 4, 2, 128, 4, 2048, "int8", device=DEV)
+    x = rows(g, 4, 90, 2, 128)
+    cache.sssd_kv8_append(0, x, x, ints([0, 5, 0, 9]))
+    before = cache.cache.clone()
+    p = rows(g, 1, 2011, 2, 128, dtype=torch.bfloat16)
+    cache.sssd_kv8_append(0, p, p, ints([0]), first=2)
+    want = Cache(2, 128, "int8", DEV)
+    want.append(0, p[0])
+    out = [torch.zeros(1, 1000, 2, 128, device=DEV) for _ in range(2)]
+    cache.sssd_kv8_read(0, ints([777]), None, *out, first=2)
+    assert torch.equal(out[0][0].double(), want.x[777:1777]) and torch.equal(out[1], out[0])
+    assert cache.sssd_kv8_sync() == SSSD_OK
+    page = 2 * 64 * 128
+    for slot in (0, 1, 3):
+        a, b = (t[slot * 64 * page:(slot + 1) * 64 * page] for t in (before, cache.cache))
+        assert torch.equal(a, b)
+
+
+def test_rows_at_odd_addresses():
+    g = torch.Generator(device=DEV).manual_seed(4)
+    for dtype in (torch.float32, torch.bfloat16):
+        cache = kv8.Kv8Cache(1, 2, 2, 64, 2, 64, "e4m3", device=DEV)
+        x = rows(g, 2, 40, 2, 64, dtype=dtype)
+        odd = torch.empty(x.numel() + 1, dtype=dtype, device=DEV)[1:].view(x.shape)
+        odd.copy_(x)
+        cache.sssd_kv8_append(0, odd, x.transpose(0, 1).contiguous().transpose(0, 1), ints([0, 3]))
+        k, v = read_all(cache, 0, [40, 43], 43, torch.float32)
+        back = [torch.zeros(2 * 43 * 2 * 64 + 1, dtype=torch.bfloat16, device=DEV)[1:].view(2, 43, 2, 64) for _ in range(2)]
+        cache.sssd_kv8_read(0, None, ints([40, 43]), *back)
+        assert torch.equal(k[:, :40], back[0][:, :40].float()) and torch.equal(k[1], v[1]) and torch.equal(k[0, :40], v[0, :40])
+        one = x[:, :, :1].expand(2, 40, 2, 64)          # one head for both: stride 0
+        cache.sssd_kv8_append(0, one, one, ints([0, 0]))
+        k, _ = read_all(cache, 0, [40, 40], 40)
+        assert torch.equal(k[:, :, 0], k[:, :, 1])
+
+
+@pytest.mark.parametrize("what", ["negative", "long", "count", "page", "page_low"])
+def test_rejected_sequences_are_left_alone(what):
+    cache = kv8.Kv8Cache(1, 2, 2, 64, 3, 96, "e4m3", n_pages=12, device=DEV)
+    t = table(cache)
+    lens, counts = [40, 40, 40], [20, 20, 20]
+    if what == "negative":
+        lens[1] = -1
+    if what == "long":
+        lens[1] = 77
+    if what == "count":
+        counts[1] = 21
+    if what == "page":
+        t[1, 1] = 12
+    if what == "page_low":
+        t[1, 1] = -1
+    cache.sssd_kv8_set_block_table(t)
+    cache.cache.fill_(0x11)
+    x = torch.randn(3, 20, 2, 64, device=DEV)
+    before = cache.cache.clone()
+    cache.sssd_kv8_append(0, x, x, ints(lens), counts=ints(counts))
+    assert cache.sssd_kv8_sync() == SSSD_ENOSPACE and cache.sssd_kv8_sync() == SSSD_OK
+    page = 2 * 64 * 64
+    touched = {int(p) for b in (0, 2) for p in t[b, 1:2]}
+    for p in range(12):
+        same = torch.equal(before[p * page:(p + 1) * page], cache.cache[p * page:(p + 1) * page])
+        assert same == (p not in touched), p
+    out = [torch.full((3, 20, 2, 64), 7.25, device=DEV) for _ in range(2)]
+    cache.sssd_kv8_read(0, ints(lens), ints(counts), *out)
+    assert cache.sssd_kv8_sync() == SSSD_ENOSPACE
+    assert all((o[1] == 7.25).all() and not (o[[0, 2]] == 7.25).any() for o in out)
+
+
+def test_bad_parents_are_taken_as_the_row_before():
+    cache = kv8.Kv8Cache(1, 2, 2, 64, 1, 96, "int8", device=DEV)
+    rope = kv8.Rope(64, 100.0, device=DEV)
+    x = torch.randn(1, 6, 2, 64, device=DEV)
+    got = []
+    for parents, code in (([0, 0, 7, -1, 4, 3], SSSD_ENOSPACE), ([0, 0, 1, 2, 3, 3], SSSD_OK)):
+        q = torch.zeros_like(x)
+        cache.sssd_kv8_append(0, x, x, ints([10]), rope=rope, parents=ints([parents]), q=x, q_out=q)
+        assert cache.sssd_kv8_sync() == code
+        got.append([q] + read_all(cache, 0, [16], 16))
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+PATHS = [list(range(1, 32)), [2, 3, 4, 5, 6, 7, 8, 9, 10, 11], [1, 2, 3, 30, 31], [31], [], [2 * i for i in range(1, 16)],
+         [i + (i > 5) + (i > 9) + (i > 17) for i in range(1, 28)]]
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("d,paged", [(64, True), (128, False)])
+def test_commit_moves_the_path(fmt, d, paged):
+    g = torch.Generator(device=DEV).manual_seed(13)
+    n, max_seq, L, nkv = 32, 160, 2, 2
+    bad = [([2, 1], 2, 5), ([3, 3], 2, 5), ([1, 32], 2, 5), ([1, 2], 32, 5), ([1, 2], -1, 5), ([2, 4], 2, 129), ([2, 4], 2, -3)]
+    paths, lens = PATHS + [p for p, _, _ in bad], [0, 1, 31, 20, 64, 100, 33] + [l for _, _, l in bad]
+    B = len(paths)
+    cache = kv8.Kv8Cache(L, 4, nkv, d, B, max_seq, fmt, device=DEV)
+    if paged:
+        cache.sssd_kv8_set_block_table(table(cache))
+    want = []
+    for layer in range(L):
+        x = [rows(g, B, max_seq, nkv, d) for _ in range(2)]
+        held_lens = [min(max(l, 0) + n, max_seq) for l in lens]
+        cache.sssd_kv8_append(layer, *x, ints([0] * B), counts=ints([max(l, 0) for l in lens]))
+        new = [rows(g, B, n, nkv, d) for _ in range(2)]
+        fits = [max(l, 0) if l + n <= max_seq else max_seq - n for l in lens]
+        cache.sssd_kv8_append(layer, *new, ints(fits))
+        for b in range(B):
+            for i in range(2):
+                c = Cache(nkv, d, fmt, DEV)
+                c.append(0, x[i][b, :max(lens[b], 0)])
+                c.append(fits[b], new[i][b])
+                if b < len(PATHS):
+                    c.commit(lens[b], paths[b])
+                want.append(c.x)
+    path = torch.full((B, n), -1, dtype=torch.int32)
+    for b, p in enumerate(paths):
+        path[b, 0] = 0
+        path[b, 1:len(p) + 1] = torch.tensor(p, dtype=torch.int32)
+    accepted = [len(p) for p in PATHS] + [a for _, a, _ in bad]
+    dlens = ints(lens)
+    print(f"kv8 commit {fmt} {d} paged={paged}", flush=True)
+    cache.sssd_kv8_commit_tree(n, dlens, ints(accepted), path.to(DEV))
+    assert cache.sssd_kv8_sync() == SSSD_ENOSPACE
+    now = dlens.tolist()
+    assert now == [l + len(p) + 1 for l, p in zip(lens, PATHS)] + lens[len(PATHS):]
+    for layer in range(L):
+        kept = [now[b] if b < len(PATHS) else len(want[(layer * B + b) * 2]) for b in range(B)]
+        got = read_all(cache, layer, kept, max_seq)
+        for b in range(B):
+            for i in range(2):
+                assert torch.equal(got[i][b, :kept[b]].double(), want[(layer * B + b) * 2 + i][:kept[b]]), (layer, b, i)
+    # chains only advance
+    cache.sssd_kv8_commit_tree(4, dlens, ints([0, 1, 2, 3] + [0] * (B - 4)))
+    assert [a - b for a, b in zip(dlens.tolist(), now)][:4] == [1, 2, 3, 4]
+
+
+def test_pages_behind_four_gib():
+    """A pool of 5 GB whose last pages hold the sequence."""
+    pages = 5 * (1 << 30) // (8 * 64 * 128)
+    cache = kv8.Kv8Cache(1, 8, 8, 128, 1, 96, "e4m3", n_pages=pages, device=DEV)
+    cache.sssd_kv8_set_block_table(ints([[pages - 1, 0, pages - 2]]))
+    x = torch.randn(1, 80, 8, 128, device=DEV)
+    cache.sssd_kv8_append(0, x, x, ints([0]))
+    want = Cache(8, 128, "e4m3", DEV)
+    want.append(0, x[0])
+    k, v = read_all(cache, 0, [80], 80)
+    assert torch.equal(k[0].double(), want.x) and torch.equal(v, k)
+    assert cache.sssd_kv8_sync() == SSSD_OK
