@@ -12,6 +12,7 @@
 #pragma once
 #include "../../include/sssd_kv8.h"
 #include "common.h"
+#include "handover.h"
 
 typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
@@ -94,14 +95,14 @@ __device__ __forceinline__ bool kv8_rows(const int32_t *lens, const int32_t *cou
     return len >= 0 && count >= 0 && count <= n && (int64_t)len + count <= max_seq;
 }
 
-// The draft tree of one sequence, in lanes 0 .. n-1 of a wave (n <= 32): every lane's word of visible new rows, itself and its ancestors.
-// Five rounds of doubling: a lane adds what the row sees that it points to and points to where that one pointed.  bad: a parent
+// The draft tree of one sequence, in lanes 0 .. n-1 of a wave (n <= 32), each with its row's parent: every lane's word of visible new rows,
+// itself and its ancestors.  Five rounds of doubling: a lane adds what the row sees that it points to and points to where that one pointed.  bad: a parent
 // outside [0, lane), taken as lane - 1.
-__device__ __forceinline__ uint32_t kv8_tree_word(const int32_t *parents, int n, int lane, bool &bad)
+__device__ __forceinline__ uint32_t kv8_tree_word(int up, int n, int lane, bool &bad)
 {
-    int up = lane > 0 && lane < n ? parents[lane] : 0;
     bad = lane > 0 && lane < n && (up < 0 || up >= lane);
     if (bad) up = lane - 1;
+    if (lane == 0 || lane >= n) up = 0;
     uint32_t word = 1u << (lane & 31);
 #pragma unroll
     for (int i = 0; i < 5; ++i) {
@@ -153,6 +154,8 @@ hipError_t launch_kv8_commit(const Kv8StoreArgs &a, int fmt, int d, int layers, 
 // How the attention's work is cut: `share` segments of a sequence at most, `passes` over the cache for the 16-row tiles of queries.
 struct Kv8Plan {
     int passes, share;
+    int in_die;               // a (sequence, kv head)'s workgroups run on one die, where its segments can be merged inside the launch
+    int by_length, first_turns;   // sequences start longest first; those from turn first_turns on shortest first
 };
 constexpr int KV8_GROUPS = 512, KV8_MAX_TILES = 4;   // workgroups of a launch whose segments are merged, row tiles of a pass
 struct Kv8AttnArgs {
@@ -167,6 +170,7 @@ struct Kv8AttnArgs {
     float2 *part_ml;         // ... reference of the exponents (log2), sum of probabilities
     int rows_pad;            // rows of a (sequence, kv head) in whole tiles
     Kv8Plan plan;
+    Hand hand;               // words for segments merged inside the launch, or none
     int32_t *status;
 };
 Kv8Plan kv8_plan(int B, int n, int gq, int nkv);

@@ -1,6 +1,9 @@
 // Attention of a step's new rows over a KV cache in 8 bits.
 #include "kv8.h"
 
+#ifndef WGS
+#define WGS 256
+#endif
 namespace {
 
 __device__ __forceinline__ f32x4 mfma16(const half8_t &a, const half8_t &b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
@@ -112,32 +115,163 @@ __device__ __forceinline__ void store4(const Rows8 &o, char *row, int ch, const 
     }
 }
 
+// The segments of ROWS query rows r0, r0 + step, ... (below r_end) of a (sequence, kv head) merged by one wave, in fixed order: lanes
+// 16s .. 16s+15 take segments s, s+4, ... with HD/16 channels each, U of them in one round of independent loads.  MANY: in several rounds.
+// DIE: workgroups of this launch, on this die, stored them.
+template <int HD, int ROWS, int U, bool MANY, bool DIE>
+__device__ __forceinline__ void merge_rows(const Kv8AttnArgs &a, int b, int kvh, int r0, int step, int r_end, int n_seg, int lane)
+{
+    constexpr int E = HD / 16;
+    const int sg = lane >> 4, cl = lane & 15;
+    const size_t slot0 = ((size_t)b * a.g.nkv + kvh) * a.plan.share * a.rows_pad;
+    const float *part_o = a.part_o + slot0 * HD;
+    const float2 *part_ml = a.part_ml + slot0;
+    const DieBuffer die_o(part_o, (size_t)n_seg * a.rows_pad * HD * sizeof(float)), die_ml(part_ml, (size_t)n_seg * a.rows_pad * sizeof(float2));
+    auto row = [&](int i) { return min(r0 + i * step, r_end - 1); };
+    auto stats = [&](int s, int r) { return DIE ? die_ml.load2((s * a.rows_pad + r) * 8) : part_ml[s * a.rows_pad + r]; };
+    float num[ROWS][E], den[ROWS], m_all[ROWS];
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        m_all[i] = NEG_BIG;
+        if (MANY)
+            for (int s = lane; s < n_seg; s += 64) m_all[i] = fmaxf(m_all[i], stats(s, row(i)).x);
+        den[i] = 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) num[i][e] = 0.f;
+    }
+    for (int base = 0; base < (MANY ? n_seg : 1); base += 4 * U) {
+        f32x4 pv[ROWS][U][E / 4];
+        float2 ml[ROWS][U];
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i)
+#pragma unroll
+            for (int u = 0; u < U; ++u) {   // past the last segment: that one again, not added
+                const int s = min(base + 4 * u + sg, n_seg - 1), at = (s * a.rows_pad + row(i)) * HD + cl * E;
+                ml[i][u] = stats(s, row(i));
+#pragma unroll
+                for (int e = 0; e < E; e += 4) pv[i][u][e / 4] = DIE ? die_o.load4(at * 4, e * 4) : *reinterpret_cast<const f32x4 *>(part_o + at + e);
+            }
+        if (base == 0) {
+#pragma unroll
+            for (int i = 0; i < ROWS; ++i) {
+                if (!MANY) {
+#pragma unroll
+                    for (int u = 0; u < U; ++u) m_all[i] = fmaxf(m_all[i], ml[i][u].x);
+                    m_all[i] = rows_max(m_all[i]);
+                } else {
+#pragma unroll
+                    for (int x = 32; x > 0; x >>= 1) m_all[i] = fmaxf(m_all[i], __shfl_xor(m_all[i], x));
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i)
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const bool on = base + 4 * u + sg < n_seg;
+                const float w = on ? __builtin_amdgcn_exp2f(ml[i][u].x - m_all[i]) : 0.f;
+                den[i] = on ? __builtin_fmaf(w, ml[i][u].y, den[i]) : den[i];
+#pragma unroll
+                for (int e = 0; e < E; ++e) num[i][e] = on ? __builtin_fmaf(w, pv[i][u][e / 4][e % 4], num[i][e]) : num[i][e];
+            }
+    }
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        den[i] = rows_sum(den[i]);
+        const float inv = den[i] != 0.f ? 1.f / den[i] : 0.f;   // a row that sees nothing: 0
+        const int r = r0 + i * step;
+        if (r >= r_end) continue;
+        const RowOut o(r, a.gq, kvh);
+        char *to = a.out.at(b, o.j, o.head);
+#pragma unroll
+        for (int e = 0; e < E; e += 4) {
+            f32x4 y;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) y[x] = rows_sum(num[i][e + x]) * inv;
+            if (sg == e / 4) store4(a.out, to, cl * E + e, y);
+        }
+    }
+}
+
+// Sequence `rank` of the batch by length, longest first, equal ones in their order; B <= 64.
+__device__ __forceinline__ int sequence_of_rank(const Kv8AttnArgs &a, int rank, int lane)
+{
+    int len = 0, count = 0;
+    const int b = min(lane, a.B - 1);
+    const bool ok = kv8_rows(a.lens, a.counts, b, a.n, a.g.max_seq, len, count);
+    const int mine = ok ? len + count : 0;
+    int before = 0;
+    for (int j = 0; j < a.B; ++j) {
+        const int x = __builtin_amdgcn_readlane(mine, j);
+        before += x > mine || (x == mine && j < lane);
+    }
+    return (int)__builtin_ctzll(__ballot(lane < a.B && before == rank));
+}
+
+// Positions t0 .. t0+31 that a row sees, bit by bit: the old ones from `low` on (or among the first), of the new ones those of its word.
+__device__ __forceinline__ uint32_t visible(int t0, int len, int low, int sinks, uint32_t word)
+{
+    auto below = [](int x) { return x <= 0 ? 0u : x >= 32 ? ~0u : (1u << x) - 1u; };
+    const int at = t0 - len;
+    const uint32_t old = below(-at) & (~below(low - t0) | below(sinks - t0));
+    const uint32_t fresh = at >= 32 ? 0u : at >= 0 ? word >> at : at > -32 ? word << -at : 0u;
+    return old | fresh;
+}
+
 // PARTS: the query operand is float16 (1: bf16 queries) or float16 hi + lo (2: float32 queries), and so are the probabilities.
+// grid: workgroups of one (sequence, kv head) have block indexes of one residue modulo 8: its segments, and their passes next to each other.
 template <int HD, int FMT, int RT, int PARTS>
 __global__ __launch_bounds__(NWAVE * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void kv8_attn_kernel(Kv8AttnArgs a)
 {
-    constexpr int KS = HD / 32, DT = HD / 16, QT = DT / 4, TR = RT <= 2 ? RT : 2;
+    constexpr int KS = HD / 32, DT = HD / 16, QT = DT / 4, TR = RT <= 3 ? RT : 2;
     constexpr int QREC = RT * KS * PARTS * 64, RRED = NWAVE * (NWAVE - 1) * TR * QT * 64;
     __shared__ u32x4 lds[QREC > RRED ? QREC : RRED];
     __shared__ float row_scale_s[RT * 16];
     __shared__ uint32_t word_s[RT * 16];
-    __shared__ int low_s[RT * 16], depth_s[32];
+    __shared__ int low_s[RT * 16], way_s;
     __shared__ float2 ml_s[NWAVE][RT * 16];
     __shared__ float vref_s[NWAVE];
 
     const int passes = a.plan.passes, share = a.plan.share, nkv = a.g.nkv;
-    uint32_t id = blockIdx.x;
-    const int pass = (int)(id % (uint32_t)passes);
-    id /= (uint32_t)passes;
-    const int segment = (int)(id % (uint32_t)share);
-    id /= (uint32_t)share;
-    const int b = (int)(id / (uint32_t)nkv), kvh = (int)id - b * nkv;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int q = lane >> 4, c = lane & 15;
-    int len, count;
-    const bool ok = kv8_rows(a.lens, a.counts, b, a.n, a.g.max_seq, len, count);
+    int pass, segment, turn, kvh;
+    {
+        const uint32_t slot = blockIdx.x >> 3, x = slot / (uint32_t)passes, row = x / (uint32_t)share;
+        pass = (int)(slot - x * passes);
+        segment = (int)(x - row * share);
+        const uint32_t u = row * 8 + ((blockIdx.x - row) & 7);   // heads rotate over the dies
+        turn = (int)(u / (uint32_t)nkv);
+        kvh = (int)u - turn * nkv;
+    }
+    if (turn >= a.B) return;   // groups are in whole eights
+    int b = turn;
+    if (a.plan.by_length) b = sequence_of_rank(a, turn < a.plan.first_turns ? turn : a.B - 1 - (turn - a.plan.first_turns), lane);
     const int rt0 = pass * RT;
-    if (!ok) {   // zeros
+
+    // A thread's share of the queries is requested ahead of everything that depends on lens: eight channels of a row at a time.
+    constexpr int TPR = HD / 8, RPP = NWAVE * 64 / TPR, QN = (RT * 16 + RPP - 1) / RPP;   // threads of a row, rows at a time
+    const int q_part = threadIdx.x % TPR, q_row = threadIdx.x / TPR;
+    float qx[QN][8];
+    u32x4 qv[QN][PARTS];
+#pragma unroll
+    for (int i = 0; i < QN; ++i) {
+        const RowOut o(min(rt0 * 16 + i * RPP + q_row, a.n * a.gq - 1), a.gq, kvh);   // past the last: that one again, used by no row
+        const char *row = a.q.at(b, o.j, o.head);
+        if (a.q.vec) {
+#pragma unroll
+            for (int x = 0; x < PARTS; ++x) qv[i][x] = *reinterpret_cast<const u32x4 *>(row + q_part * 16 * PARTS + x * 16);
+        } else {
+#pragma unroll
+            for (int x = 0; x < 8; ++x)
+                qx[i][x] = PARTS == 1 ? bf16_to_f32(reinterpret_cast<const uint16_t *>(row)[q_part * 8 + x]) : reinterpret_cast<const float *>(row)[q_part * 8 + x];
+        }
+    }
+    int up = lane - 1;
+    if (a.parents && lane < a.n) up = a.parents[(size_t)b * a.n + lane];
+
+    int len, count;
+    if (!kv8_rows(a.lens, a.counts, b, a.n, a.g.max_seq, len, count)) {   // zeros
         if (segment == 0) {
             if (kvh == 0 && pass == 0 && threadIdx.x == 0) atomicOr(a.status, KV8_RANGE);
             for (int i = threadIdx.x; i < RT * 16 * (HD / 4); i += NWAVE * 64) {
@@ -171,7 +305,7 @@ __global__ __launch_bounds__(NWAVE * 64) __attribute__((amdgpu_waves_per_eu(2, 2
         return x;
     };
     int chunk = 0;
-    Ahead now = look(0), next = look(1);
+    Ahead now = look(0), next = now;
 
     constexpr int KR = HD / 32, VR = HD / 32;   // 16-byte records of a lane
     u32x4 k[KR], v[VR];
@@ -192,69 +326,66 @@ __global__ __launch_bounds__(NWAVE * 64) __attribute__((amdgpu_waves_per_eu(2, 2
     };
     load_k(0);
     load_v(0);
+    if (n_it > 64) next = look(1);
 
     // Query operands: a row's channels times a power of two that brings its largest below 2^15, as float16.
-    {
-        constexpr int TPR = HD / 8, RPP = NWAVE * 64 / TPR;   // threads of a row, rows at a time
-        const int part = threadIdx.x % TPR;
 #pragma unroll
-        for (int r0 = 0; r0 < RT * 16; r0 += RPP) {
-            const int r = r0 + (int)threadIdx.x / TPR;
-            float x[8];
+    for (int i = 0; i < QN; ++i) {
+        const int r = i * RPP + q_row;
+        if (a.q.vec) {
+            if (PARTS == 1) {
+                unpack_bf16x8(qv[i][0], qx[i]);
+            } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = 0.f;
-            if (rt0 * 16 + r < rows) {
-                const RowOut o(rt0 * 16 + r, a.gq, kvh);
-                load8(a.q, a.q.at(b, o.j, o.head), part * 8, x);
+                for (int x = 0; x < 8; ++x) qx[i][x] = bits_f32(qv[i][PARTS == 2 ? x >> 2 : 0][x & 3]);
             }
-            float most = 0.f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(x[i]));
-#pragma unroll
-            for (int i = TPR / 2; i > 0; i >>= 1) most = fmaxf(most, __shfl_xor(most, i));
-            const int e = (int)(f32_bits(most) >> 23);   // 2^(e-127) <= most < 2^(e-126)
-            const int up = e == 0 || e == 255 ? 127 : min(268 - e, 253);   // biased exponent of the factor, 2^(141-e)
-            const float f = bits_f32((uint32_t)up << 23);
-            u32x4 hi, lo;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint32_t h, l;
-                if (PARTS == 2) split_half2(x[2 * i] * f, x[2 * i + 1] * f, h, l);
-                else h = pack_half2(x[2 * i] * f, x[2 * i + 1] * f), l = 0;
-                hi[i] = h;
-                lo[i] = l;
-            }
-            if (r >= RT * 16) continue;   // an odd tile of 64 channels
-            const int rec = (((r >> 4) * KS + (part >> 2)) * PARTS) * 64 + (part & 3) * 16 + (r & 15);
-            lds[rec] = hi;
-            if (PARTS == 2) lds[rec + 64] = lo;
-            if (part == 0) row_scale_s[r] = bits_f32((uint32_t)(254 - up) << 23);
         }
+        float most = 0.f;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) most = fmaxf(most, fabsf(qx[i][x]));
+#pragma unroll
+        for (int x = TPR / 2; x > 0; x >>= 1) most = fmaxf(most, __shfl_xor(most, x));
+        const int e = (int)(f32_bits(most) >> 23);   // 2^(e-127) <= most < 2^(e-126)
+        const int to = e == 0 || e == 255 ? 127 : min(268 - e, 253);   // biased exponent of the factor, 2^(141-e)
+        const float f = bits_f32((uint32_t)to << 23);
+        u32x4 hi, lo;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            uint32_t h, l = 0;
+            if (PARTS == 2) split_half2(qx[i][2 * x] * f, qx[i][2 * x + 1] * f, h, l);
+            else h = pack_half2(qx[i][2 * x] * f, qx[i][2 * x + 1] * f);
+            hi[x] = h;
+            lo[x] = l;
+        }
+        if (QN * RPP > RT * 16 && r >= RT * 16) continue;   // an odd tile of 64 channels
+        const int rec = (((r >> 4) * KS + (q_part >> 2)) * PARTS) * 64 + (q_part & 3) * 16 + (r & 15);
+        lds[rec] = hi;
+        if (PARTS == 2) lds[rec + 64] = lo;
+        if (q_part == 0) row_scale_s[r] = bits_f32((uint32_t)(254 - to) << 23);
     }
     // What the rows see of the new ones, and where their windows begin.
-    {
-        bool bad = false;
-        uint32_t word = a.parents ? kv8_tree_word(a.parents + (size_t)b * a.n, count, lane, bad) : kv8_chain_word(lane & 31);
-        if (segment == 0 && kvh == 0 && pass == 0 && wave == 0 && __any(bad) && lane == 0) atomicOr(a.status, KV8_RANGE);
+    if (wave == 0) {
+        uint32_t word = kv8_chain_word(lane & 31);
+        if (a.parents) {
+            bool bad;
+            word = kv8_tree_word(up, count, lane, bad);
+            if (segment == 0 && kvh == 0 && pass == 0 && __any(bad) && lane == 0) atomicOr(a.status, KV8_RANGE);
+        }
         const int depth = __popc(word) - 1;
-        if (wave == 0 && lane < 32) depth_s[lane] = depth;
         if (a.window > 0 && a.window < count) {   // ancestors farther than the window go, but for those among the first positions
             uint32_t near = 0;
             for (int i = 0; i < count; ++i) {
-                const int d = __shfl(depth, i);
+                const int d = __builtin_amdgcn_readlane(depth, i);
                 if (depth - d < a.window || len + d < a.sinks) near |= 1u << i;
             }
             word &= near;
         }
-#pragma unroll
-        for (int t = 0; t < (RT * 16 + 63) / 64; ++t) {
-            const int r = t * 64 + lane, j = min(RowOut(rt0 * 16 + r, a.gq, kvh).j, 31);
-            const uint32_t w = (uint32_t)__shfl((int)word, j);
-            const int d = __shfl(depth, j);
-            if (wave == 0 && r < RT * 16) {
-                word_s[r] = w;
-                low_s[r] = a.window > 0 ? len + d - a.window + 1 : 0;
-            }
+        const int r = lane, j = min(RowOut(rt0 * 16 + r, a.gq, kvh).j, 31);
+        const uint32_t w = (uint32_t)__shfl((int)word, j);
+        const int d = __shfl(depth, j);
+        if (r < RT * 16) {
+            word_s[r] = w;
+            low_s[r] = a.window > 0 ? len + d - a.window + 1 : 0;
         }
     }
     __syncthreads();
@@ -263,15 +394,17 @@ __global__ __launch_bounds__(NWAVE * 64) __attribute__((amdgpu_waves_per_eu(2, 2
 #pragma unroll
     for (int t = 0; t < RT; ++t) row_scale[t] = row_scale_s[t * 16 + c] * soft;
 
-    f32x4 o[RT][DT];
-    float m_run[RT], l_run[RT], v_ref = 0.f;
+    f32x4 o[RT][DT], l_run[RT];   // l_run: sums of probabilities, by a product with ones: the same in every register of a lane's column
+    float m_run[RT];
+    int v_ref = -256;   // biased exponent of a scale; below all of them: none yet
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) o[t][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        l_run[t] = f32x4{0.f, 0.f, 0.f, 0.f};
         m_run[t] = NEG_BIG;
-        l_run[t] = 0.f;
     }
+    const half8_t ones = __builtin_bit_cast(half8_t, u32x4{0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u});
     const int all_from = a.window > 0 ? len + count - a.window : 0;   // every row sees the old positions from here on
 
     for (int i = 0; i < n_it; ++i) {
@@ -282,7 +415,9 @@ __global__ __launch_bounds__(NWAVE * 64) __attribute__((amdgpu_waves_per_eu(2, 2
         }
         const int t0 = span.block(first + wave + NWAVE * i) * 32;
         const float k_scale = bits_f32((uint32_t)__builtin_amdgcn_readlane((int)f32_bits(now.scale.x), i & 63));
-        const float v_scale = bits_f32((uint32_t)__builtin_amdgcn_readlane((int)f32_bits(now.scale.y), i & 63));
+        const int v_e = __builtin_amdgcn_readlane((int)f32_bits(now.scale.y), i & 63) >> 23 & 255;
+        int ql = lane;
+        if (RT * PARTS > 2) asm volatile("" : "+v"(ql));   // the query operands are read again for every block: hoisted, they would not fit the registers
         f32x4 s[RT][2];   // s[t][u][r]: position t0 + 16u + 4q + r for query row c of tile t
 #pragma unroll
         for (int t = 0; t < RT; ++t) s[t][0] = s[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -298,34 +433,29 @@ __global__ __launch_bounds__(NWAVE * 64) __attribute__((amdgpu_waves_per_eu(2, 2
             for (int t = 0; t < RT; ++t)
 #pragma unroll
                 for (int part = 0; part < PARTS; ++part) {
-                    const half8_t qq = __builtin_bit_cast(half8_t, lds[((t * KS + ks) * PARTS + part) * 64 + lane]);
+                    const half8_t qq = __builtin_bit_cast(half8_t, lds[((t * KS + ks) * PARTS + part) * 64 + ql]);
 #pragma unroll
                     for (int u = 0; u < 2; ++u) s[t][u] = mfma16(kk[u], qq, s[t][u]);
                 }
         }
         load_k(i + 1);
-        if (t0 + 32 > len || (t0 < all_from && t0 + 32 > a.sinks)) {   // not all of the block is seen by all rows
-#pragma unroll
-            for (int t = 0; t < RT; ++t) {
-                const uint32_t word = word_s[t * 16 + c];
-                const int low = low_s[t * 16 + c];
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int p = t0 + 16 * u + 4 * q + r, x = p - len;
-                        const bool sees = x < 0 ? p >= low || p < a.sinks : x < 32 && (word >> (x & 31) & 1u);
-                        if (!sees) s[t][u][r] = -INFINITY;
-                    }
-            }
-        }
-        float sc[RT], mx[RT];
+        const bool whole = t0 + 32 <= len && (t0 >= all_from || t0 + 32 <= a.sinks);   // all rows see all of the block
+        float mx[RT];
         bool grow = false;
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
-            sc[t] = row_scale[t] * k_scale;
-            float m = fmaxf(fmaxf(fmaxf(s[t][0][0], s[t][0][1]), fmaxf(s[t][0][2], s[t][0][3])), fmaxf(fmaxf(s[t][1][0], s[t][1][1]), fmaxf(s[t][1][2], s[t][1][3])));
-            mx[t] = rows_max(m) * sc[t];
+            const float sc = row_scale[t] * k_scale;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) s[t][u] *= sc;
+            if (!whole) {
+                const uint32_t mine = visible(t0, len, low_s[t * 16 + c], a.sinks, word_s[t * 16 + c]) >> (4 * q);
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) s[t][u][r] = mine & (1u << (16 * u + r)) ? s[t][u][r] : -INFINITY;
+            }
+            const float m = fmaxf(fmaxf(fmaxf(s[t][0][0], s[t][0][1]), fmaxf(s[t][0][2], s[t][0][3])), fmaxf(fmaxf(s[t][1][0], s[t][1][1]), fmaxf(s[t][1][2], s[t][1][3])));
+            mx[t] = rows_max(m);
             grow = grow || mx[t] > m_run[t] + REF_MOST;
         }
         if (__any(grow)) {
@@ -333,33 +463,27 @@ __global__ __launch_bounds__(NWAVE * 64) __attribute__((amdgpu_waves_per_eu(2, 2
             for (int t = 0; t < RT; ++t) {
                 const float m_new = mx[t] > m_run[t] + REF_MOST ? mx[t] - REF_BELOW : m_run[t], alpha = __builtin_amdgcn_exp2f(m_run[t] - m_new);
                 m_run[t] = m_new;
-                if (i == 0) continue;
                 l_run[t] *= alpha;
 #pragma unroll
                 for (int dt = 0; dt < DT; ++dt) o[t][dt] *= alpha;
             }
         }
-        // The sums are in units of v_ref, a V scale: they move to a larger one only when a block's outgrows it by 2^4.
-        if (v_scale > 16.f * v_ref) {
-            const float down = v_ref / v_scale;   // powers of two
-            if (i > 0) {
+        // The sums are in units of 2^(v_ref - 127), a V scale: they move to a larger one only when a block's outgrows it by 2^4.
+        if (v_e > v_ref + 4) {
+            const float down = bits_f32((uint32_t)max(v_ref - v_e + 127, 0) << 23);
 #pragma unroll
-                for (int t = 0; t < RT; ++t)
+            for (int t = 0; t < RT; ++t)
 #pragma unroll
-                    for (int dt = 0; dt < DT; ++dt) o[t][dt] *= down;
-            }
-            v_ref = v_scale;
+                for (int dt = 0; dt < DT; ++dt) o[t][dt] *= down;
+            v_ref = v_e;
         }
-        const float ratio = v_scale / v_ref;
+        const float ratio = bits_f32((uint32_t)max(v_e - v_ref + 127, 0) << 23);
         u32x4 pk[RT][PARTS];
 #pragma unroll
         for (int t = 0; t < RT; ++t)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e >> 1][2 * (e & 1)], sc[t], -m_run[t]));
-                const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e >> 1][2 * (e & 1) + 1], sc[t], -m_run[t]));
-                l_run[t] += p0;
-                l_run[t] += p1;
+                const float p0 = __builtin_amdgcn_exp2f(s[t][e >> 1][2 * (e & 1)] - m_run[t]), p1 = __builtin_amdgcn_exp2f(s[t][e >> 1][2 * (e & 1) + 1] - m_run[t]);
                 uint32_t hi, lo;
                 if (PARTS == 2) {
                     split_half2(p0, p1, hi, lo);
@@ -369,6 +493,10 @@ __global__ __launch_bounds__(NWAVE * 64) __attribute__((amdgpu_waves_per_eu(2, 2
                 }
                 pk[t][0][e] = hi;
             }
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+#pragma unroll
+            for (int part = 0; part < PARTS; ++part) l_run[t] = mfma16(ones, __builtin_bit_cast(half8_t, pk[t][part]), l_run[t]);
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) {
             const u32x4 &w = v[dt >> 1];
@@ -387,11 +515,9 @@ __global__ __launch_bounds__(NWAVE * 64) __attribute__((amdgpu_waves_per_eu(2, 2
     f32x4 own[RT][QT];
     __syncthreads();   // the query operands have been read
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        l_run[t] = rows_sum(l_run[t]);
-        if (q == 0) ml_s[wave][t * 16 + c] = float2{m_run[t], l_run[t]};
-    }
-    if (lane == 0) vref_s[wave] = v_ref;
+    for (int t = 0; t < RT; ++t)
+        if (q == 0) ml_s[wave][t * 16 + c] = float2{m_run[t], l_run[t][0]};
+    if (lane == 0) vref_s[wave] = v_ref < 0 ? 0.f : bits_f32((uint32_t)v_ref << 23);
 #pragma unroll
     for (int w = 0; w < NWAVE; ++w)
         if (w == wave)
@@ -450,9 +576,32 @@ __global__ __launch_bounds__(NWAVE * 64) __attribute__((amdgpu_waves_per_eu(2, 2
             }
         }
     }
+    if (cut.n == 1 || !a.hand.words) return;
+    const int group = (turn * nkv + kvh) * passes + pass;   // by turn, not by sequence: both count to B
+    HandWay way = hand_wait(a.hand, group, cut.n, hand_arrive(a.hand, group), &way_s);
+    if (way == HAND_TURN_IN) way = hand_turn_in(a.hand, group, cut.n, &way_s);
+    uint64_t left = way == HAND_SHARE ? hand_leave(a.hand, group) : 0;   // under way while the shares are done
+    if (way != HAND_NOTHING) {   // the rows of this pass shared out over the waves of all segments
+        const int r_end = min(rows, (rt0 + RT) * 16), step = (way == HAND_ALL ? 1 : cut.n) * NWAVE;
+        int r = rt0 * 16 + (way == HAND_ALL ? wave : wave * cut.n + segment);
+        // as many rows at once as the wave has, up to four, when they have few segments
+#define KV8_MERGE(ROWS, U, MANY) for (; r < r_end; r += ROWS * step) merge_rows<HD, ROWS, U, MANY, true>(a, b, kvh, r, step, r_end, cut.n, lane)
+        if (cut.n > 8) KV8_MERGE(1, 5, true);
+        else if (cut.n > 4) {
+            if (r + step < r_end) KV8_MERGE(2, 2, false);
+            else KV8_MERGE(1, 2, false);
+        } else {
+            if (r + 2 * step < r_end) KV8_MERGE(4, 1, false);
+            else if (r + step < r_end) KV8_MERGE(2, 1, false);
+            else KV8_MERGE(1, 1, false);
+        }
+#undef KV8_MERGE
+    }
+    if (way != HAND_SHARE) left = hand_leave(a.hand, group);
+    hand_clear(a.hand, group, cut.n, left);
 }
 
-// One wave per query row: lanes 16s .. 16s+15 take segments s, s+4, ...
+// The merge as a launch of its own, where a group's segments are not on one die: one wave per query row.
 template <int HD> __global__ __launch_bounds__(256) void kv8_merge_kernel(Kv8AttnArgs a, int R)
 {
     const uint32_t task = blockIdx.x * 4 + (threadIdx.x >> 6), nkv = a.g.nkv;
@@ -461,44 +610,12 @@ template <int HD> __global__ __launch_bounds__(256) void kv8_merge_kernel(Kv8Att
     int len, count;
     if (!kv8_rows(a.lens, a.counts, b, a.n, a.g.max_seq, len, count) || r >= count * a.gq) return;
     const Cut cut = cut_of(span_of(len, count, a.window, a.sinks).n, a.plan.share);
-    if (cut.n == 1) return;
-    const int lane = threadIdx.x & 63, sg = lane >> 4, cl = lane & 15;
-    constexpr int E = HD / 16;   // channels of a lane
-    const size_t slot = ((size_t)b * nkv + kvh) * a.plan.share * a.rows_pad + r;
-    float m = NEG_BIG;
-    for (int s = sg; s < cut.n; s += 4) m = fmaxf(m, a.part_ml[slot + (size_t)s * a.rows_pad].x);
-    m = rows_max(m);
-    float den = 0.f, num[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) num[e] = 0.f;
-    for (int s = sg; s < cut.n; s += 4) {
-        const size_t at = slot + (size_t)s * a.rows_pad;
-        const float2 ml = a.part_ml[at];
-        const float w = __builtin_amdgcn_exp2f(ml.x - m);
-        den += w * ml.y;
-#pragma unroll
-        for (int e = 0; e < E; e += 4) {
-            const f32x4 x = *reinterpret_cast<const f32x4 *>(a.part_o + at * HD + cl * E + e);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) num[e + i] += w * x[i];
-        }
-    }
-    den = rows_sum(den);
-    const float inv = den != 0.f ? 1.f / den : 0.f;
-    const RowOut o(r, a.gq, kvh);
-    char *to = a.out.at(b, o.j, o.head);
-#pragma unroll
-    for (int e = 0; e < E; e += 4) {
-        f32x4 y;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] = rows_sum(num[e + i]) * inv;
-        if (sg == e / 4) store4(a.out, to, cl * E + e, y);
-    }
+    if (cut.n > 1) merge_rows<HD, 1, 5, true, false>(a, b, kvh, r, 1, r + 1, cut.n, threadIdx.x & 63);
 }
 
 template <int HD, int FMT, int PARTS> hipError_t launch_parts(const Kv8AttnArgs &a, int rt, hipStream_t s)
 {
-    const dim3 grid((uint32_t)a.B * a.g.nkv * a.plan.share * a.plan.passes), block(NWAVE * 64);
+    const dim3 grid(((uint32_t)a.B * a.g.nkv + 7) / 8 * 8 * a.plan.share * a.plan.passes), block(NWAVE * 64);
     switch (rt) {
     case 1: hipLaunchKernelGGL((kv8_attn_kernel<HD, FMT, 1, PARTS>), grid, block, 0, s, a); break;
     case 2: hipLaunchKernelGGL((kv8_attn_kernel<HD, FMT, 2, PARTS>), grid, block, 0, s, a); break;
@@ -512,7 +629,7 @@ template <int HD> hipError_t launch_hd(const Kv8AttnArgs &a, int fmt, int rt, hi
     hipError_t e;
     if (fmt == SSSD_KV8_E4M3) e = a.q.bf16 ? launch_parts<HD, SSSD_KV8_E4M3, 1>(a, rt, s) : launch_parts<HD, SSSD_KV8_E4M3, 2>(a, rt, s);
     else e = a.q.bf16 ? launch_parts<HD, SSSD_KV8_INT8, 1>(a, rt, s) : launch_parts<HD, SSSD_KV8_INT8, 2>(a, rt, s);
-    if (e != hipSuccess || a.plan.share == 1) return e;
+    if (e != hipSuccess || a.plan.share == 1 || a.hand.words) return e;
     const int R = a.n * a.gq;
     hipLaunchKernelGGL(kv8_merge_kernel<HD>, dim3(((uint32_t)a.B * a.g.nkv * R + 3) / 4), dim3(256), 0, s, a, R);
     return hipGetLastError();
@@ -525,12 +642,16 @@ Kv8Plan kv8_plan(int B, int n, int gq, int nkv)
     const int tiles = (n * gq + 15) / 16;
     Kv8Plan p;
     p.passes = (tiles + KV8_MAX_TILES - 1) / KV8_MAX_TILES;
-    const int64_t units = (int64_t)B * nkv * p.passes, share = 256 / units;
+    const int64_t units = (int64_t)B * nkv * p.passes, share = WGS / units;
     p.share = share < 1 ? 1 : share > 64 ? 64 : (int)share;
+    p.in_die = B * nkv % 8 == 0 && units <= HAND_GROUPS;
+    p.by_length = B > 1 && B <= 64 && nkv % 8 == 0;
+    const int slots = nkv / 8 * p.share * p.passes;   // of a sequence on a die, which takes 32 workgroups at once
+    p.first_turns = p.by_length && slots * B > 32 && slots * B <= 64 ? (32 + slots - 1) / slots : B;
     return p;
 }
 
-size_t kv8_attention_ws(int d) { return (size_t)KV8_GROUPS * KV8_MAX_TILES * 16 * (d * sizeof(float) + sizeof(float2)); }
+size_t kv8_attention_ws(int d) { return HAND_WORDS + (size_t)KV8_GROUPS * KV8_MAX_TILES * 16 * (d * sizeof(float) + sizeof(float2)); }
 
 hipError_t launch_kv8_attention(Kv8AttnArgs a, int fmt, int d, void *ws, hipStream_t s)
 {
@@ -538,7 +659,8 @@ hipError_t launch_kv8_attention(Kv8AttnArgs a, int fmt, int d, void *ws, hipStre
     a.plan = kv8_plan(a.B, a.n, a.gq, a.g.nkv);
     const int rt = (tiles + a.plan.passes - 1) / a.plan.passes;
     a.rows_pad = tiles * 16;
-    a.part_o = reinterpret_cast<float *>(ws);
+    a.hand = Hand{a.plan.share > 1 && a.plan.in_die ? (uint64_t *)ws : nullptr, nullptr, HAND_POLLS};
+    a.part_o = reinterpret_cast<float *>((char *)ws + HAND_WORDS);
     a.part_ml = reinterpret_cast<float2 *>(a.part_o + (size_t)KV8_GROUPS * KV8_MAX_TILES * 16 * d);
     return d == 128 ? launch_hd<128>(a, fmt, rt, s) : launch_hd<64>(a, fmt, rt, s);
 }

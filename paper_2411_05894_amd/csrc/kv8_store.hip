@@ -352,7 +352,7 @@ template <int HD, int FMT> __global__ __launch_bounds__(2 * HD) void append_kern
         int dep = j;
         if (a.parents) {
             bool bad;
-            const uint32_t word = kv8_tree_word(a.parents + (size_t)b * a.n, count, lane, bad);
+            const uint32_t word = kv8_tree_word(lane < count ? a.parents[(size_t)b * a.n + lane] : 0, count, lane, bad);
             if (step == 0 && h == 0 && threadIdx.x < 64 && __any(bad) && lane == 0) atomicOr(a.status, KV8_RANGE);
             dep = __popc((uint32_t)__shfl((int)word, j & 31)) - 1;
         }
