@@ -57,19 +57,31 @@ def _lib() -> C.CDLL:
     return _bound
 
 
-def _rows(t: torch.Tensor, device: torch.device) -> Rows:
-    """[B][n][heads][channels] as the C ABI takes them."""
-    assert t.dim() == 4 and t.dtype in TYPES, "rows are [B][n][heads][head_dim], float32 or bfloat16"
-    assert t.device == device, f"rows on {t.device}, the cache (or the frequencies) on {device}"
-    assert t.stride(3) == 1 or t.shape[3] == 1, "a head's channels must lie in a row"
-    return Rows(t.data_ptr(), TYPES[t.dtype], t.stride(0), t.stride(1), t.stride(2))
+def _rows(t: torch.Tensor, device: int) -> Rows:
+    """[B][n][heads][channels] as the C ABI takes them; device: the number of the GPU, -1 for none."""
+    stride = t.stride()
+    assert len(stride) == 4 and t.dtype in TYPES, "rows are [B][n][heads][head_dim], float32 or bfloat16"
+    assert t.get_device() == device, f"rows on {t.device}, the cache (or the frequencies) on GPU {device}"
+    assert stride[3] == 1 or t.shape[3] == 1, "a head's channels must lie in a row"
+    return Rows(t.data_ptr(), TYPES[t.dtype], stride[0], stride[1], stride[2])
 
 
-def _ints(t: Optional[torch.Tensor], shape, device: torch.device) -> Optional[int]:
+def _ints(t: Optional[torch.Tensor], shape, device: int) -> Optional[int]:
     if t is None:
         return None
-    assert t.dtype == torch.int32 and tuple(t.shape) == tuple(shape) and t.device == device, f"int32 {tuple(shape)} on {device}"
-    return _ptr(t)
+    assert t.dtype is torch.int32 and t.shape == shape and t.get_device() == device and t.is_contiguous(), f"int32 {shape} on GPU {device}"
+    return t.data_ptr()
+
+
+def _enqueue(name: str, device: int, *args) -> None:
+    """The call on the current stream of `device`, whichever device is the current one."""
+    f = getattr(_lib(), name)
+    if torch.cuda.current_device() == device:
+        code = f(*args, torch._C._cuda_getCurrentRawStream(device))
+    else:
+        with torch.cuda.device(device):
+            code = f(*args, torch._C._cuda_getCurrentRawStream(device))
+    _check(code, name)
 
 
 def sssd_kv8_sizes(cfg: Kv8Config):
@@ -93,20 +105,21 @@ class Rope:
     def __init__(self, rotary_dims: int, base: float, interleaved: bool = False, magnitude: float = 1.0, device: str = "cuda:0", **scaling):
         self.turns = sssd_rope_frequencies(rotary_dims, base, **scaling).to(device)
         self.args = RopeArgs(self.turns.data_ptr(), rotary_dims, int(interleaved), magnitude)
+        self.ref, self.device = C.byref(self.args), self.turns.get_device()
 
 
 def sssd_op_rope(x: torch.Tensor, positions: torch.Tensor, rope: Rope, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """x [rows][heads][head_dim] with positions [rows], or [B][n][heads][head_dim] with [B][n]; out may be x."""
-    device = rope.turns.device
     if out is None:
         out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
     assert out.shape == x.shape and out.dtype == x.dtype
-    four = (lambda t: t.unsqueeze(0)) if x.dim() == 3 else (lambda t: t)
-    a, b = four(x), four(out)
-    B, n, heads, d = a.shape
-    with torch.cuda.device(device):
-        _check(_lib().sssd_op_rope(C.byref(_rows(a, device)), C.byref(_rows(b, device)), B, n, heads, d, _ints(positions, x.shape[:-2], device),
-                                   C.byref(rope.args), torch.cuda.current_stream().cuda_stream), "sssd_op_rope")
+    at = _ints(positions, x.shape[:-2], rope.device)
+    if x.dim() == 3:
+        x, y = x.unsqueeze(0), out.unsqueeze(0)
+    else:
+        y = out
+    B, n, heads, d = x.shape
+    _enqueue("sssd_op_rope", rope.device, C.byref(_rows(x, rope.device)), C.byref(_rows(y, rope.device)), B, n, heads, d, at, rope.ref)
     return out
 
 
@@ -120,17 +133,14 @@ class Kv8Cache:
         self.cache = torch.zeros(cache_bytes, dtype=torch.uint8, device=device)
         self.workspace = torch.zeros(ws_bytes, dtype=torch.uint8, device=device)
         self.status = torch.zeros(1, dtype=torch.int32, device=device)
-        self.device = self.cache.device
+        self.device = self.cache.get_device()
         self._block_table = None
         self.args = Kv8(self.cfg, _ptr(self.cache), cache_bytes, _ptr(self.workspace), ws_bytes, None, _ptr(self.status))
+        self._ref = C.byref(self.args)
 
-    def _call(self, name: str, *args) -> None:
-        with torch.cuda.device(self.device):
-            _check(getattr(_lib(), name)(C.byref(self.args), *args, torch.cuda.current_stream().cuda_stream), name)
-
-    def _heads(self, t: torch.Tensor, heads: int) -> Rows:
-        assert tuple(t.shape[2:]) == (heads, self.cfg.head_dim), f"{tuple(t.shape)}: {heads} heads of {self.cfg.head_dim} channels are wanted"
-        return _rows(t, self.device)
+    def _heads(self, t: torch.Tensor, heads: int):
+        assert t.shape[2:] == (heads, self.cfg.head_dim), f"{tuple(t.shape)}: {heads} heads of {self.cfg.head_dim} channels are wanted"
+        return C.byref(_rows(t, self.device))
 
     def sssd_kv8_set_block_table(self, block_table: Optional[torch.Tensor]) -> None:
         """The table is read on the device when each later call executes; None: contiguous runs of pages."""
@@ -140,39 +150,39 @@ class Kv8Cache:
     def sssd_kv8_append(self, layer: int, k: torch.Tensor, v: torch.Tensor, lens: torch.Tensor, counts: Optional[torch.Tensor] = None,
                         first: int = 0, rope: Optional[Rope] = None, parents: Optional[torch.Tensor] = None,
                         q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> None:
-        B, n = k.shape[:2]
-        assert v.shape == k.shape and v.dtype == k.dtype
-        assert rope is None or rope.turns.device == self.device
-        kk, vv = self._heads(k, self.cfg.n_kv_heads), self._heads(v, self.cfg.n_kv_heads)
-        qs = [None, None]
+        B, n, nkv, _ = k.shape
+        assert v.shape == k.shape and v.dtype == k.dtype and nkv == self.cfg.n_kv_heads
+        turn = None
+        if rope is not None:
+            assert rope.device == self.device
+            turn = rope.ref
+        qq = to = None
         if q is not None:
-            assert q_out is not None and q.shape == q_out.shape and q.dtype == q_out.dtype and q.shape[:2] == k.shape[:2]
-            qs = [C.byref(self._heads(t, self.cfg.n_q_heads)) for t in (q, q_out)]
-        self._call("sssd_kv8_append", layer, first, B, n, C.byref(kk), C.byref(vv), _ints(lens, (B,), self.device),
-                   _ints(counts, (B,), self.device), C.byref(rope.args) if rope is not None else None, _ints(parents, (B, n), self.device), *qs)
+            assert q_out is not None and q.shape == q_out.shape and q.dtype == q_out.dtype and q.shape[:2] == (B, n)
+            qq, to = self._heads(q, self.cfg.n_q_heads), self._heads(q_out, self.cfg.n_q_heads)
+        _enqueue("sssd_kv8_append", self.device, self._ref, layer, first, B, n, self._heads(k, nkv), self._heads(v, nkv),
+                 _ints(lens, (B,), self.device), _ints(counts, (B,), self.device), turn, _ints(parents, (B, n), self.device), qq, to)
 
     def sssd_kv8_read(self, layer: int, start: Optional[torch.Tensor], counts: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
                       first: int = 0) -> None:
-        B, n = k.shape[:2]
-        assert v.shape == k.shape and v.dtype == k.dtype
-        kk, vv = self._heads(k, self.cfg.n_kv_heads), self._heads(v, self.cfg.n_kv_heads)
-        self._call("sssd_kv8_read", layer, first, B, n, _ints(start, (B,), self.device), _ints(counts, (B,), self.device), C.byref(kk),
-                   C.byref(vv))
+        B, n, nkv, _ = k.shape
+        assert v.shape == k.shape and v.dtype == k.dtype and nkv == self.cfg.n_kv_heads
+        _enqueue("sssd_kv8_read", self.device, self._ref, layer, first, B, n, _ints(start, (B,), self.device), _ints(counts, (B,), self.device),
+                 self._heads(k, nkv), self._heads(v, nkv))
 
     def sssd_kv8_attention(self, layer: int, q: torch.Tensor, lens: torch.Tensor, out: torch.Tensor, counts: Optional[torch.Tensor] = None,
                            parents: Optional[torch.Tensor] = None, window: int = 0, sinks: int = 0) -> None:
-        B, n = q.shape[:2]
-        assert out.shape == q.shape and out.dtype == q.dtype
-        qq, oo = self._heads(q, self.cfg.n_q_heads), self._heads(out, self.cfg.n_q_heads)
-        self._call("sssd_kv8_attention", layer, B, n, C.byref(qq), C.byref(oo), _ints(lens, (B,), self.device),
-                   _ints(counts, (B,), self.device), _ints(parents, (B, n), self.device), window, sinks)
+        B, n, nq, _ = q.shape
+        assert out.shape == q.shape and out.dtype == q.dtype and nq == self.cfg.n_q_heads
+        _enqueue("sssd_kv8_attention", self.device, self._ref, layer, B, n, self._heads(q, nq), self._heads(out, nq),
+                 _ints(lens, (B,), self.device), _ints(counts, (B,), self.device), _ints(parents, (B, n), self.device), window, sinks)
 
     def sssd_kv8_commit_tree(self, n: int, lens: torch.Tensor, accepted_len: torch.Tensor, accepted_path: Optional[torch.Tensor] = None) -> None:
         """n: rows of the step (accepted_path [B][n]); lens advances."""
         B = lens.numel()
-        self._call("sssd_kv8_commit_tree", B, n, _ints(lens, (B,), self.device), _ints(accepted_len, (B,), self.device),
-                   _ints(accepted_path, (B, n), self.device))
+        _enqueue("sssd_kv8_commit_tree", self.device, self._ref, B, n, _ints(lens, (B,), self.device), _ints(accepted_len, (B,), self.device),
+                 _ints(accepted_path, (B, n), self.device))
 
     def sssd_kv8_sync(self) -> int:
         with torch.cuda.device(self.device):
-            return _lib().sssd_kv8_sync(C.byref(self.args), torch.cuda.current_stream().cuda_stream)
+            return _lib().sssd_kv8_sync(self._ref, torch.cuda.current_stream().cuda_stream)
