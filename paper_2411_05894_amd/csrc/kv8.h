@@ -154,10 +154,9 @@ hipError_t launch_kv8_commit(const Kv8StoreArgs &a, int fmt, int d, int layers, 
 // How the attention's work is cut: `share` segments of a sequence at most, `passes` over the cache for the 16-row tiles of queries.
 struct Kv8Plan {
     int passes, share;
-    int in_die;               // a (sequence, kv head)'s workgroups run on one die, where its segments can be merged inside the launch
-    int by_length, first_turns;   // sequences start longest first; those from turn first_turns on shortest first
+    int in_die;   // a (sequence, kv head)'s workgroups run on one die, where its segments can be merged inside the launch
 };
-constexpr int KV8_GROUPS = 512, KV8_MAX_TILES = 4;   // workgroups of a launch whose segments are merged, row tiles of a pass
+constexpr int KV8_GROUPS = 512, KV8_MAX_TILES = 3;   // workgroups of a launch whose segments are merged, row tiles of a pass
 struct Kv8AttnArgs {
     Kv8Geom g;
     const uint8_t *codes;    // the layer

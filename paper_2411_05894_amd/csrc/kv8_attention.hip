@@ -1,9 +1,8 @@
 // Attention of a step's new rows over a KV cache in 8 bits.
 #include "kv8.h"
 
-#ifndef WGS
-#define WGS 256
-#endif
+#include <type_traits>
+
 namespace {
 
 __device__ __forceinline__ f32x4 mfma16(const half8_t &a, const half8_t &b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
@@ -29,6 +28,20 @@ __device__ __forceinline__ float rows_sum(float x)
     h = __builtin_amdgcn_permlane16_swap(f32_bits(x), f32_bits(x), false, false);
     return bits_f32(h[0]) + bits_f32(h[1]);
 }
+
+// max over 8 or 16 neighbouring lanes
+template <int N> __device__ __forceinline__ float row_max(float x)
+{
+    auto other = [&](auto ctrl) { return bits_f32((uint32_t)__builtin_amdgcn_mov_dpp((int)f32_bits(x), decltype(ctrl)::value, 0xF, 0xF, true)); };
+    x = fmaxf(x, other(std::integral_constant<int, 0xB1>()));          // lane ^ 1
+    x = fmaxf(x, other(std::integral_constant<int, 0x4E>()));          // lane ^ 2
+    x = fmaxf(x, other(std::integral_constant<int, 0x141>()));         // mirrored within eight
+    if (N == 16) x = fmaxf(x, other(std::integral_constant<int, 0x140>()));   // ... within sixteen
+    return x;
+}
+
+// v_maximum3_f32; fmaxf costs another instruction per score, because a product of matrices might leave a signalling NaN
+__device__ __forceinline__ float max3(float a, float b, float c) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c); }
 
 __device__ __forceinline__ uint32_t half2_bits(half2_t x) { return __builtin_bit_cast(uint32_t, x); }
 __device__ __forceinline__ uint32_t pack_half2(float a, float b)   // to nearest even
@@ -193,21 +206,6 @@ __device__ __forceinline__ void merge_rows(const Kv8AttnArgs &a, int b, int kvh,
     }
 }
 
-// Sequence `rank` of the batch by length, longest first, equal ones in their order; B <= 64.
-__device__ __forceinline__ int sequence_of_rank(const Kv8AttnArgs &a, int rank, int lane)
-{
-    int len = 0, count = 0;
-    const int b = min(lane, a.B - 1);
-    const bool ok = kv8_rows(a.lens, a.counts, b, a.n, a.g.max_seq, len, count);
-    const int mine = ok ? len + count : 0;
-    int before = 0;
-    for (int j = 0; j < a.B; ++j) {
-        const int x = __builtin_amdgcn_readlane(mine, j);
-        before += x > mine || (x == mine && j < lane);
-    }
-    return (int)__builtin_ctzll(__ballot(lane < a.B && before == rank));
-}
-
 // Positions t0 .. t0+31 that a row sees, bit by bit: the old ones from `low` on (or among the first), of the new ones those of its word.
 __device__ __forceinline__ uint32_t visible(int t0, int len, int low, int sinks, uint32_t word)
 {
@@ -235,18 +233,18 @@ __global__ __launch_bounds__(NWAVE * 64) __attribute__((amdgpu_waves_per_eu(2, 2
     const int passes = a.plan.passes, share = a.plan.share, nkv = a.g.nkv;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int q = lane >> 4, c = lane & 15;
-    int pass, segment, turn, kvh;
+    int pass, segment, b, kvh;
     {
         const uint32_t slot = blockIdx.x >> 3, x = slot / (uint32_t)passes, row = x / (uint32_t)share;
         pass = (int)(slot - x * passes);
         segment = (int)(x - row * share);
         const uint32_t u = row * 8 + ((blockIdx.x - row) & 7);   // heads rotate over the dies
-        turn = (int)(u / (uint32_t)nkv);
-        kvh = (int)u - turn * nkv;
+        b = (int)(u / (uint32_t)nkv);
+        kvh = (int)u - b * nkv;
     }
-    if (turn >= a.B) return;   // groups are in whole eights
-    int b = turn;
-    if (a.plan.by_length) b = sequence_of_rank(a, turn < a.plan.first_turns ? turn : a.B - 1 - (turn - a.plan.first_turns), lane);
+    if (b >= a.B) return;   // groups are in whole eights
+    int len, count;
+    const bool ok = kv8_rows(a.lens, a.counts, b, a.n, a.g.max_seq, len, count);
     const int rt0 = pass * RT;
 
     // A thread's share of the queries is requested ahead of everything that depends on lens: eight channels of a row at a time.
@@ -270,8 +268,7 @@ __global__ __launch_bounds__(NWAVE * 64) __attribute__((amdgpu_waves_per_eu(2, 2
     int up = lane - 1;
     if (a.parents && lane < a.n) up = a.parents[(size_t)b * a.n + lane];
 
-    int len, count;
-    if (!kv8_rows(a.lens, a.counts, b, a.n, a.g.max_seq, len, count)) {   // zeros
+    if (!ok) {   // zeros
         if (segment == 0) {
             if (kvh == 0 && pass == 0 && threadIdx.x == 0) atomicOr(a.status, KV8_RANGE);
             for (int i = threadIdx.x; i < RT * 16 * (HD / 4); i += NWAVE * 64) {
@@ -292,16 +289,17 @@ __global__ __launch_bounds__(NWAVE * 64) __attribute__((amdgpu_waves_per_eu(2, 2
 
     // Pages and scales of this wave's blocks: lane l keeps those of its block number 64 * chunk + l, one chunk ahead.
     struct Ahead {
-        int page;
+        int record;
         float2 scale;
     };
     auto look = [&](int chunk) {
         const int i = min(first + wave + NWAVE * (64 * chunk + lane), span.n - 1);
         Ahead x;
         const int entry = kv8_entry(a.g, b, span.block(i));
-        x.page = min(max(entry, 0), a.g.n_pages - 1);
-        if (entry != x.page && kvh == 0 && pass == 0) atomicOr(a.status, KV8_RANGE);
-        x.scale = a.scales[(size_t)x.page * nkv + kvh];
+        const int page = min(max(entry, 0), a.g.n_pages - 1);
+        if (entry != page && kvh == 0 && pass == 0) atomicOr(a.status, KV8_RANGE);
+        x.record = page * nkv + kvh;
+        x.scale = a.scales[(uint32_t)x.record];
         return x;
     };
     int chunk = 0;
@@ -311,8 +309,8 @@ __global__ __launch_bounds__(NWAVE * 64) __attribute__((amdgpu_waves_per_eu(2, 2
     u32x4 k[KR], v[VR];
     auto block = [&](int i) {
         const int at = i < n_it ? i : 0;
-        const int page = __builtin_amdgcn_readlane(at >> 6 == chunk ? now.page : next.page, at & 63);
-        return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(a.codes) + ((size_t)page * nkv + kvh) * (64 * HD), 0, i < n_it ? 64 * HD : 0, 0x00027000);
+        const uint32_t record = (uint32_t)__builtin_amdgcn_readlane(at >> 6 == chunk ? now.record : next.record, at & 63);
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(a.codes) + (size_t)record * (64 * HD), 0, i < n_it ? 64 * HD : 0, 0x00027000);
     };
     auto load_k = [&](int i) {
         const auto p = block(i);
@@ -343,8 +341,7 @@ __global__ __launch_bounds__(NWAVE * 64) __attribute__((amdgpu_waves_per_eu(2, 2
         float most = 0.f;
 #pragma unroll
         for (int x = 0; x < 8; ++x) most = fmaxf(most, fabsf(qx[i][x]));
-#pragma unroll
-        for (int x = TPR / 2; x > 0; x >>= 1) most = fmaxf(most, __shfl_xor(most, x));
+        most = row_max<TPR>(most);
         const int e = (int)(f32_bits(most) >> 23);   // 2^(e-127) <= most < 2^(e-126)
         const int to = e == 0 || e == 255 ? 127 : min(268 - e, 253);   // biased exponent of the factor, 2^(141-e)
         const float f = bits_f32((uint32_t)to << 23);
@@ -421,32 +418,39 @@ __global__ __launch_bounds__(NWAVE * 64) __attribute__((amdgpu_waves_per_eu(2, 2
         f32x4 s[RT][2];   // s[t][u][r]: position t0 + 16u + 4q + r for query row c of tile t
 #pragma unroll
         for (int t = 0; t < RT; ++t) s[t][0] = s[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+        // The operands of a step (32 channels, hi or lo) are read a step ahead: LDS answers after some hundred cycles, and one wave alone has
+        // nothing else to do meanwhile.
+        u32x4 qq[2][RT];
+        auto fetch = [&](int x) {
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            half8_t kk[2];
+            for (int t = 0; t < RT; ++t) qq[x & 1][t] = lds[(t * KS * PARTS + x) * 64 + ql];
+        };
+        half8_t kk[2];
+        fetch(0);
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const u32x4 &w = k[u * (KS / 2) + ks % (KS / 2)];
-                kk[u] = ks < KS / 2 ? codes_half8<FMT>(w[0], w[1], 1.f) : codes_half8<FMT>(w[2], w[3], 1.f);
+        for (int x = 0; x < KS * PARTS; ++x) {
+            if (x + 1 < KS * PARTS) fetch(x + 1);
+            if (x % PARTS == 0) {
+                const int ks = x / PARTS;
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const u32x4 &w = k[u * (KS / 2) + ks % (KS / 2)];
+                    kk[u] = ks < KS / 2 ? codes_half8<FMT>(w[0], w[1], 1.f) : codes_half8<FMT>(w[2], w[3], 1.f);
+                }
             }
 #pragma unroll
             for (int t = 0; t < RT; ++t)
 #pragma unroll
-                for (int part = 0; part < PARTS; ++part) {
-                    const half8_t qq = __builtin_bit_cast(half8_t, lds[((t * KS + ks) * PARTS + part) * 64 + ql]);
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) s[t][u] = mfma16(kk[u], qq, s[t][u]);
-                }
+                for (int u = 0; u < 2; ++u) s[t][u] = mfma16(kk[u], __builtin_bit_cast(half8_t, qq[x & 1][t]), s[t][u]);
+            if (RT * PARTS > 2) __builtin_amdgcn_sched_barrier(0);
         }
         load_k(i + 1);
         const bool whole = t0 + 32 <= len && (t0 >= all_from || t0 + 32 <= a.sinks);   // all rows see all of the block
-        float mx[RT];
+        float sc[RT], mx[RT];   // mx: of the lane's own eight positions
         bool grow = false;
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
-            const float sc = row_scale[t] * k_scale;
-#pragma unroll
-            for (int u = 0; u < 2; ++u) s[t][u] *= sc;
+            sc[t] = row_scale[t] * k_scale;
             if (!whole) {
                 const uint32_t mine = visible(t0, len, low_s[t * 16 + c], a.sinks, word_s[t * 16 + c]) >> (4 * q);
 #pragma unroll
@@ -454,14 +458,14 @@ __global__ __launch_bounds__(NWAVE * 64) __attribute__((amdgpu_waves_per_eu(2, 2
 #pragma unroll
                     for (int r = 0; r < 4; ++r) s[t][u][r] = mine & (1u << (16 * u + r)) ? s[t][u][r] : -INFINITY;
             }
-            const float m = fmaxf(fmaxf(fmaxf(s[t][0][0], s[t][0][1]), fmaxf(s[t][0][2], s[t][0][3])), fmaxf(fmaxf(s[t][1][0], s[t][1][1]), fmaxf(s[t][1][2], s[t][1][3])));
-            mx[t] = rows_max(m);
-            grow = grow || mx[t] > m_run[t] + REF_MOST;
+            mx[t] = max3(max3(s[t][0][0], s[t][0][1], s[t][0][2]), max3(s[t][0][3], s[t][1][0], s[t][1][1]), max3(s[t][1][2], s[t][1][3], s[t][1][3]));
+            grow = grow || mx[t] * sc[t] > m_run[t] + REF_MOST;
         }
         if (__any(grow)) {
 #pragma unroll
             for (int t = 0; t < RT; ++t) {
-                const float m_new = mx[t] > m_run[t] + REF_MOST ? mx[t] - REF_BELOW : m_run[t], alpha = __builtin_amdgcn_exp2f(m_run[t] - m_new);
+                const float m = rows_max(mx[t]) * sc[t];
+                const float m_new = m > m_run[t] + REF_MOST ? m - REF_BELOW : m_run[t], alpha = __builtin_amdgcn_exp2f(m_run[t] - m_new);
                 m_run[t] = m_new;
                 l_run[t] *= alpha;
 #pragma unroll
@@ -483,7 +487,8 @@ __global__ __launch_bounds__(NWAVE * 64) __attribute__((amdgpu_waves_per_eu(2, 2
         for (int t = 0; t < RT; ++t)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float p0 = __builtin_amdgcn_exp2f(s[t][e >> 1][2 * (e & 1)] - m_run[t]), p1 = __builtin_amdgcn_exp2f(s[t][e >> 1][2 * (e & 1) + 1] - m_run[t]);
+                const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e >> 1][2 * (e & 1)], sc[t], -m_run[t]));
+                const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e >> 1][2 * (e & 1) + 1], sc[t], -m_run[t]));
                 uint32_t hi, lo;
                 if (PARTS == 2) {
                     split_half2(p0, p1, hi, lo);
@@ -577,7 +582,7 @@ __global__ __launch_bounds__(NWAVE * 64) __attribute__((amdgpu_waves_per_eu(2, 2
         }
     }
     if (cut.n == 1 || !a.hand.words) return;
-    const int group = (turn * nkv + kvh) * passes + pass;   // by turn, not by sequence: both count to B
+    const int group = (b * nkv + kvh) * passes + pass;
     HandWay way = hand_wait(a.hand, group, cut.n, hand_arrive(a.hand, group), &way_s);
     if (way == HAND_TURN_IN) way = hand_turn_in(a.hand, group, cut.n, &way_s);
     uint64_t left = way == HAND_SHARE ? hand_leave(a.hand, group) : 0;   // under way while the shares are done
@@ -619,8 +624,7 @@ template <int HD, int FMT, int PARTS> hipError_t launch_parts(const Kv8AttnArgs 
     switch (rt) {
     case 1: hipLaunchKernelGGL((kv8_attn_kernel<HD, FMT, 1, PARTS>), grid, block, 0, s, a); break;
     case 2: hipLaunchKernelGGL((kv8_attn_kernel<HD, FMT, 2, PARTS>), grid, block, 0, s, a); break;
-    case 3: hipLaunchKernelGGL((kv8_attn_kernel<HD, FMT, 3, PARTS>), grid, block, 0, s, a); break;
-    default: hipLaunchKernelGGL((kv8_attn_kernel<HD, FMT, 4, PARTS>), grid, block, 0, s, a); break;
+    default: hipLaunchKernelGGL((kv8_attn_kernel<HD, FMT, 3, PARTS>), grid, block, 0, s, a); break;
     }
     return hipGetLastError();
 }
@@ -640,14 +644,24 @@ template <int HD> hipError_t launch_hd(const Kv8AttnArgs &a, int fmt, int rt, hi
 Kv8Plan kv8_plan(int B, int n, int gq, int nkv)
 {
     const int tiles = (n * gq + 15) / 16;
+    const int64_t heads = (int64_t)B * nkv;
     Kv8Plan p;
-    p.passes = (tiles + KV8_MAX_TILES - 1) / KV8_MAX_TILES;
-    const int64_t units = (int64_t)B * nkv * p.passes, share = WGS / units;
+    double best = 0;
+    for (int rt = KV8_MAX_TILES; rt >= 1; --rt) {
+        const int passes = (tiles + rt - 1) / rt;
+        const int64_t units = heads * passes;
+        static const double block[4] = {0, 0.75, 1.0, 1.4};
+        const double cost = units <= 256 ? block[rt] / (256 / units) : block[rt] * ((units + 255) / 256);
+        if (rt == KV8_MAX_TILES || cost < best) {
+            best = cost;
+            p.passes = passes;
+        }
+    }
+    const int64_t units = heads * p.passes;
+    int64_t share = 256 / units;
+    if (share * units <= 192) share = 512 / units;
     p.share = share < 1 ? 1 : share > 64 ? 64 : (int)share;
-    p.in_die = B * nkv % 8 == 0 && units <= HAND_GROUPS;
-    p.by_length = B > 1 && B <= 64 && nkv % 8 == 0;
-    const int slots = nkv / 8 * p.share * p.passes;   // of a sequence on a die, which takes 32 workgroups at once
-    p.first_turns = p.by_length && slots * B > 32 && slots * B <= 64 ? (32 + slots - 1) / slots : B;
+    p.in_die = heads % 8 == 0 && units <= HAND_GROUPS;
     return p;
 }
 

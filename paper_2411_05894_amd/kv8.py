@@ -111,7 +111,7 @@ class Rope:
 def sssd_op_rope(x: torch.Tensor, positions: torch.Tensor, rope: Rope, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """x [rows][heads][head_dim] with positions [rows], or [B][n][heads][head_dim] with [B][n]; out may be x."""
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
     assert out.shape == x.shape and out.dtype == x.dtype
     at = _ints(positions, x.shape[:-2], rope.device)
     if x.dim() == 3:
