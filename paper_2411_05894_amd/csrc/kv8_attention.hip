@@ -8,7 +8,6 @@ namespace {
 __device__ __forceinline__ f32x4 mfma16(const half8_t &a, const half8_t &b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
 constexpr float NEG_BIG = -1.0e30f;
-constexpr int NWAVE = 4;
 // Probabilities are kept below 2^15 (the largest float16 is 65504): the reference of the exponents is put 2^7 below a row's maximum and
 // follows once the maximum has outgrown it by 2^15.  So they lose no bits to float16's small numbers until they are 2^-21 of the largest.
 constexpr float REF_BELOW = 7.f, REF_MOST = 15.f;
@@ -218,17 +217,17 @@ __device__ __forceinline__ uint32_t visible(int t0, int len, int low, int sinks,
 
 // PARTS: the query operand is float16 (1: bf16 queries) or float16 hi + lo (2: float32 queries), and so are the probabilities.
 // grid: workgroups of one (sequence, kv head) have block indexes of one residue modulo 8: its segments, and their passes next to each other.
-template <int HD, int FMT, int RT, int PARTS>
-__global__ __launch_bounds__(NWAVE * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void kv8_attn_kernel(Kv8AttnArgs a)
+template <int HD, int FMT, int RT, int PARTS, int NW>
+__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void kv8_attn_kernel(Kv8AttnArgs a)
 {
-    constexpr int KS = HD / 32, DT = HD / 16, QT = DT / 4, TR = RT <= 3 ? RT : 2;
-    constexpr int QREC = RT * KS * PARTS * 64, RRED = NWAVE * (NWAVE - 1) * TR * QT * 64;
+    constexpr int KS = HD / 32, DT = HD / 16, QT = DT / NW, TR = NW == 4 ? RT : RT <= 2 ? RT : 2;
+    constexpr int QREC = RT * KS * PARTS * 64, RRED = NW * (NW - 1) * TR * QT * 64;
     __shared__ u32x4 lds[QREC > RRED ? QREC : RRED];
     __shared__ float row_scale_s[RT * 16];
     __shared__ uint32_t word_s[RT * 16];
     __shared__ int low_s[RT * 16], way_s;
-    __shared__ float2 ml_s[NWAVE][RT * 16];
-    __shared__ float vref_s[NWAVE];
+    __shared__ float2 ml_s[NW][RT * 16];
+    __shared__ float vref_s[NW];
 
     const int passes = a.plan.passes, share = a.plan.share, nkv = a.g.nkv;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -248,7 +247,7 @@ __global__ __launch_bounds__(NWAVE * 64) __attribute__((amdgpu_waves_per_eu(2, 2
     const int rt0 = pass * RT;
 
     // A thread's share of the queries is requested ahead of everything that depends on lens: eight channels of a row at a time.
-    constexpr int TPR = HD / 8, RPP = NWAVE * 64 / TPR, QN = (RT * 16 + RPP - 1) / RPP;   // threads of a row, rows at a time
+    constexpr int TPR = HD / 8, RPP = NW * 64 / TPR, QN = (RT * 16 + RPP - 1) / RPP;   // threads of a row, rows at a time
     const int q_part = threadIdx.x % TPR, q_row = threadIdx.x / TPR;
     float qx[QN][8];
     u32x4 qv[QN][PARTS];
@@ -271,7 +270,7 @@ __global__ __launch_bounds__(NWAVE * 64) __attribute__((amdgpu_waves_per_eu(2, 2
     if (!ok) {   // zeros
         if (segment == 0) {
             if (kvh == 0 && pass == 0 && threadIdx.x == 0) atomicOr(a.status, KV8_RANGE);
-            for (int i = threadIdx.x; i < RT * 16 * (HD / 4); i += NWAVE * 64) {
+            for (int i = threadIdx.x; i < RT * 16 * (HD / 4); i += NW * 64) {
                 const int r = rt0 * 16 + i / (HD / 4);
                 const RowOut o(r, a.gq, kvh);
                 if (o.j < a.n) store4(a.out, a.out.at(b, o.j, o.head), i % (HD / 4) * 4, f32x4{0.f, 0.f, 0.f, 0.f});
@@ -285,7 +284,7 @@ __global__ __launch_bounds__(NWAVE * 64) __attribute__((amdgpu_waves_per_eu(2, 2
     const Cut cut = cut_of(span.n, share);
     if (segment >= cut.n) return;
     const int first = segment * cut.each, n_blk = min(cut.each, span.n - first);
-    const int n_it = n_blk > wave ? (n_blk - wave + NWAVE - 1) / NWAVE : 0;
+    const int n_it = n_blk > wave ? (n_blk - wave + NW - 1) / NW : 0;
 
     // Pages and scales of this wave's blocks: lane l keeps those of its block number 64 * chunk + l, one chunk ahead.
     struct Ahead {
@@ -293,7 +292,7 @@ __global__ __launch_bounds__(NWAVE * 64) __attribute__((amdgpu_waves_per_eu(2, 2
         float2 scale;
     };
     auto look = [&](int chunk) {
-        const int i = min(first + wave + NWAVE * (64 * chunk + lane), span.n - 1);
+        const int i = min(first + wave + NW * (64 * chunk + lane), span.n - 1);
         Ahead x;
         const int entry = kv8_entry(a.g, b, span.block(i));
         const int page = min(max(entry, 0), a.g.n_pages - 1);
@@ -410,7 +409,7 @@ __global__ __launch_bounds__(NWAVE * 64) __attribute__((amdgpu_waves_per_eu(2, 2
             now = next;
             next = look(chunk + 1);
         }
-        const int t0 = span.block(first + wave + NWAVE * i) * 32;
+        const int t0 = span.block(first + wave + NW * i) * 32;
         const float k_scale = bits_f32((uint32_t)__builtin_amdgcn_readlane((int)f32_bits(now.scale.x), i & 63));
         const int v_e = __builtin_amdgcn_readlane((int)f32_bits(now.scale.y), i & 63) >> 23 & 255;
         int ql = lane;
@@ -524,20 +523,20 @@ __global__ __launch_bounds__(NWAVE * 64) __attribute__((amdgpu_waves_per_eu(2, 2
         if (q == 0) ml_s[wave][t * 16 + c] = float2{m_run[t], l_run[t][0]};
     if (lane == 0) vref_s[wave] = v_ref < 0 ? 0.f : bits_f32((uint32_t)v_ref << 23);
 #pragma unroll
-    for (int w = 0; w < NWAVE; ++w)
+    for (int w = 0; w < NW; ++w)
         if (w == wave)
 #pragma unroll
             for (int t = 0; t < RT; ++t)
 #pragma unroll
                 for (int x = 0; x < QT; ++x) own[t][x] = o[t][w * QT + x];
     auto part = [&](int quarter, int from, int t, int x) -> f32x4 & {
-        return red[(((quarter * (NWAVE - 1) + from - (from > quarter ? 1 : 0)) * TR + t % TR) * QT + x) * 64 + lane];
+        return red[(((quarter * (NW - 1) + from - (from > quarter ? 1 : 0)) * TR + t % TR) * QT + x) * 64 + lane];
     };
 #pragma unroll
     for (int tt = 0; tt < RT; tt += TR) {
         if (tt > 0) __syncthreads();
 #pragma unroll
-        for (int w = 0; w < NWAVE; ++w)
+        for (int w = 0; w < NW; ++w)
             if (w != wave)
 #pragma unroll
                 for (int t = tt; t < tt + TR && t < RT; ++t)
@@ -547,11 +546,11 @@ __global__ __launch_bounds__(NWAVE * 64) __attribute__((amdgpu_waves_per_eu(2, 2
 #pragma unroll
         for (int t = tt; t < tt + TR && t < RT; ++t) {
             const int row = (rt0 + t) * 16 + c;
-            float2 s4[NWAVE];
+            float2 s4[NW];
             float m_all = NEG_BIG;
 #pragma unroll
-            for (int i = 0; i < NWAVE; ++i) {
-                s4[i] = ml_s[(wave + i) & (NWAVE - 1)][t * 16 + c];
+            for (int i = 0; i < NW; ++i) {
+                s4[i] = ml_s[(wave + i) & (NW - 1)][t * 16 + c];
                 m_all = fmaxf(m_all, s4[i].x);
             }
             float l_all = 0.f;
@@ -559,8 +558,8 @@ __global__ __launch_bounds__(NWAVE * 64) __attribute__((amdgpu_waves_per_eu(2, 2
 #pragma unroll
             for (int x = 0; x < QT; ++x) y[x] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int i = 0; i < NWAVE; ++i) {
-                const int w = (wave + i) & (NWAVE - 1);
+            for (int i = 0; i < NW; ++i) {
+                const int w = (wave + i) & (NW - 1);
                 const float f = __builtin_amdgcn_exp2f(s4[i].x - m_all), fv = f * vref_s[w];
                 l_all += s4[i].y * f;
 #pragma unroll
@@ -587,7 +586,7 @@ __global__ __launch_bounds__(NWAVE * 64) __attribute__((amdgpu_waves_per_eu(2, 2
     if (way == HAND_TURN_IN) way = hand_turn_in(a.hand, group, cut.n, &way_s);
     uint64_t left = way == HAND_SHARE ? hand_leave(a.hand, group) : 0;   // under way while the shares are done
     if (way != HAND_NOTHING) {   // the rows of this pass shared out over the waves of all segments
-        const int r_end = min(rows, (rt0 + RT) * 16), step = (way == HAND_ALL ? 1 : cut.n) * NWAVE;
+        const int r_end = min(rows, (rt0 + RT) * 16), step = (way == HAND_ALL ? 1 : cut.n) * NW;
         int r = rt0 * 16 + (way == HAND_ALL ? wave : wave * cut.n + segment);
         // as many rows at once as the wave has, up to four, when they have few segments
 #define KV8_MERGE(ROWS, U, MANY) for (; r < r_end; r += ROWS * step) merge_rows<HD, ROWS, U, MANY, true>(a, b, kvh, r, step, r_end, cut.n, lane)
@@ -620,12 +619,26 @@ template <int HD> __global__ __launch_bounds__(256) void kv8_merge_kernel(Kv8Att
 
 template <int HD, int FMT, int PARTS> hipError_t launch_parts(const Kv8AttnArgs &a, int rt, hipStream_t s)
 {
-    const dim3 grid(((uint32_t)a.B * a.g.nkv + 7) / 8 * 8 * a.plan.share * a.plan.passes), block(NWAVE * 64);
-    switch (rt) {
-    case 1: hipLaunchKernelGGL((kv8_attn_kernel<HD, FMT, 1, PARTS>), grid, block, 0, s, a); break;
-    case 2: hipLaunchKernelGGL((kv8_attn_kernel<HD, FMT, 2, PARTS>), grid, block, 0, s, a); break;
-    default: hipLaunchKernelGGL((kv8_attn_kernel<HD, FMT, 3, PARTS>), grid, block, 0, s, a); break;
+    const dim3 grid(((uint32_t)a.B * a.g.nkv + 7) / 8 * 8 * a.plan.share * a.plan.passes);
+    // Eight waves to a workgroup where a compute unit has one workgroup, of long segments and more than a wave alone on its SIMD gets done while
+    // the cache streams: float32 queries, or several passes over the cache.  us, four / eight: 8B f32 B = 4, n = 9, 32768 73 / 67; 70B B = 16,
+    // n = 9, 2048 bf16 30.9 / 26.8, f32 36.4 / 34.1; B = 7, n = 13, 700..1500 f32 23.3 / 21.0; not: bf16 in one pass, 8B B = 4, 32768 57.3 / 59.7,
+    // many segments, f32 B = 1, 2048 11.4 / 13.0, two workgroups on a unit, B = 16, n = 32, 500 13.4 / 19.6
+    const bool eight = HD == 128 && rt > 1 && a.plan.share <= 8 && (int64_t)a.B * a.g.nkv * a.plan.share * a.plan.passes <= 256 && (PARTS == 2 || a.plan.passes > 1);
+#define KV8_ATTN(RT, NW) hipLaunchKernelGGL((kv8_attn_kernel<HD, FMT, RT, PARTS, NW>), grid, dim3(NW * 64), 0, s, a)
+    if constexpr (HD == 128) {
+        if (eight) {
+            if (rt == 2) KV8_ATTN(2, 8);
+            else KV8_ATTN(3, 8);
+            return hipGetLastError();
+        }
     }
+    switch (rt) {
+    case 1: KV8_ATTN(1, 4); break;
+    case 2: KV8_ATTN(2, 4); break;
+    default: KV8_ATTN(3, 4); break;
+    }
+#undef KV8_ATTN
     return hipGetLastError();
 }
 template <int HD> hipError_t launch_hd(const Kv8AttnArgs &a, int fmt, int rt, hipStream_t s)
