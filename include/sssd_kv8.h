@@ -100,12 +100,12 @@ int sssd_rope_frequencies(const sssd_rope_config *cfg, double *turns);
  * (the product in 64 bits, so that far positions keep their angle) and multiplied by `magnitude`. */
 typedef struct {
     const double *turns; /* device, [rotary_dims/2] */
-    int32_t rotary_dims; /* even, 2 .. head_dim */
+    int32_t rotary_dims; /* even, 2 .. head_dim, at most 1024 */
     int32_t pairs;       /* SSSD_ROPE_HALVES or SSSD_ROPE_NEIGHBOURS */
     float magnitude;     /* 1, or what a scaling for long contexts asks for */
 } sssd_rope;
 
-/* out = x rotated: [B][n][heads][head_dim] each, of one type; out may be x itself (same data and strides), else
+/* out = x rotated: [B][n][heads][head_dim] each (heads <= 65535, head_dim <= 8192), of one type; out may be x itself (same data and strides), else
  * they must not overlap.  positions: device int32 [B][n]. */
 int sssd_op_rope(const sssd_rows *x, const sssd_rows *out, int32_t B, int32_t n, int32_t heads, int32_t head_dim,
                  const int32_t *positions, const sssd_rope *rope, void *stream);

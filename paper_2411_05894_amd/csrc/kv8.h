@@ -127,10 +127,12 @@ __device__ __forceinline__ void rope_cos_sin(const Rope8 &rp, int position, doub
     s *= rp.magnitude;
 }
 
-// A rotation shared out over threads: an item is a unit (rope_unit) of a row, through `per` heads.
+// A rotation shared out over workgroups: `rows` rows and `per` heads each, a unit at a time.
+constexpr int ROPE_TABLE = 512, ROPE_ROWS = 4;   // pairs of a workgroup's rows in LDS (sssd_rope_config allows 512 a row); rows of a workgroup
 struct RopeWork {
-    int d, heads, per, unit;      // unit: 8, 2 or 1
-    uint32_t n, units, items;     // units of a row; items: rows x units
+    int d, heads, per, unit;      // unit: 8 channels, 2 or 1
+    uint32_t n, units, rows, total;   // units of a row and head; rows of the whole call
+    Div by_units;
 };
 RopeWork rope_work(int B, int n, int d, int heads, int r, bool neighbours, int threads);
 

@@ -68,7 +68,7 @@ int make_rows(const sssd_rows *r, int B, int n, int heads, Rows8 &out)
 
 bool make_rope(const sssd_rope *r, int head_dim, Rope8 &out)
 {
-    if (!r->turns || r->rotary_dims < 2 || r->rotary_dims % 2 || r->rotary_dims > head_dim) return false;
+    if (!r->turns || r->rotary_dims < 2 || r->rotary_dims % 2 || r->rotary_dims > head_dim || r->rotary_dims > 2 * ROPE_TABLE) return false;
     if (r->pairs != SSSD_ROPE_HALVES && r->pairs != SSSD_ROPE_NEIGHBOURS) return false;
     out = Rope8{r->turns, r->rotary_dims, r->pairs == SSSD_ROPE_NEIGHBOURS, r->magnitude};
     return true;
@@ -115,12 +115,12 @@ int sssd_rope_frequencies(const sssd_rope_config *c, double *turns)
 int sssd_op_rope(const sssd_rows *x, const sssd_rows *out, int32_t B, int32_t n, int32_t heads, int32_t head_dim, const int32_t *positions,
                  const sssd_rope *rope, void *stream)
 {
-    if (B <= 0 || n <= 0 || heads <= 0 || heads > 65535 || head_dim <= 0 || !positions || !rope) return SSSD_EINVAL;
+    if (B <= 0 || n <= 0 || heads <= 0 || heads > 65535 || head_dim <= 0 || head_dim > 8192 || !positions || !rope) return SSSD_EINVAL;
     Rows8 from, to;
     Rope8 rp;
     if (make_rows(x, B, n, heads, from) || make_rows(out, B, n, heads, to) || from.bf16 != to.bf16 || !make_rope(rope, head_dim, rp)) return SSSD_EINVAL;
     if (from.p == to.p && (from.bs != to.bs || from.rs != to.rs || from.hs != to.hs)) return SSSD_EINVAL;
-    if ((int64_t)B * n > MOST_THREADS / head_dim) return SSSD_ECAPACITY;
+    if ((int64_t)B * n > MOST_THREADS / 256) return SSSD_ECAPACITY;
     HIP_TRY(launch_rope(from, to, positions, rp, rope_work(B, n, head_dim, heads, rp.r, rp.neighbours, 256), (hipStream_t)stream));
     return SSSD_OK;
 }
@@ -166,7 +166,7 @@ int sssd_kv8_append(const sssd_kv8 *kv, int32_t layer, int32_t first, int32_t B,
         if (make_rows(q, B, n, c.n_q_heads, a.q) || make_rows(q_out, B, n, c.n_q_heads, a.q_out) || a.q.bf16 != a.q_out.bf16) return SSSD_EINVAL;
         if (a.q.p == a.q_out.p && (a.q.bs != a.q_out.bs || a.q.rs != a.q_out.rs || a.q.hs != a.q_out.hs)) return SSSD_EINVAL;
         // with the threads that store: both halves of what a launch may have
-        if ((int64_t)B * n > MOST_THREADS / 2 / c.head_dim / c.n_q_heads || (int64_t)B * a.blocks > MOST_THREADS / 2 / (4 * c.head_dim) / c.n_kv_heads)
+        if ((int64_t)B * n > MOST_THREADS / 2 / (2 * c.head_dim) || (int64_t)B * a.blocks > MOST_THREADS / 2 / (4 * c.head_dim) / c.n_kv_heads)
             return SSSD_ECAPACITY;
         a.work = rope_work(B, n, c.head_dim, c.n_q_heads, a.rope.r, a.rope.neighbours, 2 * c.head_dim);
     }

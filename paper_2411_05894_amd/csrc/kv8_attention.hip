@@ -590,7 +590,9 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
         int r = rt0 * 16 + (way == HAND_ALL ? wave : wave * cut.n + segment);
         // as many rows at once as the wave has, up to four, when they have few segments
 #define KV8_MERGE(ROWS, U, MANY) for (; r < r_end; r += ROWS * step) merge_rows<HD, ROWS, U, MANY, true>(a, b, kvh, r, step, r_end, cut.n, lane)
-        if (cut.n > 8) KV8_MERGE(1, 5, true);
+        if (cut.n > 32) KV8_MERGE(1, 8, true);
+        else if (cut.n > 16) KV8_MERGE(1, 8, false);
+        else if (cut.n > 8) KV8_MERGE(1, 4, false);
         else if (cut.n > 4) {
             if (r + step < r_end) KV8_MERGE(2, 2, false);
             else KV8_MERGE(1, 2, false);

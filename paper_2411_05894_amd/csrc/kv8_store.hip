@@ -168,72 +168,94 @@ __device__ __forceinline__ void rotate_place(const Rope8 &rp, const Rows8 &r, co
     }
 }
 
-// One row's units of the rotation: by halves U pairs (i .. i+U-1 with their partners), as neighbours U/2 pairs that lie in a row, and U
-// channels that pass.  A thread takes its unit through heads h0 .. h1-1: the angles are worked out once.
-template <int U> __device__ __forceinline__ void rope_unit(const Rope8 &rp, const Rows8 &x, const Rows8 &out, int b, int j, int position, int unit, int d, int h0, int h1)
+// Rows of heads rotated by a workgroup of T threads: R rows, heads h0 .. h1-1 of each.  The angles of the rows' pairs are worked out once, in LDS
+// (some thirty instructions each); then the threads pass over the rows in the order of memory, a unit each: by halves U pairs (i .. i+U-1 with
+// their partners), as neighbours U/2 pairs that lie in a row, or U channels that pass.
+// Measured against a thread with the angles of eight pairs in registers that takes them through several heads (32 places of 256 bytes at a time, a
+// row's stride apart): 8191 rows of 40 heads of 128, bf16, 49.6 -> 36 us cold, whatever the number of heads requested at once.
+struct RopeRow {
+    int b, j, position, on;   // on: 0 where the row is left as it is
+};
+template <int T, int U, typename Row>
+__device__ __forceinline__ void rope_units(const Rope8 &rp, const Rows8 &x, const Rows8 &out, const RopeWork &w, int rows, int h0, int h1, const float2 *table, Row row)
 {
-    const int half = rp.r >> 1;
+    const int half = rp.r >> 1, units = w.units;
     const bool halves = !rp.neighbours;
     const int turning = halves ? half / U : rp.r / U;      // U divides them
-    const bool pass = unit >= turning;
-    const int ch = pass ? rp.r + (unit - turning) * U : unit * U;
-    auto get = [&](const char *row, int at, float (&v)[U]) {
-        if constexpr (U == 8) load8(x, row, at, v);
-        else
+    const uint32_t per_row = (uint32_t)(h1 - h0) * units, all = per_row * rows;
+    for (uint32_t i = threadIdx.x; i < all; i += T) {
+        uint32_t r = 0, z = i;   // a workgroup's rows are ROPE_ROWS at most
 #pragma unroll
-            for (int i = 0; i < U; ++i) v[i] = load1(x, row, at + i);
-    };
-    auto put = [&](char *row, int at, const float (&v)[U]) {
-        if constexpr (U == 8) store8(out, row, at, v);
-        else
+        for (int y = 1; y < ROPE_ROWS; ++y)
+            if (z >= per_row) {
+                z -= per_row;
+                ++r;
+            }
+        const uint32_t h = (uint32_t)w.by_units((int)z);
+        const int unit = (int)(z - h * units);
+        const RopeRow at = row((int)r);
+        if (!at.on) continue;
+        const char *src = x.at(at.b, at.j, h0 + (int)h);
+        char *dst = out.at(at.b, at.j, h0 + (int)h);
+        const bool pass = unit >= turning;
+        const int ch = pass ? rp.r + (unit - turning) * U : unit * U;
+        const float2 *cs = table + r * half;
+        if constexpr (U == 8) {
+            float v[8];
+            if (pass) {
+                if (x.p == out.p) continue;
+                load8(x, src, ch, v);
+            } else if (halves) {
+                float u[8], y[8];
+                load8(x, src, ch, u);
+                load8(x, src, ch + half, y);
 #pragma unroll
-            for (int i = 0; i < U; ++i) store1(out, row, at + i, v[i]);
-    };
-    if (pass) {
-        if (x.p == out.p) return;
-        for (int h = h0; h < h1; ++h) {
-            const char *row = x.at(b, j, h);
-            char *to = out.at(b, j, h);
-            if constexpr (U == 8) {
-                float v[U];
-                get(row, ch, v);
-                put(to, ch, v);
+                for (int e = 0; e < 8; ++e) {
+                    const float2 t = cs[ch + e];
+                    v[e] = u[e] * t.x - y[e] * t.y;
+                    y[e] = y[e] * t.x + u[e] * t.y;
+                }
+                store8(out, dst, ch + half, y);
             } else {
-                for (int i = 0; i < U && ch + i < d; ++i) store1(out, to, ch + i, load1(x, row, ch + i));
-            }
-        }
-        return;
-    }
-    float c[U], s[U];
+                load8(x, src, ch, v);
 #pragma unroll
-    for (int i = 0; i < U; ++i)
-        if (halves) rope_cos_sin(rp, position, rp.turns[ch + i], c[i], s[i]);
-        else if (i % 2 == 0) rope_cos_sin(rp, position, rp.turns[(ch + i) >> 1], c[i], s[i]);
-    for (int h = h0; h < h1; ++h) {
-        const char *row = x.at(b, j, h);
-        char *to = out.at(b, j, h);
-        float v[U];
-        get(row, ch, v);
-        if (halves) {
-            float w[U], a[U];
-            get(row, ch + half, w);
-#pragma unroll
-            for (int i = 0; i < U; ++i) {
-                a[i] = v[i] * c[i] - w[i] * s[i];
-                w[i] = w[i] * c[i] + v[i] * s[i];
+                for (int e = 0; e < 8; e += 2) {
+                    const float2 t = cs[(ch + e) >> 1];
+                    const float u = v[e];
+                    v[e] = u * t.x - v[e + 1] * t.y;
+                    v[e + 1] = v[e + 1] * t.x + u * t.y;
+                }
             }
-            put(to, ch, a);
-            put(to, ch + half, w);
-        } else {
-#pragma unroll
-            for (int i = 0; i + 1 < U; i += 2) {
-                const float a = v[i];
-                v[i] = a * c[i] - v[i + 1] * s[i];
-                v[i + 1] = v[i + 1] * c[i] + a * s[i];
-            }
-            put(to, ch, v);
+            store8(out, dst, ch, v);
+        } else if (pass) {
+            if (x.p == out.p) continue;
+            for (int e = 0; e < U && ch + e < w.d; ++e) store1(out, dst, ch + e, load1(x, src, ch + e));
+        } else {   // a pair
+            const int other = halves ? ch + half : ch + 1;
+            const float2 t = cs[halves ? ch : ch >> 1];
+            const float u = load1(x, src, ch), y = load1(x, src, other);
+            store1(out, dst, ch, u * t.x - y * t.y);
+            store1(out, dst, other, y * t.x + u * t.y);
         }
     }
+}
+template <int T, typename Row>
+__device__ __forceinline__ void rope_rows(const Rope8 &rp, const Rows8 &x, const Rows8 &out, const RopeWork &w, int group, int chunk, float2 *table, RopeRow *rows_s, Row row)
+{
+    const uint32_t row0 = (uint32_t)group * w.rows;
+    const int rows = (int)min((uint32_t)w.rows, w.total - row0), half = rp.r >> 1;
+    if ((int)threadIdx.x < rows) rows_s[threadIdx.x] = row(row0 + threadIdx.x);
+    __syncthreads();
+    for (int i = threadIdx.x; i < rows * half; i += T) {
+        const int r = i / half;
+        rope_cos_sin(rp, rows_s[r].position, rp.turns[i - r * half], table[i].x, table[i].y);
+    }
+    __syncthreads();
+    const int h0 = chunk * w.per, h1 = min(h0 + w.per, w.heads);
+    auto of = [&](int r) { return rows_s[r]; };
+    if (w.unit == 8) rope_units<T, 8>(rp, x, out, w, rows, h0, h1, table, of);
+    else if (w.unit == 2) rope_units<T, 2>(rp, x, out, w, rows, h0, h1, table, of);
+    else rope_units<T, 1>(rp, x, out, w, rows, h0, h1, table, of);
 }
 
 struct RopeArgs {
@@ -243,13 +265,14 @@ struct RopeArgs {
     RopeWork w;
 };
 
-template <int U> __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a)
+__global__ __launch_bounds__(256) void rope_kernel(RopeArgs a)
 {
-    const uint32_t item = blockIdx.x * 256u + threadIdx.x;
-    if (item >= a.w.items) return;
-    const uint32_t row = item / a.w.units, unit = item - row * a.w.units, b = row / a.w.n, j = row - b * a.w.n;
-    const int h0 = blockIdx.y * a.w.per;
-    rope_unit<U>(a.rope, a.x, a.out, b, j, a.positions[row], unit, a.w.d, h0, min(h0 + a.w.per, a.w.heads));
+    __shared__ float2 table[ROPE_TABLE];
+    __shared__ RopeRow rows_s[ROPE_ROWS];
+    rope_rows<256>(a.rope, a.x, a.out, a.w, blockIdx.x, blockIdx.y, table, rows_s, [&](uint32_t row) {
+        const uint32_t b = row / a.w.n;
+        return RopeRow{(int)b, (int)(row - b * a.w.n), a.positions[row], 1};
+    });
 }
 
 // The page of block `step` of the rows that a call moves for sequence b, or -1: a block past them, or the sequence is rejected, which one of
@@ -284,34 +307,32 @@ template <int HD, int FMT> __global__ __launch_bounds__(2 * HD) void append_kern
     constexpr int T = 2 * HD;
     __shared__ float most_s[HD / 32];
     __shared__ __align__(16) uint8_t turn_s[32 * Turn<HD>::PITCH];
-    __shared__ int32_t up_s[128];   // at most 33 rows and the rest of two trees
+    __shared__ float2 table[ROPE_ROWS * HD / 2];
+    __shared__ RopeRow rows_s[ROPE_ROWS];
     const int lane = threadIdx.x & 63;
     int id = blockIdx.x;
     int len, count;
     if (id >= store_groups) {
         id -= store_groups;
-        const RopeWork &w = a.work;
-        const int groups = (int)((w.items + T - 1) / T), chunk = id / groups;
-        const uint32_t first = (uint32_t)(id - chunk * groups) * T, item = min(first + threadIdx.x, w.items - 1);
-        const uint32_t row = item / w.units, unit = item - row * w.units;
-        const int b = (int)(row / w.n), j = (int)row - b * a.n;
-        int dep = j;
-        if (a.parents) {   // a workgroup's rows, 33 at most, may be of several sequences: their trees in LDS, where a thread walks up
-            const int b0 = (int)(first / w.units / w.n), b1 = (int)(min(first + T - 1, w.items - 1) / w.units / w.n);
-            for (int i = threadIdx.x; i < (b1 - b0 + 1) * a.n; i += T) up_s[i] = a.parents[(size_t)b0 * a.n + i];
-            __syncthreads();
-            const int32_t *up = up_s + (b - b0) * a.n;
-            dep = 0;
-            for (int x = j; x > 0; ++dep) {
-                const int y = up[x];
-                x = y < 0 || y >= x ? x - 1 : y;
+        const int groups = (int)((a.work.total + a.work.rows - 1) / a.work.rows), chunk = id / groups;
+        rope_rows<T>(a.rope, a.q, a.q_out, a.work, id - chunk * groups, chunk, table, rows_s, [&](uint32_t row) {
+            RopeRow r;
+            r.b = (int)(row / a.work.n);
+            r.j = (int)row - r.b * a.n;
+            int len, count;
+            r.on = kv8_rows(a.lens, a.counts, r.b, a.n, a.g.max_seq, len, count) && r.j < count;
+            r.position = len + r.j;
+            if (a.parents && r.on) {   // a thread walks up; a workgroup has few rows
+                const int32_t *up = a.parents + (size_t)r.b * a.n;
+                int depth = 0;
+                for (int x = r.j; x > 0; ++depth) {
+                    const int y = up[x];
+                    x = y < 0 || y >= x ? x - 1 : y;
+                }
+                r.position = len + depth;
             }
-        }
-        const int h0 = chunk * w.per, h1 = min(h0 + w.per, w.heads);
-        if (first + threadIdx.x >= w.items || !kv8_rows(a.lens, a.counts, b, a.n, a.g.max_seq, len, count) || j >= count) return;
-        if (w.unit == 8) rope_unit<8>(a.rope, a.q, a.q_out, b, j, len + dep, unit, HD, h0, h1);
-        else if (w.unit == 2) rope_unit<2>(a.rope, a.q, a.q_out, b, j, len + dep, unit, HD, h0, h1);
-        else rope_unit<1>(a.rope, a.q, a.q_out, b, j, len + dep, unit, HD, h0, h1);
+            return r;
+        });
         return;
     }
     const int is_v = id & 1;
@@ -509,28 +530,34 @@ __global__ __launch_bounds__(64) void advance_kernel(Kv8StoreArgs a, const int32
 
 }  // namespace
 
-// Units of eight channels where pairs and the channels that pass divide into them, else single pairs.  A thread works its unit's angles out
-// once (some thirty instructions a pair) for `per` heads: as many as leave eight workgroups to every compute unit, up to eight.
+// Units of eight channels where pairs and the channels that pass divide into them, else single pairs.  A workgroup takes as many rows as its
+// table of angles holds while eight workgroups are left for every compute unit, and all heads; few rows are cut by heads, too.
 RopeWork rope_work(int B, int n, int d, int heads, int r, bool neighbours, int threads)
 {
     RopeWork w;
     const int turning = neighbours ? r : r / 2;
     w.unit = turning % 8 == 0 && (d - r) % 8 == 0 ? 8 : (neighbours ? 2 : 1);
-    const int units = turning / w.unit + (d - r + w.unit - 1) / w.unit;
-    w.n = n; w.d = d; w.heads = heads; w.units = units;
-    w.items = (uint32_t)B * n * units;
-    const int64_t groups = ((int64_t)w.items + threads - 1) / threads * heads;
-    w.per = (int)(groups / 2048 < 1 ? 1 : groups / 2048 > 8 ? 8 : groups / 2048);
+    w.units = turning / w.unit + (d - r + w.unit - 1) / w.unit;
+    w.n = n; w.d = d; w.heads = heads;
+    w.total = (uint32_t)B * n;
+    const uint32_t fit = ROPE_TABLE * 2 / r, want = w.total / 2048;
+    w.rows = want < 1 ? 1 : want > ROPE_ROWS ? ROPE_ROWS : want;
+    if (w.rows > fit) w.rows = fit;
+    const uint32_t groups = (w.total + w.rows - 1) / w.rows;
+    const int64_t most = ((int64_t)heads * w.units + threads - 1) / threads;   // a unit for every thread
+    int64_t chunks = groups < 512 ? 512 / groups : 1;
+    if (chunks > most) chunks = most;
+    w.per = (int)((heads + chunks - 1) / chunks);
+    const uint32_t exact = UINT32_MAX / w.units / w.units;   // of by_units
+    if ((uint32_t)w.per > exact) w.per = exact;
+    w.by_units = Div((int)w.units);
     return w;
 }
 
 hipError_t launch_rope(const Rows8 &x, const Rows8 &out, const int32_t *positions, const Rope8 &rope, const RopeWork &w, hipStream_t s)
 {
     const RopeArgs a{x, out, positions, rope, w};
-    const dim3 grid((w.items + 255) / 256, (w.heads + w.per - 1) / w.per);
-    if (w.unit == 8) hipLaunchKernelGGL(rope_kernel<8>, grid, dim3(256), 0, s, a);
-    else if (w.unit == 2) hipLaunchKernelGGL(rope_kernel<2>, grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL(rope_kernel<1>, grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL(rope_kernel, dim3((w.total + w.rows - 1) / w.rows, (w.heads + w.per - 1) / w.per), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
@@ -544,8 +571,8 @@ hipError_t launch_rope(const Rows8 &x, const Rows8 &out, const int32_t *position
 
 hipError_t launch_kv8_append(const Kv8StoreArgs &a, int fmt, int d, hipStream_t s)
 {
-    const int store = a.B * a.blocks * a.g.nkv * 2, T = 2 * d;
-    const int turn = a.q.p ? (int)((a.work.items + T - 1) / T) * ((a.work.heads + a.work.per - 1) / a.work.per) : 0;
+    const int store = a.B * a.blocks * a.g.nkv * 2;
+    const int turn = a.q.p ? (int)((a.work.total + a.work.rows - 1) / a.work.rows) * ((a.work.heads + a.work.per - 1) / a.work.per) : 0;
     KV8_LAUNCH(append_kernel, store + turn, a, store);
     return hipGetLastError();
 }

@@ -32,7 +32,7 @@ def check(x, positions, got, rotary, interleaved, magnitude=1.0, **scaling):
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("interleaved", [False, True])
-@pytest.mark.parametrize("d,rotary", [(128, 128), (64, 64), (128, 64), (128, 32), (64, 6), (80, 80), (96, 50), (64, 2), (50, 48), (7, 4)])
+@pytest.mark.parametrize("d,rotary", [(128, 128), (64, 64), (128, 64), (128, 32), (64, 6), (80, 80), (96, 50), (64, 2), (50, 48), (7, 4), (1024, 1024), (600, 514)])
 def test_rotation(dtype, interleaved, d, rotary):
     g = torch.Generator(device=DEV).manual_seed(d + rotary)
     rows, heads = 37, 5

@@ -78,7 +78,7 @@ def test_rope_refuses():
         ref = lambda s: C.byref(s) if s is not None else None  # noqa: E731
         return L.sssd_op_rope(ref(a["x"]), ref(a["out"]), a["B"], a["n"], a["heads"], a["d"], a["positions"], ref(a["rope"]), None)
     for bad in (dict(x=None), dict(out=None), dict(x=rows(data=None)), dict(out=rows(type=1)), dict(x=rows(type=2)), dict(x=rows(data=FAKE + 2)), dict(B=0), dict(n=0),
-                dict(heads=0), dict(heads=65536), dict(d=0), dict(positions=None), dict(rope=None), dict(rope=rope(turns=None)), dict(rope=rope(rotary=66)),
+                dict(heads=0), dict(heads=65536), dict(d=0), dict(d=8193), dict(d=2048, rope=rope(rotary=1026)), dict(positions=None), dict(rope=None), dict(rope=rope(turns=None)), dict(rope=rope(rotary=66)),
                 dict(rope=rope(rotary=3)), dict(rope=rope(rotary=0)), dict(rope=rope(pairs=2)), dict(n=2, out=rows(r=1280))):
         assert call(**bad) == SSSD_EINVAL, bad
     assert call(B=1 << 20, n=1 << 10, out=rows()) == SSSD_ECAPACITY
