@@ -64,6 +64,7 @@ typedef struct {
     const int32_t *block_table; /* device, or NULL: sequence b owns pages b*blocks_per_seq and following;
                                    NULL needs n_pages >= max_batch * blocks_per_seq                       */
     int32_t *status;            /* device int32 [1], zero-filled once by the caller: what sssd_kv8_sync reports */
+    uint32_t flags;             /* 0 or SSSD_NO_WAIT, as for sssd_verify_init: the same results, slower     */
 } sssd_kv8;
 
 /* Rows of heads in device memory: element (b, j, head, channel) lies `b*batch_stride + j*row_stride +
@@ -120,7 +121,7 @@ int sssd_op_rope(const sssd_rows *x, const sssd_rows *out, int32_t B, int32_t n,
  *   parents  NULL: chains, depth(j) = j.  Else device int32 [B][n] as in sssd_verify_step_tree (n <= 32)
  *   q, q_out both NULL, or with rope: [B][n][n_q_heads][head_dim], q_out = q rotated likewise (rows below counts[b]
  *            only), of one type, which need not be k's; q_out may be q itself
- * n is any (a prompt comes in one call).  A sequence with lens[b] < 0, lens[b] + counts[b] > max_seq, counts[b] outside
+ * n is any (a prompt comes in one call; above max_seq only with counts).  A sequence with lens[b] < 0, lens[b] + counts[b] > max_seq, counts[b] outside
  * 0..n or a page outside the pool for a block it writes is rejected: nothing of it is written, and the status raised; a
  * parent outside [0, j) is treated as j-1 and raises the status.  Sequences of one call must not share a page they write.
  */

@@ -44,6 +44,7 @@ int check_cache(const sssd_kv8 *kv, int layer, Sizes8 &S)
     if (rc) return rc;
     if (!kv->cache || (uintptr_t)kv->cache % ALIGN || !kv->status || layer < 0 || layer >= kv->cfg.n_layers) return SSSD_EINVAL;
     if (!kv->block_table && (int64_t)S.n_pages < (int64_t)kv->cfg.max_batch * S.blocks_per_seq) return SSSD_EINVAL;
+    if (kv->flags & ~SSSD_NO_WAIT) return SSSD_EINVAL;
     if (kv->cache_bytes < S.cache_bytes) return SSSD_ECAPACITY;
     return SSSD_OK;
 }
@@ -134,7 +135,7 @@ static int store_args(const sssd_kv8 *kv, int32_t layer, int32_t first, int32_t 
     if (rc) return rc;
     const sssd_kv8_config &c = kv->cfg;
     if (first < 0 || B <= 0 || n <= 0) return SSSD_EINVAL;
-    if ((int64_t)first + B > c.max_batch || n > c.max_seq) return SSSD_ECAPACITY;
+    if ((int64_t)first + B > c.max_batch || (n > c.max_seq && !counts)) return SSSD_ECAPACITY;
     a = Kv8StoreArgs{};
     if ((rc = make_rows(k, B, n, c.n_kv_heads, a.k)) || (rc = make_rows(v, B, n, c.n_kv_heads, a.v))) return rc;
     if (a.k.bf16 != a.v.bf16) return SSSD_EINVAL;
@@ -143,8 +144,8 @@ static int store_args(const sssd_kv8 *kv, int32_t layer, int32_t first, int32_t 
     a.scales = (float2 *)(a.codes + S.scales_at);
     a.layer_bytes = S.layer_bytes;
     a.first = first; a.B = B; a.n = n;
-    a.blocks = (n + 2 * KV8_BLOCK - 2) / KV8_BLOCK;   // the first may begin at a block's last row
-    if (a.blocks > S.blocks_per_seq) a.blocks = S.blocks_per_seq;
+    a.blocks = S.blocks_per_seq;
+    if (n <= c.max_seq && (n + 2 * KV8_BLOCK - 2) / KV8_BLOCK < a.blocks) a.blocks = (n + 2 * KV8_BLOCK - 2) / KV8_BLOCK;   // the first may begin at a block's last row
     a.lens = lens; a.counts = counts; a.status = kv->status;
     if ((int64_t)B * a.blocks > MOST_THREADS / (4 * c.head_dim) / c.n_kv_heads) return SSSD_ECAPACITY;
     return SSSD_OK;
@@ -201,6 +202,7 @@ int sssd_kv8_attention(const sssd_kv8 *kv, int32_t layer, int32_t B, int32_t n, 
     a.scales = (const float2 *)(a.codes + S.scales_at);
     a.B = B; a.n = n; a.gq = c.n_q_heads / c.n_kv_heads;
     a.lens = lens; a.counts = counts; a.parents = parents; a.window = window; a.sinks = sinks; a.status = kv->status;
+    a.hand.polls = kv->flags & SSSD_NO_WAIT ? 0 : HAND_POLLS;
     // a row of queries and a thread each in the merge, at most 32 passes of 256 threads a kv head otherwise
     if ((int64_t)B * c.n_q_heads > MOST_THREADS / (32 * 256)) return SSSD_ECAPACITY;
     HIP_TRY(launch_kv8_attention(a, c.format, c.head_dim, kv->workspace, (hipStream_t)stream));

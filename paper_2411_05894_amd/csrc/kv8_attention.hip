@@ -590,8 +590,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
         int r = rt0 * 16 + (way == HAND_ALL ? wave : wave * cut.n + segment);
         // as many rows at once as the wave has, up to four, when they have few segments
 #define KV8_MERGE(ROWS, U, MANY) for (; r < r_end; r += ROWS * step) merge_rows<HD, ROWS, U, MANY, true>(a, b, kvh, r, step, r_end, cut.n, lane)
-        if (cut.n > 32) KV8_MERGE(1, 8, true);
-        else if (cut.n > 16) KV8_MERGE(1, 8, false);
+        if (cut.n > 16) KV8_MERGE(1, 8, false);   // 32 at most: eight heads share 256 workgroups
         else if (cut.n > 8) KV8_MERGE(1, 4, false);
         else if (cut.n > 4) {
             if (r + step < r_end) KV8_MERGE(2, 2, false);
@@ -688,7 +687,7 @@ hipError_t launch_kv8_attention(Kv8AttnArgs a, int fmt, int d, void *ws, hipStre
     a.plan = kv8_plan(a.B, a.n, a.gq, a.g.nkv);
     const int rt = (tiles + a.plan.passes - 1) / a.plan.passes;
     a.rows_pad = tiles * 16;
-    a.hand = Hand{a.plan.share > 1 && a.plan.in_die ? (uint64_t *)ws : nullptr, nullptr, HAND_POLLS};
+    a.hand.words = a.plan.share > 1 && a.plan.in_die ? (uint64_t *)ws : nullptr;
     a.part_o = reinterpret_cast<float *>((char *)ws + HAND_WORDS);
     a.part_ml = reinterpret_cast<float2 *>(a.part_o + (size_t)KV8_GROUPS * KV8_MAX_TILES * 16 * d);
     return d == 128 ? launch_hd<128>(a, fmt, rt, s) : launch_hd<64>(a, fmt, rt, s);

@@ -7,7 +7,7 @@ from typing import Optional
 
 import torch
 
-from .binding import _check, _ptr, lib
+from .binding import SSSD_NO_WAIT, _check, _ptr, lib
 
 FORMATS = {"e4m3": 0, "int8": 1}
 SCALINGS = {"none": 0, "linear": 1, "bands": 2}
@@ -20,7 +20,7 @@ class Kv8Config(C.Structure):
 
 class Kv8(C.Structure):
     _fields_ = [("cfg", Kv8Config), ("cache", C.c_void_p), ("cache_bytes", C.c_size_t), ("workspace", C.c_void_p),
-                ("ws_bytes", C.c_size_t), ("block_table", C.c_void_p), ("status", C.c_void_p)]
+                ("ws_bytes", C.c_size_t), ("block_table", C.c_void_p), ("status", C.c_void_p), ("flags", C.c_uint32)]
 
 
 class Rows(C.Structure):
@@ -58,11 +58,13 @@ def _lib() -> C.CDLL:
 
 
 def _rows(t: torch.Tensor, device: int) -> Rows:
-    """[B][n][heads][channels] as the C ABI takes them; device: the number of the GPU, -1 for none."""
+    """[B][n][heads][channels], or [n][heads][channels], as the C ABI takes them; device: the number of the GPU, -1 for none."""
     stride = t.stride()
-    assert len(stride) == 4 and t.dtype in TYPES, "rows are [B][n][heads][head_dim], float32 or bfloat16"
+    assert len(stride) in (3, 4) and t.dtype in TYPES, "rows are [B][n][heads][head_dim], float32 or bfloat16"
     assert t.get_device() == device, f"rows on {t.device}, the cache (or the frequencies) on GPU {device}"
-    assert stride[3] == 1 or t.shape[3] == 1, "a head's channels must lie in a row"
+    assert stride[-1] == 1 or t.shape[-1] == 1, "a head's channels must lie in a row"
+    if len(stride) == 3:
+        return Rows(t.data_ptr(), TYPES[t.dtype], 0, stride[0], stride[1])
     return Rows(t.data_ptr(), TYPES[t.dtype], stride[0], stride[1], stride[2])
 
 
@@ -73,15 +75,15 @@ def _ints(t: Optional[torch.Tensor], shape, device: int) -> Optional[int]:
     return t.data_ptr()
 
 
-def _enqueue(name: str, device: int, *args) -> None:
+def _enqueue(call, device: int, *args) -> None:
     """The call on the current stream of `device`, whichever device is the current one."""
-    f = getattr(_lib(), name)
     if torch.cuda.current_device() == device:
-        code = f(*args, torch._C._cuda_getCurrentRawStream(device))
+        code = call(*args, torch._C._cuda_getCurrentRawStream(device))
     else:
         with torch.cuda.device(device):
-            code = f(*args, torch._C._cuda_getCurrentRawStream(device))
-    _check(code, name)
+            code = call(*args, torch._C._cuda_getCurrentRawStream(device))
+    if code:
+        _check(code, call.__name__)
 
 
 def sssd_kv8_sizes(cfg: Kv8Config):
@@ -113,13 +115,10 @@ def sssd_op_rope(x: torch.Tensor, positions: torch.Tensor, rope: Rope, out: Opti
     if out is None:
         out = torch.empty_like(x, memory_format=torch.contiguous_format)
     assert out.shape == x.shape and out.dtype == x.dtype
-    at = _ints(positions, x.shape[:-2], rope.device)
-    if x.dim() == 3:
-        x, y = x.unsqueeze(0), out.unsqueeze(0)
-    else:
-        y = out
-    B, n, heads, d = x.shape
-    _enqueue("sssd_op_rope", rope.device, C.byref(_rows(x, rope.device)), C.byref(_rows(y, rope.device)), B, n, heads, d, at, rope.ref)
+    shape = x.shape
+    B, n = shape[:2] if len(shape) == 4 else (1, shape[0])
+    _enqueue(_lib().sssd_op_rope, rope.device, C.byref(_rows(x, rope.device)), C.byref(_rows(out, rope.device)), B, n, shape[-2], shape[-1],
+             _ints(positions, shape[:-2], rope.device), rope.ref)
     return out
 
 
@@ -127,7 +126,7 @@ class Kv8Cache:
     """Owns the device buffers (as torch tensors) of a cache in 8 bits."""
 
     def __init__(self, n_layers: int, n_q_heads: int, n_kv_heads: int, head_dim: int, max_batch: int, max_seq: int, fmt: str = "e4m3",
-                 n_pages: int = 0, device: str = "cuda:0"):
+                 n_pages: int = 0, device: str = "cuda:0", no_wait: bool = False):
         self.cfg = Kv8Config(FORMATS[fmt], n_layers, n_q_heads, n_kv_heads, head_dim, max_batch, max_seq, n_pages)
         cache_bytes, ws_bytes, self.blocks_per_seq, self.n_pages = sssd_kv8_sizes(self.cfg)
         self.cache = torch.zeros(cache_bytes, dtype=torch.uint8, device=device)
@@ -135,7 +134,8 @@ class Kv8Cache:
         self.status = torch.zeros(1, dtype=torch.int32, device=device)
         self.device = self.cache.get_device()
         self._block_table = None
-        self.args = Kv8(self.cfg, _ptr(self.cache), cache_bytes, _ptr(self.workspace), ws_bytes, None, _ptr(self.status))
+        self.args = Kv8(self.cfg, _ptr(self.cache), cache_bytes, _ptr(self.workspace), ws_bytes, None, _ptr(self.status),
+                        SSSD_NO_WAIT if no_wait else 0)
         self._ref = C.byref(self.args)
 
     def _heads(self, t: torch.Tensor, heads: int):
@@ -160,27 +160,27 @@ class Kv8Cache:
         if q is not None:
             assert q_out is not None and q.shape == q_out.shape and q.dtype == q_out.dtype and q.shape[:2] == (B, n)
             qq, to = self._heads(q, self.cfg.n_q_heads), self._heads(q_out, self.cfg.n_q_heads)
-        _enqueue("sssd_kv8_append", self.device, self._ref, layer, first, B, n, self._heads(k, nkv), self._heads(v, nkv),
+        _enqueue(_lib().sssd_kv8_append, self.device, self._ref, layer, first, B, n, self._heads(k, nkv), self._heads(v, nkv),
                  _ints(lens, (B,), self.device), _ints(counts, (B,), self.device), turn, _ints(parents, (B, n), self.device), qq, to)
 
     def sssd_kv8_read(self, layer: int, start: Optional[torch.Tensor], counts: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
                       first: int = 0) -> None:
         B, n, nkv, _ = k.shape
         assert v.shape == k.shape and v.dtype == k.dtype and nkv == self.cfg.n_kv_heads
-        _enqueue("sssd_kv8_read", self.device, self._ref, layer, first, B, n, _ints(start, (B,), self.device), _ints(counts, (B,), self.device),
+        _enqueue(_lib().sssd_kv8_read, self.device, self._ref, layer, first, B, n, _ints(start, (B,), self.device), _ints(counts, (B,), self.device),
                  self._heads(k, nkv), self._heads(v, nkv))
 
     def sssd_kv8_attention(self, layer: int, q: torch.Tensor, lens: torch.Tensor, out: torch.Tensor, counts: Optional[torch.Tensor] = None,
                            parents: Optional[torch.Tensor] = None, window: int = 0, sinks: int = 0) -> None:
         B, n, nq, _ = q.shape
         assert out.shape == q.shape and out.dtype == q.dtype and nq == self.cfg.n_q_heads
-        _enqueue("sssd_kv8_attention", self.device, self._ref, layer, B, n, self._heads(q, nq), self._heads(out, nq),
+        _enqueue(_lib().sssd_kv8_attention, self.device, self._ref, layer, B, n, self._heads(q, nq), self._heads(out, nq),
                  _ints(lens, (B,), self.device), _ints(counts, (B,), self.device), _ints(parents, (B, n), self.device), window, sinks)
 
     def sssd_kv8_commit_tree(self, n: int, lens: torch.Tensor, accepted_len: torch.Tensor, accepted_path: Optional[torch.Tensor] = None) -> None:
         """n: rows of the step (accepted_path [B][n]); lens advances."""
         B = lens.numel()
-        _enqueue("sssd_kv8_commit_tree", self.device, self._ref, B, n, _ints(lens, (B,), self.device), _ints(accepted_len, (B,), self.device),
+        _enqueue(_lib().sssd_kv8_commit_tree, self.device, self._ref, B, n, _ints(lens, (B,), self.device), _ints(accepted_len, (B,), self.device),
                  _ints(accepted_path, (B, n), self.device))
 
     def sssd_kv8_sync(self) -> int:

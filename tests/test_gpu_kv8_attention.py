@@ -282,3 +282,21 @@ def test_pages_behind_four_gib():
         outs.append(torch.zeros_like(q))
         c.sssd_kv8_attention(0, q, ints([76]), outs[-1])
     assert torch.equal(*outs)
+
+
+@pytest.mark.parametrize("nq,nkv,d,B,n", [
+    (32, 8, 128, 4, 9), (32, 8, 128, 2, 32), (64, 8, 128, 2, 9), (64, 8, 128, 7, 13), (64, 8, 128, 1, 1), (32, 8, 128, 33, 5),   # one pass and several, four and eight waves
+    (64, 8, 64, 3, 9), (16, 2, 64, 1, 7), (16, 2, 128, 3, 7), (24, 8, 128, 5, 5), (48, 8, 64, 20, 6)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_plans(nq, nkv, d, B, n, dtype):
+    """Passes, row tiles, waves and segments of every kind, segments joined inside the launch and by a second one; those joined without waiting give
+    the same bits."""
+    lens = [(1700 * (b + 1)) % 2300 + (b == 0) * 1500 for b in range(B)]
+    batch = Batch("int8" if n % 2 else "e4m3", nq, nkv, d, lens, n, paged=True, seed=n)
+    print(f"kv8 plan {nq}/{nkv}x{d} B {B} n {n} {dtype}", flush=True)
+    want = batch.check(dtype)
+    batch.cache.args.flags = 2       # SSSD_NO_WAIT
+    for _ in range(3):
+        assert torch.equal(batch.check(dtype), want)
+    batch.cache.args.flags = 0
+    assert torch.equal(batch.check(dtype), want)

@@ -366,3 +366,41 @@ def test_pages_behind_four_gib():
     k, v = read_all(cache, 0, [80], 80)
     assert torch.equal(k[0].double(), want.x) and torch.equal(v, k)
     assert cache.sssd_kv8_sync() == SSSD_OK
+
+
+def test_a_padded_batch_longer_than_the_cache():
+    """Rows past counts may reach beyond max_seq: they are not read."""
+    cache = kv8.Kv8Cache(1, 2, 2, 64, 2, 70, "e4m3", device=DEV)
+    x = torch.randn(2, 128, 2, 64, device=DEV)
+    cache.sssd_kv8_append(0, x, x, ints([0, 30]), counts=ints([70, 33]))
+    assert cache.sssd_kv8_sync() == SSSD_OK
+    out = [torch.full((2, 128, 2, 64), 7.25, device=DEV) for _ in range(2)]
+    cache.sssd_kv8_read(0, ints([0, 30]), ints([70, 33]), *out)
+    assert cache.sssd_kv8_sync() == SSSD_OK
+    for b, n in ((0, 70), (1, 33)):
+        want = Cache(2, 64, "e4m3", DEV)
+        if b:
+            want.x = torch.zeros(30, 2, 64, dtype=torch.float64, device=DEV)
+            cache.sssd_kv8_read(0, ints([0, 0]), ints([0, 30]), *(old := [torch.zeros(2, 30, 2, 64, device=DEV) for _ in range(2)]))
+            want.x = old[0][1].double()
+        want.append(30 * b, x[b, :n])
+        assert torch.equal(out[0][b, :n].double(), want.x[30 * b:]) and (out[0][b, n:] == 7.25).all()
+    cache.sssd_kv8_append(0, x, x, ints([0, 30]), counts=ints([71, 33]))
+    assert cache.sssd_kv8_sync() == SSSD_ENOSPACE
+
+
+def test_nothing_to_do():
+    """Counts of zero: no row is read or written, and that is no error; neither is a commit of nothing accepted."""
+    cache = kv8.Kv8Cache(1, 2, 2, 64, 2, 64, "int8", device=DEV)
+    before = cache.cache.clone()
+    x = torch.full((2, 5, 2, 64), float("nan"), device=DEV)
+    rope = kv8.Rope(64, 100.0, device=DEV)
+    q = torch.full_like(x, 2.5)
+    cache.sssd_kv8_append(0, x, x, ints([0, 64]), counts=ints([0, 0]), rope=rope, q=x, q_out=q)
+    assert torch.equal(before, cache.cache) and (q == 2.5).all()
+    cache.sssd_kv8_read(0, ints([64, 0]), ints([0, 0]), q, q)
+    cache.sssd_kv8_attention(0, q, ints([0, 64]), q.clone(), counts=ints([0, 0]))
+    assert (q == 2.5).all() and cache.sssd_kv8_sync() == SSSD_OK
+    lens = ints([3, 7])
+    cache.sssd_kv8_commit_tree(5, lens, ints([0, 0]), ints([[0, -1, -1, -1, -1]] * 2))
+    assert lens.tolist() == [4, 8] and torch.equal(before, cache.cache) and cache.sssd_kv8_sync() == SSSD_OK

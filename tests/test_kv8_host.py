@@ -22,7 +22,7 @@ def config(**change):
 def cache(**change):
     cfg = config(**{k: v for k, v in change.items() if k in [f[0] for f in kv8.Kv8Config._fields_]})
     size, ws, _, _ = kv8.sssd_kv8_sizes(cfg)
-    a = dict(cfg=cfg, cache=FAKE, cache_bytes=size, workspace=FAKE, ws_bytes=ws, block_table=None, status=FAKE)
+    a = dict(cfg=cfg, cache=FAKE, cache_bytes=size, workspace=FAKE, ws_bytes=ws, block_table=None, status=FAKE, flags=0)
     a.update({k: v for k, v in change.items() if k in a})
     return kv8.Kv8(*a.values())
 
@@ -110,7 +110,7 @@ def refused(call, code, **change):
 def test_cache_calls_refuse():
     append, read, attention, commit = calls()
     for call in (append, read, attention, commit):
-        for bad in (dict(kv=None), dict(B=0), dict(B=-1), dict(n=0), dict(kv=cache(cache=None)), dict(kv=cache(cache=FAKE + 16)), dict(kv=cache(status=None)),
+        for bad in (dict(kv=None), dict(B=0), dict(B=-1), dict(n=0), dict(kv=cache(cache=None)), dict(kv=cache(cache=FAKE + 16)), dict(kv=cache(status=None)), dict(kv=cache(flags=1)),
                     dict(kv=cache(n_pages=11))):       # too few pages without a table
             refused(call, SSSD_EINVAL, **bad)
         for bad in (dict(B=4), dict(n=101), dict(kv=cache(cache_bytes=1))):
@@ -153,7 +153,7 @@ def test_the_binding_checks_tensors():
     with pytest.raises(AssertionError):
         kv8._rows(x.half(), -1)
     with pytest.raises(AssertionError):
-        kv8._rows(x[0], -1)
+        kv8._rows(x[0, 0], -1)
     with pytest.raises(AssertionError):
         kv8._rows(x.transpose(2, 3), -1)     # channels not in a row
     with pytest.raises(AssertionError):
