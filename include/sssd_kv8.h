@@ -122,8 +122,8 @@ int sssd_op_rope(const sssd_rows *x, const sssd_rows *out, int32_t B, int32_t n,
  *   q, q_out both NULL, or with rope: [B][n][n_q_heads][head_dim], q_out = q rotated likewise (rows below counts[b]
  *            only), of one type, which need not be k's; q_out may be q itself
  * n is any (a prompt comes in one call; above max_seq only with counts).  A sequence with lens[b] < 0, lens[b] + counts[b] > max_seq, counts[b] outside
- * 0..n or a page outside the pool for a block it writes is rejected: nothing of it is written, and the status raised; a
- * parent outside [0, j) is treated as j-1 and raises the status.  Sequences of one call must not share a page they write.
+ * 0..n or a page outside the pool for a block it writes is rejected: nothing of it is stored, and the status raised (its
+ * queries are rotated all the same in the last case, and left alone in the others); a parent outside [0, j) is treated as j-1 and raises the status.  Sequences of one call must not share a page they write.
  */
 int sssd_kv8_append(const sssd_kv8 *kv, int32_t layer, int32_t first, int32_t B, int32_t n, const sssd_rows *k,
                     const sssd_rows *v, const int32_t *lens, const int32_t *counts, const sssd_rope *rope,
@@ -141,7 +141,8 @@ int sssd_kv8_read(const sssd_kv8 *kv, int32_t layer, int32_t first, int32_t B, i
  * Attention of n <= 32 new rows of each of the sequences in slots 0 .. B-1, which are in the cache (sssd_kv8_append):
  * softmax(q . k / sqrt(head_dim)) over what a row sees, times v.
  *   q, out   [B][n][n_q_heads][head_dim], of one type; q already rotated.  They must not overlap.  Scores, softmax and sums are
- *            held to 32-bit accuracy for SSSD_F32; for SSSD_BF16 probabilities are rounded to 11 bits
+ *            held to 32-bit accuracy for SSSD_F32; for SSSD_BF16 probabilities are rounded to 11 bits.  Any finite q will do
+ *            whose scores are in float32's range; a row of q that is no finite number spoils its own results alone
  *   lens, counts, parents  as in sssd_kv8_append: row j sees the old rows (below lens[b]) and, of the new ones, itself
  *            and its ancestors
  *   window   0: all of them.  Else those fewer than `window` positions behind the row's own (a new row's position is

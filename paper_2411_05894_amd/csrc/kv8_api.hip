@@ -122,7 +122,9 @@ int sssd_op_rope(const sssd_rows *x, const sssd_rows *out, int32_t B, int32_t n,
     if (make_rows(x, B, n, heads, from) || make_rows(out, B, n, heads, to) || from.bf16 != to.bf16 || !make_rope(rope, head_dim, rp)) return SSSD_EINVAL;
     if (from.p == to.p && (from.bs != to.bs || from.rs != to.rs || from.hs != to.hs)) return SSSD_EINVAL;
     if ((int64_t)B * n > MOST_THREADS / 256) return SSSD_ECAPACITY;
-    HIP_TRY(launch_rope(from, to, positions, rp, rope_work(B, n, head_dim, heads, rp.r, rp.neighbours, 256), (hipStream_t)stream));
+    const RopeWork w = rope_work(B, n, head_dim, heads, rp.r, rp.neighbours, 256);
+    if ((int64_t)((w.total + w.rows - 1) / w.rows) * ((heads + w.per - 1) / w.per) > MOST_THREADS / 256) return SSSD_ECAPACITY;
+    HIP_TRY(launch_rope(from, to, positions, rp, w, (hipStream_t)stream));
     return SSSD_OK;
 }
 
@@ -201,7 +203,9 @@ int sssd_kv8_attention(const sssd_kv8 *kv, int32_t layer, int32_t B, int32_t n, 
     a.codes = (const uint8_t *)kv->cache + (size_t)layer * S.layer_bytes;
     a.scales = (const float2 *)(a.codes + S.scales_at);
     a.B = B; a.n = n; a.gq = c.n_q_heads / c.n_kv_heads;
-    a.lens = lens; a.counts = counts; a.parents = parents; a.window = window; a.sinks = sinks; a.status = kv->status;
+    a.lens = lens; a.counts = counts; a.parents = parents; a.status = kv->status;
+    a.window = window < c.max_seq ? window : 0;   // nothing is farther back
+    a.sinks = sinks < c.max_seq ? sinks : c.max_seq;
     a.hand.polls = kv->flags & SSSD_NO_WAIT ? 0 : HAND_POLLS;
     // a row of queries and a thread each in the merge, at most 32 passes of 256 threads a kv head otherwise
     if ((int64_t)B * c.n_q_heads > MOST_THREADS / (32 * 256)) return SSSD_ECAPACITY;

@@ -7,10 +7,13 @@ namespace {
 
 __device__ __forceinline__ f32x4 mfma16(const half8_t &a, const half8_t &b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
-constexpr float NEG_BIG = -1.0e30f;
+constexpr float NONE = -3.402823466e38f;   // reference of a row that has seen nothing: below every score
 // Probabilities are kept below 2^15 (the largest float16 is 65504): the reference of the exponents is put 2^7 below a row's maximum and
 // follows once the maximum has outgrown it by 2^15.  So they lose no bits to float16's small numbers until they are 2^-21 of the largest.
 constexpr float REF_BELOW = 7.f, REF_MOST = 15.f;
+// From scores of this size on they are rounded before the reference is subtracted: unrounded products of the row's largest could lie above a
+// reference made of a rounded one by more than float16 holds.
+constexpr float HUGE_SCORE = 0x1p20f;
 
 // max / sum over the four lanes 16 apart that share a query row
 __device__ __forceinline__ float rows_max(float x)
@@ -26,6 +29,13 @@ __device__ __forceinline__ float rows_sum(float x)
     x = bits_f32(h[0]) + bits_f32(h[1]);
     h = __builtin_amdgcn_permlane16_swap(f32_bits(x), f32_bits(x), false, false);
     return bits_f32(h[0]) + bits_f32(h[1]);
+}
+
+// A score's distance from the reference, the score rounded on the way as it is where it is huge.
+__device__ __forceinline__ float above(float s, float sc, float m)
+{
+#pragma clang fp contract(off)
+    return s * sc - m;
 }
 
 // max over 8 or 16 neighbouring lanes
@@ -144,7 +154,7 @@ __device__ __forceinline__ void merge_rows(const Kv8AttnArgs &a, int b, int kvh,
     float num[ROWS][E], den[ROWS], m_all[ROWS];
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
-        m_all[i] = NEG_BIG;
+        m_all[i] = NONE;
         if (MANY)
             for (int s = lane; s < n_seg; s += 64) m_all[i] = fmaxf(m_all[i], stats(s, row(i)).x);
         den[i] = 0.f;
@@ -398,9 +408,10 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) o[t][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
         l_run[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-        m_run[t] = NEG_BIG;
+        m_run[t] = NONE;
     }
     const half8_t ones = __builtin_bit_cast(half8_t, u32x4{0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u});
+    bool huge = false;   // some row's reference has been HUGE_SCORE
     const int all_from = a.window > 0 ? len + count - a.window : 0;   // every row sees the old positions from here on
 
     for (int i = 0; i < n_it; ++i) {
@@ -446,10 +457,10 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
         load_k(i + 1);
         const bool whole = t0 + 32 <= len && (t0 >= all_from || t0 + 32 <= a.sinks);   // all rows see all of the block
         float sc[RT], mx[RT];   // mx: of the lane's own eight positions
-        bool grow = false;
+        bool grow = huge;
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
-            sc[t] = row_scale[t] * k_scale;
+            sc[t] = __builtin_amdgcn_fmed3f(row_scale[t] * k_scale, 0x1p-126f, 0x1p127f);   // neither 0 nor infinite: times -INFINITY or 0
             if (!whole) {
                 const uint32_t mine = visible(t0, len, low_s[t * 16 + c], a.sinks, word_s[t * 16 + c]) >> (4 * q);
 #pragma unroll
@@ -458,18 +469,27 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
                     for (int r = 0; r < 4; ++r) s[t][u][r] = mine & (1u << (16 * u + r)) ? s[t][u][r] : -INFINITY;
             }
             mx[t] = max3(max3(s[t][0][0], s[t][0][1], s[t][0][2]), max3(s[t][0][3], s[t][1][0], s[t][1][1]), max3(s[t][1][2], s[t][1][3], s[t][1][3]));
-            grow = grow || mx[t] * sc[t] > m_run[t] + REF_MOST;
+            grow = grow || above(mx[t], sc[t], m_run[t]) > REF_MOST;
         }
         if (__any(grow)) {
 #pragma unroll
             for (int t = 0; t < RT; ++t) {
-                const float m = rows_max(mx[t]) * sc[t];
-                const float m_new = m > m_run[t] + REF_MOST ? m - REF_BELOW : m_run[t], alpha = __builtin_amdgcn_exp2f(m_run[t] - m_new);
+                const float m = rows_max(mx[t]);
+                const float m_new = above(m, sc[t], m_run[t]) > REF_MOST ? above(m, sc[t], REF_BELOW) : m_run[t], alpha = __builtin_amdgcn_exp2f(m_run[t] - m_new);
                 m_run[t] = m_new;
+                huge = huge || __any(fabsf(m_new) >= HUGE_SCORE && m_new != NONE);
                 l_run[t] *= alpha;
 #pragma unroll
                 for (int dt = 0; dt < DT; ++dt) o[t][dt] *= alpha;
             }
+            if (huge)
+#pragma unroll
+                for (int t = 0; t < RT; ++t) {
+                    const bool mine = fabsf(m_run[t]) >= HUGE_SCORE;   // by the row alone: the others change none of its bits
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) s[t][u] = mine ? s[t][u] * sc[t] : s[t][u];
+                    sc[t] = mine ? 1.f : sc[t];
+                }
         }
         // The sums are in units of 2^(v_ref - 127), a V scale: they move to a larger one only when a block's outgrows it by 2^4.
         if (v_e > v_ref + 4) {
@@ -547,7 +567,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
         for (int t = tt; t < tt + TR && t < RT; ++t) {
             const int row = (rt0 + t) * 16 + c;
             float2 s4[NW];
-            float m_all = NEG_BIG;
+            float m_all = NONE;
 #pragma unroll
             for (int i = 0; i < NW; ++i) {
                 s4[i] = ml_s[(wave + i) & (NW - 1)][t * 16 + c];

@@ -163,6 +163,50 @@ def test_a_sharp_and_a_flat_softmax():
         batch.check(torch.float32, q=q)
 
 
+def extreme(keys, channel, q, dtype):
+    """One head whose keys are `keys` in one channel; -> (out, want, sum of p |v|)."""
+    d, n = 64, 4
+    rows = len(keys)
+    cache = kv8.Kv8Cache(1, 2, 1, d, 1, rows, "e4m3", device=DEV)
+    k, v = torch.zeros(1, rows, 1, d, device=DEV), torch.randn(1, rows, 1, d, device=DEV, generator=torch.Generator(device=DEV).manual_seed(17))
+    k[0, :, 0, channel] = torch.tensor(keys, device=DEV)
+    cache.sssd_kv8_append(0, k, v, ints([0]))
+    kk, vv = torch.empty_like(k), torch.empty_like(v)
+    cache.sssd_kv8_read(0, None, None, kk, vv)
+    assert torch.equal(kk, k)                      # the keys are codes
+    qq = torch.zeros(1, n, 2, d, device=DEV)
+    qq[..., 0] = torch.tensor(q, device=DEV)
+    qq = qq.to(dtype)
+    out = torch.zeros_like(qq)
+    cache.sssd_kv8_attention(0, qq, ints([rows - n]), out)
+    assert cache.sssd_kv8_sync() == SSSD_OK
+    want, mass, _ = attend(qq[0], kk[0].double(), vv[0].double(), rows - n)
+    return out[0].double(), want, mass
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_scores_of_every_magnitude(dtype):
+    """Neighbouring keys are a sixteenth of the largest apart, so with scores of 2^11 and more only the largest count, and these are equal: the result is
+    their values' mean, off by the 16 roundings of 2^-24 of the bound above and by those of bf16.  With scores of 0, from whatever scales, it is the
+    mean of all that is seen."""
+    bound = 2.0 ** -20 if dtype == torch.float32 else 2.0 ** -20 + 2.0 ** -11 + torch.finfo(dtype).eps / 2 * (1 + 2.0 ** -10)
+    for sign in (1.0, -1.0):
+        for size in (2.0 ** 10, 2.0 ** 50, 2.0 ** -60):
+            keys = [sign * size * (1 + (7 * i) % 16) for i in range(300)]
+            for score in (2.0 ** 11, 2.0 ** 20, 2.0 ** 24, 2.0 ** 27, 2.0 ** 28, 2.0 ** 29, 2.0 ** 32, 2.0 ** 50, 1.0e30, 1.0e34):
+                q = score / size * 1.2345678
+                if not 1e-37 < q < 1e37:
+                    continue
+                out, want, mass = extreme(keys, 0, q, dtype)
+                assert ((out - want).abs() <= bound * mass).all(), (sign, size, score)
+    for q, size in ((1e-30, 2.0 ** -120), (2e-38, 2.0 ** -126), (1e38, 2.0 ** 126), (1e38, 2.0 ** -126), (1e-37, 2.0 ** 126), (1e-41, 1.0)):
+        out, want, mass = extreme([size * (1 + i % 2) for i in range(75)], 1, q, dtype)
+        assert ((out - want).abs() <= bound * mass).all(), (q, size)
+    for q, size in ((1e-30, 2.0 ** -120), (2e-38, 2.0 ** -126)):
+        out, want, mass = extreme([size * (1 + i % 2) for i in range(75)], 0, q, dtype)
+        assert ((out - want).abs() <= bound * mass).all(), (q, size)
+
+
 def test_numbers_that_are_none():
     """A row of q that is no number spoils its own output alone; the rows that follow a sequence in its last block, and whole pages that nobody
     owns, may hold anything."""
