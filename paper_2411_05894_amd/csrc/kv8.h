@@ -22,6 +22,15 @@ constexpr int KV8_BLOCK = 32;   // positions of a page
 // Bits of the status word
 constexpr int KV8_RANGE = 1, KV8_NOT_FINITE = 2;
 
+// All cache lines of a kernel's arguments requested at once: read where they are used they cost a round trip to memory each, one behind the other.
+template <typename T> __device__ __forceinline__ void warm(const T &args)
+{
+    const uint32_t *p = reinterpret_cast<const uint32_t *>(&args);
+#pragma unroll
+    for (size_t i = 0; i < sizeof(T) / 4; i += 16) asm volatile("" ::"s"(p[i]));
+    asm volatile("" ::"s"(p[sizeof(T) / 4 - 1]));
+}
+
 struct Kv8Geom {
     const int32_t *table;   // device [max_batch][blocks_per_seq], or nullptr: contiguous runs
     int blocks_per_seq, n_pages, nkv, max_seq;
@@ -52,11 +61,30 @@ __device__ __forceinline__ float load1(const Rows8 &r, const char *row, int ch)
 {
     return r.bf16 ? bf16_to_f32(reinterpret_cast<const uint16_t *>(row)[ch]) : reinterpret_cast<const float *>(row)[ch];
 }
+__device__ __forceinline__ void load_pair(const Rows8 &r, const char *row, int i, int j, float &x, float &y)   // neither waits for the other
+{
+    if (r.bf16) {
+        const uint16_t u = reinterpret_cast<const uint16_t *>(row)[i], v = reinterpret_cast<const uint16_t *>(row)[j];
+        x = bf16_to_f32(u);
+        y = bf16_to_f32(v);
+    } else {
+        x = reinterpret_cast<const float *>(row)[i];
+        y = reinterpret_cast<const float *>(row)[j];
+    }
+}
 __device__ __forceinline__ void load8(const Rows8 &r, const char *row, int ch, float (&x)[8])
 {
-    if (!r.vec) {
+    if (!r.vec) {   // one branch on the type for all eight: none of the loads waits for another
+        if (r.bf16) {
+            uint16_t u[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = load1(r, row, ch + i);
+            for (int i = 0; i < 8; ++i) u[i] = reinterpret_cast<const uint16_t *>(row)[ch + i];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = bf16_to_f32(u[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = reinterpret_cast<const float *>(row)[ch + i];
+        }
     } else if (r.bf16) {
         unpack_bf16x8(*reinterpret_cast<const u32x4 *>(row + ch * 2), x);
     } else {
@@ -65,6 +93,34 @@ __device__ __forceinline__ void load8(const Rows8 &r, const char *row, int ch, f
         for (int i = 0; i < 4; ++i) {
             x[i] = lo[i];
             x[4 + i] = hi[i];
+        }
+    }
+}
+// Eight channels as they were loaded, in one or two registers of 16 bytes: turned into numbers only when they are used, so that nothing waits for them
+// before.
+__device__ __forceinline__ void fetch8(const Rows8 &r, const char *row, int ch, u32x4 &lo, u32x4 &hi)
+{
+    if (!r.vec) {
+        float x[8];
+        load8(r, row, ch, x);
+        lo = u32x4{f32_bits(x[0]), f32_bits(x[1]), f32_bits(x[2]), f32_bits(x[3])};
+        hi = u32x4{f32_bits(x[4]), f32_bits(x[5]), f32_bits(x[6]), f32_bits(x[7])};
+    } else if (r.bf16) {
+        lo = *reinterpret_cast<const u32x4 *>(row + ch * 2);
+    } else {
+        lo = *reinterpret_cast<const u32x4 *>(row + ch * 4);
+        hi = *reinterpret_cast<const u32x4 *>(row + ch * 4 + 16);
+    }
+}
+__device__ __forceinline__ void decode8(const Rows8 &r, const u32x4 &lo, const u32x4 &hi, float (&x)[8])
+{
+    if (r.vec && r.bf16) {
+        unpack_bf16x8(lo, x);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[i] = bits_f32(lo[i]);
+            x[4 + i] = bits_f32(hi[i]);
         }
     }
 }
@@ -77,8 +133,13 @@ __device__ __forceinline__ void store1(const Rows8 &r, char *row, int ch, float 
 __device__ __forceinline__ void store8(const Rows8 &r, char *row, int ch, const float (&x)[8])
 {
     if (!r.vec) {
+        if (r.bf16) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) store1(r, row, ch + i, x[i]);
+            for (int i = 0; i < 8; ++i) reinterpret_cast<uint16_t *>(row)[ch + i] = (uint16_t)pack_bf16x2(x[i], 0.f);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) reinterpret_cast<float *>(row)[ch + i] = x[i];
+        }
     } else if (r.bf16) {
         *reinterpret_cast<u32x4 *>(row + ch * 2) = u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
     } else {
@@ -117,6 +178,7 @@ struct Rope8 {
     const double *turns;
     int r, neighbours;
     float magnitude;
+    Div by_half;   // quotients by r / 2
 };
 // cos and sin of 2 pi frac(position * turns), times the magnitude.  The product in 64 bits: at position 10^6 a 32-bit angle is off by 0.06.
 __device__ __forceinline__ void rope_cos_sin(const Rope8 &rp, int position, double turns, float &c, float &s)
@@ -142,6 +204,7 @@ struct Kv8StoreArgs {
     float2 *scales;
     size_t layer_bytes;
     int first, B, n, blocks;   // blocks: of a sequence that a call may touch at most
+    int per, chunks;           // append, read: kv heads of a workgroup, workgroups for all of them
     Rows8 k, v, q, q_out;      // q.p null: no queries
     const int32_t *lens, *counts, *parents;
     Rope8 rope;                // turns null: none
@@ -149,8 +212,8 @@ struct Kv8StoreArgs {
     int32_t *status;
 };
 hipError_t launch_rope(const Rows8 &x, const Rows8 &out, const int32_t *positions, const Rope8 &rope, const RopeWork &w, hipStream_t s);
-hipError_t launch_kv8_append(const Kv8StoreArgs &a, int fmt, int d, hipStream_t s);
-hipError_t launch_kv8_read(const Kv8StoreArgs &a, int fmt, int d, hipStream_t s);
+hipError_t launch_kv8_append(Kv8StoreArgs a, int fmt, int d, hipStream_t s);
+hipError_t launch_kv8_read(Kv8StoreArgs a, int fmt, int d, hipStream_t s);
 hipError_t launch_kv8_commit(const Kv8StoreArgs &a, int fmt, int d, int layers, const int32_t *accepted, const int32_t *path, int32_t *lens, hipStream_t s);
 
 // How the attention's work is cut: `share` segments of a sequence at most, `passes` over the cache for the 16-row tiles of queries.

@@ -71,7 +71,7 @@ bool make_rope(const sssd_rope *r, int head_dim, Rope8 &out)
 {
     if (!r->turns || r->rotary_dims < 2 || r->rotary_dims % 2 || r->rotary_dims > head_dim || r->rotary_dims > 2 * ROPE_TABLE) return false;
     if (r->pairs != SSSD_ROPE_HALVES && r->pairs != SSSD_ROPE_NEIGHBOURS) return false;
-    out = Rope8{r->turns, r->rotary_dims, r->pairs == SSSD_ROPE_NEIGHBOURS, r->magnitude};
+    out = Rope8{r->turns, r->rotary_dims, r->pairs == SSSD_ROPE_NEIGHBOURS, r->magnitude, Div(r->rotary_dims / 2)};
     return true;
 }
 

@@ -5,6 +5,9 @@
 
 namespace {
 
+#ifndef LB
+#define LB 1
+#endif
 // ------------------------------------------------------------------------------------------------ codes ----
 // The scale of a block of largest finite magnitude `most`: the smallest power of two with most <= 448 s or 127 s, at least 2^-126; 1 for
 // none.  From the bits: most = 1.m * 2^(E-127), and 448 = 1.75 * 2^8, 127 = 1.984375 * 2^6.
@@ -48,6 +51,20 @@ template <int FMT> __device__ __forceinline__ u32x4 row_codes(const float (&x)[8
                  to_codes<FMT>(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv), to_codes<FMT>(y[4] * inv, y[5] * inv, y[6] * inv, y[7] * inv)};
 }
 template <int FMT> constexpr float largest_code() { return FMT == SSSD_KV8_E4M3 ? 448.f : 127.f; }
+
+// What a workgroup of an append or a read is there for (the same for all lanes, which a quotient hides from the compiler: it would load lens and pages
+// lane by lane).
+struct StorePlace {
+    int b, step, h0, h1;
+    __device__ __forceinline__ StorePlace(const Kv8StoreArgs &a, int id)
+    {
+        const int x = __builtin_amdgcn_readfirstlane((uint32_t)id / (uint32_t)a.chunks);
+        h0 = (id - x * a.chunks) * a.per;
+        h1 = min(h0 + a.per, a.g.nkv);
+        b = __builtin_amdgcn_readfirstlane((uint32_t)x / (uint32_t)a.blocks);
+        step = x - b * a.blocks;
+    }
+};
 
 // Largest magnitude over a workgroup of 2 * HD threads.
 template <int HD> __device__ __forceinline__ float group_max(float x, float *most_s)
@@ -123,49 +140,58 @@ template <int HD> __device__ __forceinline__ u32x4 *block_record(uint8_t *codes,
 }
 
 // ------------------------------------------------------------------------------------------------- rope ----
-// Channels ch .. ch+7 of a row, rotated.  `x` holds them as they are.
-__device__ __forceinline__ void rotate8(const Rope8 &rp, const Rows8 &r, const char *row, int ch, int position, float (&x)[8])
+// Both runs of a Place rotated, of a head that is rotated as a whole: by halves they are each other's partners, and neighbours lie in a run.  own: cos
+// and sin of two of the thread's eight angles, T apart.
+template <typename Angle> __device__ __forceinline__ void rotate_whole(bool neighbours, Angle angle, float (&x)[8], float (&y)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        float &a = neighbours ? (i < 4 ? x[2 * i & 7] : y[2 * i & 7]) : x[i];
+        float &b = neighbours ? (i < 4 ? x[(2 * i & 7) + 1] : y[(2 * i & 7) + 1]) : y[i];
+        const float2 t = angle(i);
+        const float u = a;
+        a = u * t.x - b * t.y;
+        b = b * t.x + u * t.y;
+    }
+}
+// ... of a head whose first channels are.  cs: the angles of the row's pairs.  By halves the partners are fetched again (they are in a cache: another
+// thread of the workgroup has just read them).
+template <int HD>
+__device__ __forceinline__ void rotate_part(const Rope8 &rp, const Rows8 &r, const char *row, int c0, const float2 *cs, float (&x)[8], float (&y)[8])
 {
     const int half = rp.r >> 1;
-    if (rp.neighbours) {
+    auto run = [&](int ch, float (&v)[8]) {
+        if (ch >= rp.r) return;
+        if (rp.neighbours) {
 #pragma unroll
-        for (int i = 0; i < 8; i += 2)
-            if (ch + i < rp.r) {
-                float c, s;
-                rope_cos_sin(rp, position, rp.turns[(ch + i) >> 1], c, s);
-                const float a = x[i], b = x[i + 1];
-                x[i] = a * c - b * s;
-                x[i + 1] = b * c + a * s;
-            }
-        return;
-    }
+            for (int i = 0; i < 8; i += 2)
+                if (ch + i < rp.r) {
+                    const float2 t = cs[(ch + i) >> 1];
+                    const float u = v[i];
+                    v[i] = u * t.x - v[i + 1] * t.y;
+                    v[i + 1] = v[i + 1] * t.x + u * t.y;
+                }
+        } else if (half % 8 == 0) {
+            const bool low = ch < half;
+            float other[8];
+            load8(r, row, low ? ch + half : ch - half, other);
+            cs += low ? ch : ch - half;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (ch + i < rp.r) {
-            const bool low = ch + i < half;
-            float c, s;
-            rope_cos_sin(rp, position, rp.turns[low ? ch + i : ch + i - half], c, s);
-            const float other = load1(r, row, low ? ch + i + half : ch + i - half);
-            x[i] = low ? x[i] * c - other * s : x[i] * c + other * s;
+            for (int i = 0; i < 8; ++i) v[i] = low ? v[i] * cs[i].x - other[i] * cs[i].y : v[i] * cs[i].x + other[i] * cs[i].y;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (ch + i < rp.r) {
+                    const bool low = ch + i < half;
+                    const float2 t = cs[low ? ch + i : ch + i - half];
+                    const float other = load1(r, row, low ? ch + i + half : ch + i - half);
+                    v[i] = low ? v[i] * t.x - other * t.y : v[i] * t.x + other * t.y;
+                }
         }
-}
-// ... of both runs of a Place, which are each other's pairs where the whole head is rotated by halves.
-template <int HD>
-__device__ __forceinline__ void rotate_place(const Rope8 &rp, const Rows8 &r, const char *row, int c0, int position, float (&x)[8], float (&y)[8])
-{
-    if (!rp.neighbours && rp.r == HD) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            float c, s;
-            rope_cos_sin(rp, position, rp.turns[c0 + i], c, s);
-            const float a = x[i], b = y[i];
-            x[i] = a * c - b * s;
-            y[i] = b * c + a * s;
-        }
-    } else {
-        rotate8(rp, r, row, c0, position, x);
-        rotate8(rp, r, row, c0 + HD / 2, position, y);
-    }
+    };
+    asm volatile("" : "+v"(c0));   // addresses and angles anew for every head: kept over the loop, they would take a hundred registers
+    run(c0, x);
+    run(c0 + HD / 2, y);
 }
 
 // Rows of heads rotated by a workgroup of T threads: R rows, heads h0 .. h1-1 of each.  The angles of the rows' pairs are worked out once, in LDS
@@ -233,9 +259,16 @@ __device__ __forceinline__ void rope_units(const Rope8 &rp, const Rows8 &x, cons
         } else {   // a pair
             const int other = halves ? ch + half : ch + 1;
             const float2 t = cs[halves ? ch : ch >> 1];
-            const float u = load1(x, src, ch), y = load1(x, src, other);
-            store1(out, dst, ch, u * t.x - y * t.y);
-            store1(out, dst, other, y * t.x + u * t.y);
+            float u, y;
+            load_pair(x, src, ch, other, u, y);
+            const float v = u * t.x - y * t.y, w = y * t.x + u * t.y;
+            if (out.bf16) {
+                reinterpret_cast<uint16_t *>(dst)[ch] = (uint16_t)pack_bf16x2(v, 0.f);
+                reinterpret_cast<uint16_t *>(dst)[other] = (uint16_t)pack_bf16x2(w, 0.f);
+            } else {
+                reinterpret_cast<float *>(dst)[ch] = v;
+                reinterpret_cast<float *>(dst)[other] = w;
+            }
         }
     }
 }
@@ -247,7 +280,7 @@ __device__ __forceinline__ void rope_rows(const Rope8 &rp, const Rows8 &x, const
     if ((int)threadIdx.x < rows) rows_s[threadIdx.x] = row(row0 + threadIdx.x);
     __syncthreads();
     for (int i = threadIdx.x; i < rows * half; i += T) {
-        const int r = i / half;
+        const int r = rp.by_half(i);
         rope_cos_sin(rp, rows_s[r].position, rp.turns[i - r * half], table[i].x, table[i].y);
     }
     __syncthreads();
@@ -288,9 +321,18 @@ template <int T> __device__ __forceinline__ int touched_page(const Kv8StoreArgs 
     if (count == 0 || blk0 + step > last) return -1;
     if (a.g.table) {
         bool bad = false;
-        for (int i = blk0 + (int)threadIdx.x; i <= last; i += T) {
-            const int page = kv8_entry(a.g, a.first + b, i);
-            bad |= page < 0 || page >= a.g.n_pages;
+        const int32_t *entries = a.g.table + (size_t)(a.first + b) * a.g.blocks_per_seq + blk0;
+        const int n = last - blk0 + 1;
+        for (int i = (int)threadIdx.x * 4; i < n; i += T * 4) {   // four at a time, the last four once more
+            int32_t four[4];
+            if (n >= 4) {
+                __builtin_memcpy(four, entries + min(i, n - 4), sizeof(four));
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) four[e] = entries[min(e, n - 1)];
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) bad |= (uint32_t)four[e] >= (uint32_t)a.g.n_pages;
         }
         if (__syncthreads_or(bad)) {
             if (tell && step == 0 && threadIdx.x == 0) atomicOr(a.status, KV8_RANGE);
@@ -301,19 +343,20 @@ template <int T> __device__ __forceinline__ int touched_page(const Kv8StoreArgs 
 }
 
 // ----------------------------------------------------------------------------------------------- append ----
-// Workgroup = (sequence, touched block, kv head, K or V); behind them the workgroups that rotate queries.
-template <int HD, int FMT> __global__ __launch_bounds__(2 * HD) void append_kernel(Kv8StoreArgs a, int store_groups)
+// Workgroup = (sequence, touched block, `per` kv heads, K or V), MANY: more than one; behind them the workgroups that rotate queries.
+template <int HD, int FMT, bool MANY> __global__ __launch_bounds__(2 * HD, LB) void append_kernel(Kv8StoreArgs a, int storing)
 {
-    constexpr int T = 2 * HD;
-    __shared__ float most_s[HD / 32];
+    constexpr int T = 2 * HD, PITCH = HD / 2 + 2;
+    __shared__ float most_s[2][HD / 32];
     __shared__ __align__(16) uint8_t turn_s[32 * Turn<HD>::PITCH];
-    __shared__ float2 table[ROPE_ROWS * HD / 2];
+    __shared__ __align__(16) float2 table[32 * PITCH];   // angles of the block's rows, or of a workgroup's rows of queries
     __shared__ RopeRow rows_s[ROPE_ROWS];
+    warm(a);
     const int lane = threadIdx.x & 63;
     int id = blockIdx.x;
     int len, count;
-    if (id >= store_groups) {
-        id -= store_groups;
+    if (id >= storing) {
+        id -= storing;
         const int groups = (int)((a.work.total + a.work.rows - 1) / a.work.rows), chunk = id / groups;
         rope_rows<T>(a.rope, a.q, a.q_out, a.work, id - chunk * groups, chunk, table, rows_s, [&](uint32_t row) {
             RopeRow r;
@@ -337,69 +380,131 @@ template <int HD, int FMT> __global__ __launch_bounds__(2 * HD) void append_kern
     }
     const int is_v = id & 1;
     id >>= 1;
-    const int x0 = (uint32_t)id / (uint32_t)a.g.nkv, h = id - x0 * a.g.nkv, b = (uint32_t)x0 / (uint32_t)a.blocks, step = x0 - b * a.blocks;
-    const int page = touched_page<T>(a, b, step, h == 0 && !is_v, len, count);
+    const StorePlace w(a, id);
+    const int b = w.b, step = w.step, h0 = w.h0, h1 = w.h1;
+    const Place<HD> at;
+    const bool turns = !is_v && a.rope.turns, whole = a.rope.r == HD;
+    double mine[8];   // the frequencies of the thread's angles, requested ahead of what depends on lens
+    if (turns && whole) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) mine[i] = a.rope.turns[a.rope.neighbours ? (at.c >> 1) + (i & 3) + (i >> 2) * (HD / 4) : at.c + i];
+    }
+    const int page = touched_page<T>(a, b, step, h0 == 0 && !is_v, len, count);
     if (page < 0) return;
     const int blk = (len >> 5) + step;
-    const Place<HD> at;
-    const int t = blk * 32 + at.row, j = t - len;
+    const int j = blk * 32 + at.row - len;
     const Rows8 &in = is_v ? a.v : a.k;
-    float x[8], y[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = y[i] = 0.f;
-    float *scale = reinterpret_cast<float *>(a.scales + (size_t)page * a.g.nkv + h) + is_v;
-    u32x4 *record = block_record<HD>(a.codes, page, a.g.nkv, h, is_v);
     const bool is_new = j >= 0 && j < count;
-    const char *row = in.at(b, is_new ? j : 0, h);
-    if (is_new) {
-        load8(in, row, at.c, x);
-        load8(in, row, at.c + HD / 2, y);
-    }
-    if (blk * 32 < len) {   // the block holds older rows
-        u32x4 old = *record;
-        const float s = *scale;
-        if (is_v) {
-            old = Turn<HD>::rows(old, turn_s, at);
-            __syncthreads();   // turn_s is used again
+    const char *row = in.at(b, is_new ? j : 0, h0);
+    const int64_t next = in.hs * (in.bf16 ? 2 : 4);
+    // A head's rows, and what the block holds of it, are requested while the one before it is stored.
+    const bool holds = blk * 32 < len;   // older rows
+    u32x4 raw[4], old{};
+    float s_old = 0.f;
+    auto scale_of = [&](int h) { return reinterpret_cast<float *>(a.scales + (size_t)page * a.g.nkv + h) + is_v; };
+    auto fetch = [&](int h, const char *from) {
+        if (holds) {
+            old = *block_record<HD>(a.codes, page, a.g.nkv, h, is_v);
+            s_old = *scale_of(h);
         }
-        if (j < 0) {
-            from_codes<FMT>(old[0], s, x);
-            from_codes<FMT>(old[1], s, x + 4);
-            from_codes<FMT>(old[2], s, y);
-            from_codes<FMT>(old[3], s, y + 4);
+        if (is_new) {
+            fetch8(in, from, at.c, raw[0], raw[1]);
+            fetch8(in, from, at.c + HD / 2, raw[2], raw[3]);
         }
-    }
-    if (!is_v && a.rope.turns) {
-        int dep = j;
+    };
+#pragma unroll
+    for (int i = 0; i < 4; ++i) raw[i] = u32x4{0, 0, 0, 0};
+    fetch(h0, row);
+    // Angles once for all heads, in LDS (in registers they would leave fewer waves): a thread its own eight, or, of a head that is rotated in part, all
+    // threads those of the block's rows between them.  us of a prompt of 32768 in 8 heads of 128: angles for every head anew 71, once 48.
+    f32x4 *own = reinterpret_cast<f32x4 *>(table) + threadIdx.x;   // cos and sin of two angles at own[T * i]
+    float2 here[8];                                                // ... of one head alone
+    auto angle = [&](int i) {
+        if (!MANY) return here[i];
+        const f32x4 t = own[T * (i >> 1)];
+        return float2{t[2 * (i & 1)], t[2 * (i & 1) + 1]};
+    };
+    if (turns) {
+        uint32_t word = 0;
         if (a.parents) {
             bool bad;
-            const uint32_t word = kv8_tree_word(lane < count ? a.parents[(size_t)b * a.n + lane] : 0, count, lane, bad);
-            if (step == 0 && h == 0 && threadIdx.x < 64 && __any(bad) && lane == 0) atomicOr(a.status, KV8_RANGE);
-            dep = __popc((uint32_t)__shfl((int)word, j & 31)) - 1;
+            word = kv8_tree_word(lane < count ? a.parents[(size_t)b * a.n + lane] : 0, count, lane, bad);
+            if (step == 0 && h0 == 0 && threadIdx.x < 64 && __any(bad) && lane == 0) atomicOr(a.status, KV8_RANGE);
         }
-        if (is_new) rotate_place<HD>(a.rope, in, row, at.c, len + dep, x, y);
-    }
-    float most = 0.f;
-    bool odd = false;
+        auto position = [&](int j) { return len + (a.parents ? __popc((uint32_t)__shfl((int)word, j & 31)) - 1 : j); };
+        if (whole) {
+            const int p = position(j);
+            if (!MANY) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        most = fmaxf(most, fmaxf(finite(x[i]) ? fabsf(x[i]) : 0.f, finite(y[i]) ? fabsf(y[i]) : 0.f));
-        odd |= !finite(x[i]) || !finite(y[i]);
+                for (int i = 0; i < 8; ++i) rope_cos_sin(a.rope, p, mine[i], here[i].x, here[i].y);
+            } else if (is_new) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float c0, s0, c1, s1;
+                    rope_cos_sin(a.rope, p, mine[2 * i], c0, s0);
+                    rope_cos_sin(a.rope, p, mine[2 * i + 1], c1, s1);
+                    own[T * i] = f32x4{c0, s0, c1, s1};
+                }
+            }
+        } else {
+            const int first = max(len - blk * 32, 0), half = a.rope.r >> 1, all = (min(len + count - blk * 32, 32) - first) * half;
+#pragma unroll 1
+            for (int base = 0; base < all; base += T) {
+                const int e = min(base + (int)threadIdx.x, all - 1), r = a.rope.by_half(e), i = e - r * half;
+                float2 t;
+                rope_cos_sin(a.rope, position(blk * 32 + first + r - len), a.rope.turns[i], t.x, t.y);
+                table[(first + r) * PITCH + i] = t;
+            }
+            __syncthreads();
+        }
     }
-    const float s = block_scale<FMT>(group_max<HD>(most, most_s)), inv = bits_f32((254u << 23) - f32_bits(s));
-    if (__any(odd)) {
-        if (lane == 0) atomicOr(a.status, KV8_NOT_FINITE);
-        const float top = largest_code<FMT>() * s;
-        auto mend = [&](float z) { return finite(z) ? z : z != z ? 0.f : copysignf(top, z); };
+    int h = h0;
+    do {
+        float x[8], y[8];
+        decode8(in, raw[0], raw[1], x);
+        decode8(in, raw[2], raw[3], y);
+        if (holds) {
+            if (is_v) {
+                if (MANY && h > h0) __syncthreads();   // turn_s has been read
+                old = Turn<HD>::rows(old, turn_s, at);
+                __syncthreads();   // ... again
+            }
+            if (j < 0) {
+                from_codes<FMT>(old[0], s_old, x);
+                from_codes<FMT>(old[1], s_old, x + 4);
+                from_codes<FMT>(old[2], s_old, y);
+                from_codes<FMT>(old[3], s_old, y + 4);
+            }
+        }
+        if (turns && is_new) {
+            if (!whole) rotate_part<HD>(a.rope, in, row, at.c, table + at.row * PITCH, x, y);
+            else if (a.rope.neighbours) rotate_whole(true, angle, x, y);
+            else rotate_whole(false, angle, x, y);
+        }
+        if (MANY && h + 1 < h1) fetch(h + 1, row + next);
+        float most = 0.f;
+        bool odd = false;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            x[i] = mend(x[i]);
-            y[i] = mend(y[i]);
+            most = fmaxf(most, fmaxf(finite(x[i]) ? fabsf(x[i]) : 0.f, finite(y[i]) ? fabsf(y[i]) : 0.f));
+            odd |= !finite(x[i]) || !finite(y[i]);
         }
-    }
-    const u32x4 mine = row_codes<FMT>(x, y, inv);
-    *record = is_v ? Turn<HD>::record(mine, turn_s, at) : mine;
-    if (threadIdx.x == 0) *scale = s;
+        const float s = block_scale<FMT>(group_max<HD>(most, most_s[h & 1])), inv = bits_f32((254u << 23) - f32_bits(s));
+        if (__any(odd)) {
+            if (lane == 0) atomicOr(a.status, KV8_NOT_FINITE);
+            const float top = largest_code<FMT>() * s;
+            auto mend = [&](float z) { return finite(z) ? z : z != z ? 0.f : copysignf(top, z); };
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                x[i] = mend(x[i]);
+                y[i] = mend(y[i]);
+            }
+        }
+        const u32x4 mine = row_codes<FMT>(x, y, inv);
+        *block_record<HD>(a.codes, page, a.g.nkv, h, is_v) = is_v ? Turn<HD>::record(mine, turn_s, at) : mine;   // the next head's codes come behind the barrier of its maximum
+        if (threadIdx.x == 0) *scale_of(h) = s;
+        row += next;
+    } while (MANY && ++h < h1);
 }
 
 // ------------------------------------------------------------------------------------------------- read ----
@@ -409,27 +514,40 @@ template <int HD, int FMT> __global__ __launch_bounds__(2 * HD) void read_kernel
     int id = blockIdx.x;
     const int is_v = id & 1;
     id >>= 1;
-    const int x0 = (uint32_t)id / (uint32_t)a.g.nkv, h = id - x0 * a.g.nkv, b = (uint32_t)x0 / (uint32_t)a.blocks, step = x0 - b * a.blocks;
+    const StorePlace w(a, id);
+    const int b = w.b, step = w.step, h0 = w.h0, h1 = w.h1;
     int start, count;
-    const int page = touched_page<2 * HD>(a, b, step, h == 0 && !is_v, start, count);
+    const int page = touched_page<2 * HD>(a, b, step, h0 == 0 && !is_v, start, count);
     if (page < 0) return;
     const int blk = (start >> 5) + step;
     const Place<HD> at;
-    u32x4 rec = *block_record<HD>(a.codes, page, a.g.nkv, h, is_v);
-    const float2 both = a.scales[(size_t)page * a.g.nkv + h];
-    const float s = is_v ? both.y : both.x;
-    if (is_v) rec = Turn<HD>::rows(rec, turn_s, at);
     const int j = blk * 32 + at.row - start;
-    if (j < 0 || j >= count) return;
-    float x[8], y[8];
-    from_codes<FMT>(rec[0], s, x);
-    from_codes<FMT>(rec[1], s, x + 4);
-    from_codes<FMT>(rec[2], s, y);
-    from_codes<FMT>(rec[3], s, y + 4);
+    const bool wanted = j >= 0 && j < count;
     const Rows8 &out = is_v ? a.v : a.k;
-    char *row = out.at(b, j, h);
-    store8(out, row, at.c, x);
-    store8(out, row, at.c + HD / 2, y);
+    char *row = out.at(b, wanted ? j : 0, h0);
+    const float *scale = reinterpret_cast<const float *>(a.scales + (size_t)page * a.g.nkv) + is_v;
+    u32x4 rec = *block_record<HD>(a.codes, page, a.g.nkv, h0, is_v);
+    float s = scale[2 * h0];
+    for (int h = h0; h < h1; ++h, row += out.hs * (out.bf16 ? 2 : 4)) {
+        const int ahead = min(h + 1, h1 - 1);
+        const u32x4 rec_next = *block_record<HD>(a.codes, page, a.g.nkv, ahead, is_v);
+        const float s_next = scale[2 * ahead];
+        if (is_v) {
+            if (h > h0) __syncthreads();   // turn_s has been read
+            rec = Turn<HD>::rows(rec, turn_s, at);
+        }
+        if (wanted) {
+            float x[8], y[8];
+            from_codes<FMT>(rec[0], s, x);
+            from_codes<FMT>(rec[1], s, x + 4);
+            from_codes<FMT>(rec[2], s, y);
+            from_codes<FMT>(rec[3], s, y + 4);
+            store8(out, row, at.c, x);
+            store8(out, row, at.c + HD / 2, y);
+        }
+        rec = rec_next;
+        s = s_next;
+    }
 }
 
 // ----------------------------------------------------------------------------------------------- commit ----
@@ -561,31 +679,51 @@ hipError_t launch_rope(const Rows8 &x, const Rows8 &out, const int32_t *position
     return hipGetLastError();
 }
 
-#define KV8_LAUNCH(kernel, grid, ...)                                                                                                \
-    do {                                                                                                                             \
-        if (d == 128 && fmt == SSSD_KV8_E4M3) hipLaunchKernelGGL((kernel<128, SSSD_KV8_E4M3>), dim3(grid), dim3(256), 0, s, __VA_ARGS__); \
-        else if (d == 128) hipLaunchKernelGGL((kernel<128, SSSD_KV8_INT8>), dim3(grid), dim3(256), 0, s, __VA_ARGS__);               \
-        else if (fmt == SSSD_KV8_E4M3) hipLaunchKernelGGL((kernel<64, SSSD_KV8_E4M3>), dim3(grid), dim3(128), 0, s, __VA_ARGS__);    \
-        else hipLaunchKernelGGL((kernel<64, SSSD_KV8_INT8>), dim3(grid), dim3(128), 0, s, __VA_ARGS__);                              \
+#define KV8_LAUNCH(kernel, grid, ...)                                                                          \
+    do {                                                                                                       \
+        if (d == 128 && fmt == SSSD_KV8_E4M3) KV8_LAUNCH_AS((kernel(128, SSSD_KV8_E4M3)), 256, grid, __VA_ARGS__); \
+        else if (d == 128) KV8_LAUNCH_AS((kernel(128, SSSD_KV8_INT8)), 256, grid, __VA_ARGS__);                \
+        else if (fmt == SSSD_KV8_E4M3) KV8_LAUNCH_AS((kernel(64, SSSD_KV8_E4M3)), 128, grid, __VA_ARGS__);     \
+        else KV8_LAUNCH_AS((kernel(64, SSSD_KV8_INT8)), 128, grid, __VA_ARGS__);                               \
     } while (0)
+#define KV8_LAUNCH_AS(kernel, threads, grid, ...) hipLaunchKernelGGL(kernel, dim3(grid), dim3(threads), 0, s, __VA_ARGS__)
+#define APPEND_ONE(HD, FMT) append_kernel<HD, FMT, false>
+#define APPEND_MANY(HD, FMT) append_kernel<HD, FMT, true>
+#define READ(HD, FMT) read_kernel<HD, FMT>
+#define COMMIT(HD, FMT) commit_kernel<HD, FMT>
 
-hipError_t launch_kv8_append(const Kv8StoreArgs &a, int fmt, int d, hipStream_t s)
+// Workgroups of an append or a read, each of `per` kv heads while 800 are left: what is the same for all heads, the angles and the look at every page of
+// the sequence, is then done once.  us, one head / several: prompts in 8 heads of 128 with a rotation, 4001 13.9 / 11.5 (two), 8192 22.5 / 17.8 (four),
+// 32768 71 / 53 (eight, and with a block table 93 / 57); 16 prompts of 512 22.7 / 17.7; fewer workgroups, 4001 12.4 (three), 8192 21.5 (eight).
+// Reads have the pages alone: with a table, 100001 216 / 153 (four), 32768 56 / 51; without one 45 / 48.
+static int store_groups(Kv8StoreArgs &a, int most)
 {
-    const int store = a.B * a.blocks * a.g.nkv * 2;
+    const int64_t all = (int64_t)a.B * a.blocks * 2 * a.g.nkv, per = all / 800;
+    if (most > a.g.nkv) most = a.g.nkv;
+    a.per = per < 1 ? 1 : per > most ? most : (int)per;
+    a.chunks = (a.g.nkv + a.per - 1) / a.per;
+    a.per = (a.g.nkv + a.chunks - 1) / a.chunks;
+    return a.B * a.blocks * 2 * a.chunks;
+}
+
+hipError_t launch_kv8_append(Kv8StoreArgs a, int fmt, int d, hipStream_t s)
+{
+    const int store = store_groups(a, 8);
     const int turn = a.q.p ? (int)((a.work.total + a.work.rows - 1) / a.work.rows) * ((a.work.heads + a.work.per - 1) / a.work.per) : 0;
-    KV8_LAUNCH(append_kernel, store + turn, a, store);
+    if (a.per > 1) KV8_LAUNCH(APPEND_MANY, store + turn, a, store);
+    else KV8_LAUNCH(APPEND_ONE, store + turn, a, store);
     return hipGetLastError();
 }
 
-hipError_t launch_kv8_read(const Kv8StoreArgs &a, int fmt, int d, hipStream_t s)
+hipError_t launch_kv8_read(Kv8StoreArgs a, int fmt, int d, hipStream_t s)
 {
-    KV8_LAUNCH(read_kernel, a.B * a.blocks * a.g.nkv * 2, a);
+    KV8_LAUNCH(READ, store_groups(a, a.g.table ? 4 : 1), a);
     return hipGetLastError();
 }
 
 hipError_t launch_kv8_commit(const Kv8StoreArgs &a, int fmt, int d, int layers, const int32_t *accepted, const int32_t *path, int32_t *lens, hipStream_t s)
 {
-    if (path) KV8_LAUNCH(commit_kernel, layers * a.B * a.g.nkv * 2, a, accepted, path);
+    if (path) KV8_LAUNCH(COMMIT, layers * a.B * a.g.nkv * 2, a, accepted, path);
     hipLaunchKernelGGL(advance_kernel, dim3(a.B), dim3(64), 0, s, a, accepted, path, lens);
     return hipGetLastError();
 }

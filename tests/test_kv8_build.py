@@ -21,11 +21,11 @@ def test_registers_of_the_attention_kernels(tmp_path):
 
 
 def test_registers_of_the_store_kernels(tmp_path):
-    """Rows of a prompt are many small workgroups: six waves a SIMD at least."""
+    """Rows of a prompt are many small workgroups: five waves a SIMD for an append of several heads a workgroup, six for the others."""
     found = kernels("kv8_store", tmp_path)
-    assert len(found) == 4 + 4 + 4 + 1 + 1              # append, read, commit by channels and format; the advance of lens, the rotation
+    assert len(found) == 8 + 4 + 4 + 1 + 1              # append by channels, format, one head or several; read, commit; the advance of lens, the rotation
     for k, (registers, spilled, scratch) in found.items():
-        assert registers <= 80 and spilled == 0 and scratch == 0, (k, registers, spilled, scratch)
+        assert registers <= (96 if "append_kernel" in k and "Lb1" in k else 80) and spilled == 0 and scratch == 0, (k, registers, spilled, scratch)
 
 
 def _compile(job):
