@@ -3,6 +3,7 @@ marshalling only.  Tensors may have any strides as long as a head's channels lie
 from __future__ import annotations
 
 import ctypes as C
+import struct
 from typing import Optional
 
 import torch
@@ -23,11 +24,6 @@ class Kv8(C.Structure):
                 ("ws_bytes", C.c_size_t), ("block_table", C.c_void_p), ("status", C.c_void_p), ("flags", C.c_uint32)]
 
 
-class Rows(C.Structure):
-    _fields_ = [("data", C.c_void_p), ("type", C.c_int32), ("batch_stride", C.c_int64), ("row_stride", C.c_int64),
-                ("head_stride", C.c_int64)]
-
-
 class RopeConfig(C.Structure):
     _fields_ = [("rotary_dims", C.c_int32), ("base", C.c_float), ("scaling", C.c_int32), ("factor", C.c_float), ("low", C.c_float),
                 ("high", C.c_float), ("original", C.c_int32)]
@@ -37,6 +33,7 @@ class RopeArgs(C.Structure):
     _fields_ = [("turns", C.c_void_p), ("rotary_dims", C.c_int32), ("pairs", C.c_int32), ("magnitude", C.c_float)]
 
 
+ROWS = struct.Struct("@Piqqq").pack      # sssd_rows as bytes: half the time of a ctypes structure
 _bound = None
 
 
@@ -45,27 +42,29 @@ def _lib() -> C.CDLL:
     if _bound is None:
         l = lib()
         vp, i32, p = C.c_void_p, C.c_int32, C.POINTER
+        rows = vp                                # bytes, or NULL
         l.sssd_kv8_sizes.argtypes = [p(Kv8Config), p(C.c_size_t), p(C.c_size_t), p(i32), p(i32)]
         l.sssd_rope_frequencies.argtypes = [p(RopeConfig), p(C.c_double)]
-        l.sssd_op_rope.argtypes = [p(Rows), p(Rows), i32, i32, i32, i32, vp, p(RopeArgs), vp]
-        l.sssd_kv8_append.argtypes = [p(Kv8), i32, i32, i32, i32, p(Rows), p(Rows), vp, vp, p(RopeArgs), vp, p(Rows), p(Rows), vp]
-        l.sssd_kv8_read.argtypes = [p(Kv8), i32, i32, i32, i32, vp, vp, p(Rows), p(Rows), vp]
-        l.sssd_kv8_attention.argtypes = [p(Kv8), i32, i32, i32, p(Rows), p(Rows), vp, vp, vp, i32, i32, vp]
+        l.sssd_op_rope.argtypes = [rows, rows, i32, i32, i32, i32, vp, p(RopeArgs), vp]
+        l.sssd_kv8_append.argtypes = [p(Kv8), i32, i32, i32, i32, rows, rows, vp, vp, p(RopeArgs), vp, rows, rows, vp]
+        l.sssd_kv8_read.argtypes = [p(Kv8), i32, i32, i32, i32, vp, vp, rows, rows, vp]
+        l.sssd_kv8_attention.argtypes = [p(Kv8), i32, i32, i32, rows, rows, vp, vp, vp, i32, i32, vp]
         l.sssd_kv8_commit_tree.argtypes = [p(Kv8), i32, i32, vp, vp, vp, vp]
         l.sssd_kv8_sync.argtypes = [p(Kv8), vp]
         _bound = l
     return _bound
 
 
-def _rows(t: torch.Tensor, device: int) -> Rows:
+def _rows(t: torch.Tensor, device: int) -> bytes:
     """[B][n][heads][channels], or [n][heads][channels], as the C ABI takes them; device: the number of the GPU, -1 for none."""
     stride = t.stride()
-    assert len(stride) in (3, 4) and t.dtype in TYPES, "rows are [B][n][heads][head_dim], float32 or bfloat16"
+    kind = TYPES.get(t.dtype)
+    assert kind is not None and len(stride) in (3, 4), "rows are [B][n][heads][head_dim], float32 or bfloat16"
     assert t.get_device() == device, f"rows on {t.device}, the cache (or the frequencies) on GPU {device}"
     assert stride[-1] == 1 or t.shape[-1] == 1, "a head's channels must lie in a row"
     if len(stride) == 3:
-        return Rows(t.data_ptr(), TYPES[t.dtype], 0, stride[0], stride[1])
-    return Rows(t.data_ptr(), TYPES[t.dtype], stride[0], stride[1], stride[2])
+        return ROWS(t.data_ptr(), kind, 0, stride[0], stride[1])
+    return ROWS(t.data_ptr(), kind, stride[0], stride[1], stride[2])
 
 
 def _ints(t: Optional[torch.Tensor], shape, device: int) -> Optional[int]:
@@ -77,7 +76,7 @@ def _ints(t: Optional[torch.Tensor], shape, device: int) -> Optional[int]:
 
 def _enqueue(call, device: int, *args) -> None:
     """The call on the current stream of `device`, whichever device is the current one."""
-    if torch.cuda.current_device() == device:
+    if torch._C._cuda_getDevice() == device:
         code = call(*args, torch._C._cuda_getCurrentRawStream(device))
     else:
         with torch.cuda.device(device):
@@ -117,7 +116,7 @@ def sssd_op_rope(x: torch.Tensor, positions: torch.Tensor, rope: Rope, out: Opti
     assert out.shape == x.shape and out.dtype == x.dtype
     shape = x.shape
     B, n = shape[:2] if len(shape) == 4 else (1, shape[0])
-    _enqueue(_lib().sssd_op_rope, rope.device, C.byref(_rows(x, rope.device)), C.byref(_rows(out, rope.device)), B, n, shape[-2], shape[-1],
+    _enqueue(_lib().sssd_op_rope, rope.device, _rows(x, rope.device), _rows(out, rope.device), B, n, shape[-2], shape[-1],
              _ints(positions, shape[:-2], rope.device), rope.ref)
     return out
 
@@ -127,6 +126,7 @@ class Kv8Cache:
 
     def __init__(self, n_layers: int, n_q_heads: int, n_kv_heads: int, head_dim: int, max_batch: int, max_seq: int, fmt: str = "e4m3",
                  n_pages: int = 0, device: str = "cuda:0", no_wait: bool = False):
+        self.n_q_heads, self.n_kv_heads, self.head_dim = n_q_heads, n_kv_heads, head_dim
         self.cfg = Kv8Config(FORMATS[fmt], n_layers, n_q_heads, n_kv_heads, head_dim, max_batch, max_seq, n_pages)
         cache_bytes, ws_bytes, self.blocks_per_seq, self.n_pages = sssd_kv8_sizes(self.cfg)
         self.cache = torch.zeros(cache_bytes, dtype=torch.uint8, device=device)
@@ -138,9 +138,9 @@ class Kv8Cache:
                         SSSD_NO_WAIT if no_wait else 0)
         self._ref = C.byref(self.args)
 
-    def _heads(self, t: torch.Tensor, heads: int):
-        assert t.shape[2:] == (heads, self.cfg.head_dim), f"{tuple(t.shape)}: {heads} heads of {self.cfg.head_dim} channels are wanted"
-        return C.byref(_rows(t, self.device))
+    def _heads(self, t: torch.Tensor, like: torch.Tensor, shape) -> bytes:
+        assert t.shape == shape and t.dtype is like.dtype, f"{tuple(t.shape)}, {t.dtype}: {shape}, {like.dtype} is wanted"
+        return _rows(t, self.device)
 
     def sssd_kv8_set_block_table(self, block_table: Optional[torch.Tensor]) -> None:
         """The table is read on the device when each later call executes; None: contiguous runs of pages."""
@@ -150,31 +150,31 @@ class Kv8Cache:
     def sssd_kv8_append(self, layer: int, k: torch.Tensor, v: torch.Tensor, lens: torch.Tensor, counts: Optional[torch.Tensor] = None,
                         first: int = 0, rope: Optional[Rope] = None, parents: Optional[torch.Tensor] = None,
                         q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> None:
-        B, n, nkv, _ = k.shape
-        assert v.shape == k.shape and v.dtype == k.dtype and nkv == self.cfg.n_kv_heads
-        turn = None
+        B, n = k.shape[:2]
+        shape = (B, n, self.n_kv_heads, self.head_dim)
+        turn = qq = to = None
         if rope is not None:
             assert rope.device == self.device
             turn = rope.ref
-        qq = to = None
         if q is not None:
-            assert q_out is not None and q.shape == q_out.shape and q.dtype == q_out.dtype and q.shape[:2] == (B, n)
-            qq, to = self._heads(q, self.cfg.n_q_heads), self._heads(q_out, self.cfg.n_q_heads)
-        _enqueue(_lib().sssd_kv8_append, self.device, self._ref, layer, first, B, n, self._heads(k, nkv), self._heads(v, nkv),
+            assert q_out is not None
+            of_q = (B, n, self.n_q_heads, self.head_dim)
+            qq, to = self._heads(q, q, of_q), self._heads(q_out, q, of_q)
+        _enqueue(_lib().sssd_kv8_append, self.device, self._ref, layer, first, B, n, self._heads(k, k, shape), self._heads(v, k, shape),
                  _ints(lens, (B,), self.device), _ints(counts, (B,), self.device), turn, _ints(parents, (B, n), self.device), qq, to)
 
     def sssd_kv8_read(self, layer: int, start: Optional[torch.Tensor], counts: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
                       first: int = 0) -> None:
-        B, n, nkv, _ = k.shape
-        assert v.shape == k.shape and v.dtype == k.dtype and nkv == self.cfg.n_kv_heads
+        B, n = k.shape[:2]
+        shape = (B, n, self.n_kv_heads, self.head_dim)
         _enqueue(_lib().sssd_kv8_read, self.device, self._ref, layer, first, B, n, _ints(start, (B,), self.device), _ints(counts, (B,), self.device),
-                 self._heads(k, nkv), self._heads(v, nkv))
+                 self._heads(k, k, shape), self._heads(v, k, shape))
 
     def sssd_kv8_attention(self, layer: int, q: torch.Tensor, lens: torch.Tensor, out: torch.Tensor, counts: Optional[torch.Tensor] = None,
                            parents: Optional[torch.Tensor] = None, window: int = 0, sinks: int = 0) -> None:
-        B, n, nq, _ = q.shape
-        assert out.shape == q.shape and out.dtype == q.dtype and nq == self.cfg.n_q_heads
-        _enqueue(_lib().sssd_kv8_attention, self.device, self._ref, layer, B, n, self._heads(q, nq), self._heads(out, nq),
+        B, n = q.shape[:2]
+        shape = (B, n, self.n_q_heads, self.head_dim)
+        _enqueue(_lib().sssd_kv8_attention, self.device, self._ref, layer, B, n, self._heads(q, q, shape), self._heads(out, q, shape),
                  _ints(lens, (B,), self.device), _ints(counts, (B,), self.device), _ints(parents, (B, n), self.device), window, sinks)
 
     def sssd_kv8_commit_tree(self, n: int, lens: torch.Tensor, accepted_len: torch.Tensor, accepted_path: Optional[torch.Tensor] = None) -> None:

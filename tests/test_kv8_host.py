@@ -28,7 +28,7 @@ def cache(**change):
 
 
 def rows(data=FAKE, type=0, b=6400, r=640, h=64):
-    return kv8.Rows(data, type, b, r, h)
+    return kv8.ROWS(data or 0, type, b, r, h)
 
 
 def rope(turns=FAKE, rotary=64, pairs=0):
@@ -75,7 +75,7 @@ def test_rope_refuses():
     ok = dict(x=rows(), out=rows(), B=1, n=1, heads=2, d=64, positions=FAKE, rope=rope())
     def call(**change):
         a = {**ok, **change}
-        ref = lambda s: C.byref(s) if s is not None else None  # noqa: E731
+        ref = lambda s: s if s is None or isinstance(s, bytes) else C.byref(s)  # noqa: E731
         return L.sssd_op_rope(ref(a["x"]), ref(a["out"]), a["B"], a["n"], a["heads"], a["d"], a["positions"], ref(a["rope"]), None)
     for bad in (dict(x=None), dict(out=None), dict(x=rows(data=None)), dict(out=rows(type=1)), dict(x=rows(type=2)), dict(x=rows(data=FAKE + 2)), dict(B=0), dict(n=0),
                 dict(heads=0), dict(heads=65536), dict(d=0), dict(d=8193), dict(d=2048, rope=rope(rotary=1026)), dict(positions=None), dict(rope=None), dict(rope=rope(turns=None)), dict(rope=rope(rotary=66)),
@@ -85,7 +85,7 @@ def test_rope_refuses():
 
 
 def calls():
-    ref = lambda s: C.byref(s) if s is not None else None  # noqa: E731
+    ref = lambda s: s if s is None or isinstance(s, bytes) else C.byref(s)  # noqa: E731
     def append(kv=None, layer=0, first=0, B=2, n=3, k=None, v=None, lens=FAKE, rope=None, parents=None, q=None, q_out=None, **_):
         return L.sssd_kv8_append(ref(kv), layer, first, B, n, ref(k), ref(v), lens, None, ref(rope), parents, ref(q), ref(q_out), None)
     def read(kv=None, layer=0, first=0, B=2, n=3, k=None, v=None, **_):
@@ -160,5 +160,4 @@ def test_the_binding_checks_tensors():
         kv8._ints(torch.zeros(2, dtype=torch.int64), (2,), -1)
     with pytest.raises(AssertionError):
         kv8._ints(torch.zeros(3, dtype=torch.int32), (2,), -1)
-    r = kv8._rows(x[:, :, 1:], -1)
-    assert (r.batch_stride, r.row_stride, r.head_stride, r.type) == (384, 128, 64, 0)
+    assert kv8._rows(x[:, :, 1:], -1) == kv8.ROWS(x.data_ptr() + 256, 0, 384, 128, 64) and len(kv8.ROWS(0, 0, 0, 0, 0)) == 40   # sssd_rows
