@@ -1,6 +1,6 @@
-"""sssd_op_rope against 64 bits.  Bound: the angle is rounded once, as a fraction of a half turn (pi * 2^-25), cos and sin are good to 2
-units of 2^-24 and multiplied by the magnitude (one more rounding), products and sum round three times: (|a| + |b|) * magnitude *
-8 * 2^-24 in all; bf16 results are rounded once more, by half a step."""
+"""sssd_op_rope against 64 bits.  Bound: cos and sin are off by 3 * 2^-25 at most (the rest of the angle after its quarter turns, rounded to 24 bits, its
+square and the ends of two polynomials) and multiplied by the magnitude (one more rounding), products and sum round three times: (|a| + |b|) * magnitude *
+8 * 2^-24 covers all; bf16 results are rounded once more, by half a step."""
 import pytest
 import torch
 
@@ -84,3 +84,19 @@ def test_numbers_that_are_none_stay_in_their_pair():
     bad = torch.zeros_like(y, dtype=torch.bool)
     bad[0, 0, [3, 35]] = bad[1, 0, [8, 40]] = True
     assert torch.equal(~y.isfinite(), bad)
+
+
+def test_angles():
+    """(1, 0) turned: cos and sin themselves, at angles of every quarter and next to their ends."""
+    rope = kv8.Rope(128, 10000.0, device=DEV)
+    rope.turns[0], rope.turns[1], rope.turns[2], rope.turns[3] = 0.125, 0.25, 1 / 3, 0.125 + 2.0 ** -40
+    x = torch.zeros(5000, 1, 128, device=DEV)
+    x[..., :64] = 1
+    positions = torch.arange(5000, device=DEV, dtype=torch.int32) - 2000
+    positions[-100:] = torch.randint(0, 1 << 20, (100,), device=DEV, dtype=torch.int32)
+    y = kv8.sssd_op_rope(x, positions, rope).double()
+    t = positions.double()[:, None] * rope.turns
+    angle = (t - t.round()) * 2 * torch.pi
+    err = torch.stack([y[:, 0, :64] - angle.cos(), y[:, 0, 64:] - angle.sin()]).abs()
+    assert err.max() <= 3 * 2.0 ** -25
+    assert torch.equal(y[positions % 8 == 0][:, 0, 0], torch.ones_like(y[positions % 8 == 0][:, 0, 0]))
