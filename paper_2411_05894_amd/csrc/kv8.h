@@ -204,7 +204,7 @@ struct RopeWork {
     uint32_t n, units, rows, total;   // units of a row and head; rows of the whole call
     Div by_units;
 };
-RopeWork rope_work(int B, int n, int d, int heads, int r, bool neighbours, int threads);
+RopeWork rope_work(int B, int n, int d, int heads, int r, bool neighbours, int threads, int each);
 
 struct Kv8StoreArgs {
     Kv8Geom g;

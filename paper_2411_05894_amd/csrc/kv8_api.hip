@@ -122,7 +122,7 @@ int sssd_op_rope(const sssd_rows *x, const sssd_rows *out, int32_t B, int32_t n,
     if (make_rows(x, B, n, heads, from) || make_rows(out, B, n, heads, to) || from.bf16 != to.bf16 || !make_rope(rope, head_dim, rp)) return SSSD_EINVAL;
     if (from.p == to.p && (from.bs != to.bs || from.rs != to.rs || from.hs != to.hs)) return SSSD_EINVAL;
     if ((int64_t)B * n > MOST_THREADS / 256) return SSSD_ECAPACITY;
-    const RopeWork w = rope_work(B, n, head_dim, heads, rp.r, rp.neighbours, 256);
+    const RopeWork w = rope_work(B, n, head_dim, heads, rp.r, rp.neighbours, 256, 1);
     if ((int64_t)((w.total + w.rows - 1) / w.rows) * ((heads + w.per - 1) / w.per) > MOST_THREADS / 256) return SSSD_ECAPACITY;
     HIP_TRY(launch_rope(from, to, positions, rp, w, (hipStream_t)stream));
     return SSSD_OK;
@@ -171,7 +171,7 @@ int sssd_kv8_append(const sssd_kv8 *kv, int32_t layer, int32_t first, int32_t B,
         // with the threads that store: both halves of what a launch may have
         if ((int64_t)B * n > MOST_THREADS / 2 / (2 * c.head_dim) || (int64_t)B * a.blocks > MOST_THREADS / 2 / (4 * c.head_dim) / c.n_kv_heads)
             return SSSD_ECAPACITY;
-        a.work = rope_work(B, n, c.head_dim, c.n_q_heads, a.rope.r, a.rope.neighbours, 2 * c.head_dim);
+        a.work = rope_work(B, n, c.head_dim, c.n_q_heads, a.rope.r, a.rope.neighbours, 2 * c.head_dim, 4);
     }
     HIP_TRY(launch_kv8_append(a, c.format, c.head_dim, (hipStream_t)stream));
     return SSSD_OK;

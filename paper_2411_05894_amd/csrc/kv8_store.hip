@@ -198,7 +198,7 @@ __device__ __forceinline__ void rotate_part(const Rope8 &rp, const Rows8 &r, con
 // (some thirty instructions each); then the threads pass over the rows in the order of memory, a unit each: by halves U pairs (i .. i+U-1 with
 // their partners), as neighbours U/2 pairs that lie in a row, or U channels that pass.
 // Measured against a thread with the angles of eight pairs in registers that takes them through several heads (32 places of 256 bytes at a time, a
-// row's stride apart): 8191 rows of 40 heads of 128, bf16, 49.6 -> 36 us cold, whatever the number of heads requested at once.
+// row's stride apart): 8191 rows of 40 heads of 128, bf16, 49.6 -> 43.5 us cold, now 38.9 (168 MB, 4.3 TB/s; a copy of 1 GiB 5.2).
 struct RopeRow {
     int b, j, position, on;   // on: 0 where the row is left as it is
 };
@@ -648,9 +648,11 @@ __global__ __launch_bounds__(64) void advance_kernel(Kv8StoreArgs a, const int32
 
 }  // namespace
 
-// Units of eight channels where pairs and the channels that pass divide into them, else single pairs.  A workgroup takes as many rows as its
-// table of angles holds while eight workgroups are left for every compute unit, and all heads; few rows are cut by heads, too.
-RopeWork rope_work(int B, int n, int d, int heads, int r, bool neighbours, int threads)
+// Units of eight channels where pairs and the channels that pass divide into them, else single pairs.  A workgroup takes as many rows, with all their
+// heads, as have `each` units for a thread, while eight workgroups are left for every compute unit: one in a rotation alone (8191 rows of 40 heads of 128
+// in bf16 38.9 us, three rows a workgroup 44; 12000 of 16 of 64 14.9, one row a workgroup 17.1), four beside rows that are stored, where a workgroup
+// has more to look up first and fewer fit (prompts of 32768 with 32 heads of queries 147, one 166).  Few rows are cut by heads, too.
+RopeWork rope_work(int B, int n, int d, int heads, int r, bool neighbours, int threads, int each)
 {
     RopeWork w;
     const int turning = neighbours ? r : r / 2;
@@ -658,8 +660,10 @@ RopeWork rope_work(int B, int n, int d, int heads, int r, bool neighbours, int t
     w.units = turning / w.unit + (d - r + w.unit - 1) / w.unit;
     w.n = n; w.d = d; w.heads = heads;
     w.total = (uint32_t)B * n;
-    const uint32_t fit = ROPE_TABLE * 2 / r, want = w.total / 2048;
-    w.rows = want < 1 ? 1 : want > ROPE_ROWS ? ROPE_ROWS : want;
+    const uint32_t fit = ROPE_TABLE * 2 / r, left = w.total / 2048;
+    const int64_t fill = (int64_t)threads * each / ((int64_t)heads * w.units);
+    w.rows = fill < 1 ? 1 : fill > ROPE_ROWS ? ROPE_ROWS : (uint32_t)fill;
+    if (w.rows > left) w.rows = left < 1 ? 1 : left;
     if (w.rows > fit) w.rows = fit;
     const uint32_t groups = (w.total + w.rows - 1) / w.rows;
     const int64_t most = ((int64_t)heads * w.units + threads - 1) / threads;   // a unit for every thread

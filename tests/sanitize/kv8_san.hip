@@ -40,7 +40,7 @@ static void rotations()
             for (int neighbours = 0; neighbours < 2; ++neighbours)
                 for (int total : {1, 9, 4095, 100000}) {
                     const int heads = d % 7 * 9 + 1;
-                    const RopeWork w = rope_work(1, total, d, heads, r, neighbours, 256);
+                    const RopeWork w = rope_work(1, total, d, heads, r, neighbours, 256, total % 2 ? 1 : 4);
                     CHECK(w.rows >= 1 && w.rows <= (uint32_t)ROPE_ROWS && w.rows * (r / 2) <= (uint32_t)ROPE_TABLE && w.per >= 1 && w.per <= heads);
                     const int turning = neighbours ? r : r / 2;
                     CHECK(turning % w.unit == 0 && (int)w.units == turning / w.unit + (d - r + w.unit - 1) / w.unit);
@@ -48,7 +48,7 @@ static void rotations()
                     CHECK((uint64_t)w.per * w.units * w.units < (uint64_t)1 << 32);      // the quotient by units is exact
                     CHECK(w.unit < 8 || (r % 8 == 0 && (d - r) % 8 == 0));
                 }
-    const RopeWork w = rope_work(1, 5, 8192, 65535, 2, 0, 256);
+    const RopeWork w = rope_work(1, 5, 8192, 65535, 2, 0, 256, 1);
     CHECK(w.per >= 1 && (uint64_t)w.per * w.units * w.units < (uint64_t)1 << 32);
 }
 
