@@ -245,6 +245,6 @@ struct Kv8AttnArgs {
     Hand hand;               // words for segments merged inside the launch, or none
     int32_t *status;
 };
-Kv8Plan kv8_plan(int B, int n, int gq, int nkv);
+Kv8Plan kv8_plan(int B, int n, int gq, int nkv, int blocks, bool f32);   // blocks: of a sequence at most
 size_t kv8_attention_ws(int d);   // bytes behind the workspace that any call's partial results take
 hipError_t launch_kv8_attention(Kv8AttnArgs a, int fmt, int d, void *ws, hipStream_t s);

@@ -1,6 +1,7 @@
 // Attention of a step's new rows over a KV cache in 8 bits.
 #include "kv8.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace {
@@ -107,8 +108,9 @@ __device__ __forceinline__ Span span_of(int len, int count, int window, int sink
 struct Cut {
     int each, n;   // blocks per segment (the last may have fewer), segments
 };
-// By the sequence's own blocks and the call's plan alone: what the others hold changes no bit.  At least four blocks a segment, one for each wave;
-// up to eight are one segment.
+// By the sequence's own blocks and the call's plan alone: what the others hold changes no bit.  At least four blocks a segment, one for each wave (2048
+// positions with eight at least 12.5 us, so 11.5); up to eight are one segment, which need not be joined.  Long segments are whole rounds of four waves
+// (4 x 32768 57.4 us, else 59.2; 16 sequences of 4000 with 32 rows 82.7, else 86.8).
 __device__ __forceinline__ Cut cut_of(int blocks, int share)
 {
     auto up = [](int x, int y) { return (int)(((unsigned)x + (unsigned)y - 1u) / (unsigned)y); };
@@ -675,13 +677,26 @@ template <int HD> hipError_t launch_hd(const Kv8AttnArgs &a, int fmt, int rt, hi
 
 }  // namespace
 
-Kv8Plan kv8_plan(int B, int n, int gq, int nkv)
+// How a call is cut, by what the host knows of it.  A pass over the cache takes one to three row tiles of queries; more tiles read the cache less often, but
+// their workgroups have more to set up, to add over their waves and to join.
+//  - Short sequences (as long as they can be: `blocks`): a tile a pass, while its workgroups fit on the chip together.  us, one tile / as few passes as
+//    can be, of 9 rows of 8B: float32 B = 1, 300 8.2 / 11.4, 2048 9.2 / 11.5, 8192 13.9 / 16.2, 16384 18.8 / 19.3, 32768 29.0 / 26.6; B = 8, 2048
+//    19.5 / 20.0, 4096 30.6 / 26.9; bf16 B = 1, 8192 13.5 / 14.8, 16384 18.2 / 17.2; 70B float32 B = 5, 300 7.4 / 13.5; sixteen
+//    tiles, B = 2, n = 32, 4000 25.9 / 20.9; more workgroups than fit, 8B B = 16, n = 32, 500 18.5 / 13.8.
+//  - Else by rounds of 256 workgroups and what a block costs a pass of one, two and three tiles.  us, by that / fewest passes / one tile: 70B float32
+//    B = 7, n = 13, 700..1500 21.4 / 26.8 / 21.0; B = 2, n = 32, 4000 bf16 20.9 / 24.9 / 25.8; 8B B = 16, n = 32, 500 13.8 / 16.9 / 18.5;
+//    B = 4, n = 9, 32768 57.4 / 57.7 / 76.8.
+//  - Segments of a sequence so that 256 workgroups have work; twice that where 256 in whole segments leave a quarter of the chip idle (8B B = 12, 3000
+//    24.6, without 27.8; for all calls: B = 32, 2500 41, now 36).
+Kv8Plan kv8_plan(int B, int n, int gq, int nkv, int blocks, bool f32)
 {
     const int tiles = (n * gq + 15) / 16;
     const int64_t heads = (int64_t)B * nkv;
     Kv8Plan p;
+    const bool brief = heads * blocks <= (f32 ? 3500 : 2300) && heads * blocks * tiles <= (f32 ? 20000 : 13000) && heads * tiles <= 512;
+    if (brief) p.passes = tiles;
     double best = 0;
-    for (int rt = KV8_MAX_TILES; rt >= 1; --rt) {
+    for (int rt = KV8_MAX_TILES; rt >= 1 && !brief; --rt) {
         const int passes = (tiles + rt - 1) / rt;
         const int64_t units = heads * passes;
         static const double block[4] = {0, 0.75, 1.0, 1.4};
@@ -704,7 +719,9 @@ size_t kv8_attention_ws(int d) { return HAND_WORDS + (size_t)KV8_GROUPS * KV8_MA
 hipError_t launch_kv8_attention(Kv8AttnArgs a, int fmt, int d, void *ws, hipStream_t s)
 {
     const int tiles = (a.n * a.gq + 15) / 16;
-    a.plan = kv8_plan(a.B, a.n, a.gq, a.g.nkv);
+    int64_t blocks = a.g.blocks_per_seq;   // that a sequence can have
+    if (a.window > 0) blocks = std::min(blocks, ((int64_t)a.window + a.n + 30) / 32 + 1 + ((int64_t)a.sinks + 31) / 32);
+    a.plan = kv8_plan(a.B, a.n, a.gq, a.g.nkv, (int)blocks, !a.q.bf16);
     const int rt = (tiles + a.plan.passes - 1) / a.plan.passes;
     a.rows_pad = tiles * 16;
     a.hand.words = a.plan.share > 1 && a.plan.in_die ? (uint64_t *)ws : nullptr;

@@ -22,15 +22,17 @@ static void attention_plans()
     for (int nkv = 1; nkv <= 16; ++nkv)
         for (int gq : {1, 2, 3, 4, 7, 8, 16, 64})
             for (int B = 1; B <= 300; B += B < 40 ? 1 : 13)
-                for (int n = 1; n <= 32; ++n) {
-                    const Kv8Plan p = kv8_plan(B, n, gq, nkv);
-                    const int tiles = (n * gq + 15) / 16, rt = (tiles + p.passes - 1) / p.passes;
-                    CHECK(p.passes >= 1 && rt >= 1 && rt <= KV8_MAX_TILES && p.share >= 1 && p.share <= 64);
-                    // partial results lie within the workspace
-                    if (p.share > 1) CHECK((size_t)B * nkv * p.share * tiles * 16 * (128 * 4 + 8) + HAND_WORDS <= ws);
-                    // groups have a word each, and no workgroup of a group waits for more than what is resident
-                    if (p.share > 1 && p.in_die) CHECK(B * nkv * p.passes <= HAND_GROUPS && B * nkv % 8 == 0 && p.share <= 32 && B * nkv * p.passes * p.share <= 512);
-                }
+                for (int n = 1; n <= 32; ++n)
+                    for (int blocks : {1, 40, 200, 1000, 40000})
+                        for (bool f32 : {false, true}) {
+                            const Kv8Plan p = kv8_plan(B, n, gq, nkv, blocks, f32);
+                            const int tiles = (n * gq + 15) / 16, rt = (tiles + p.passes - 1) / p.passes;
+                            CHECK(p.passes >= 1 && rt >= 1 && rt <= KV8_MAX_TILES && p.share >= 1 && p.share <= 64);
+                            // partial results lie within the workspace
+                            if (p.share > 1) CHECK((size_t)B * nkv * p.share * tiles * 16 * (128 * 4 + 8) + HAND_WORDS <= ws);
+                            // groups have a word each, and no workgroup of a group waits for more than what is resident
+                            if (p.share > 1 && p.in_die) CHECK(B * nkv * p.passes <= HAND_GROUPS && B * nkv % 8 == 0 && p.share <= 32 && B * nkv * p.passes * p.share <= 512);
+                        }
 }
 
 static void rotations()

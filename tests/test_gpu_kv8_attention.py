@@ -29,10 +29,12 @@ def random_parents(n, seed):
 class Batch:
     """A filled cache and what it holds."""
 
-    def __init__(self, fmt, nq, nkv, d, lens, n, counts=None, paged=False, seed=1, spread=1.0, extra=0, cut=None):
+    def __init__(self, fmt, nq, nkv, d, lens, n, counts=None, paged=False, seed=1, spread=1.0, extra=0, cut=None, long=False):
         g = torch.Generator(device=DEV).manual_seed(seed)
         self.B, self.n, self.lens, self.counts = len(lens), n, lens, counts or [n] * len(lens)
         max_seq = max(lens) + n + extra
+        if long:                       # room for sequences so long that the queries go through the cache several tiles at a time
+            max_seq += 32 * (3500 // (self.B * nkv) + 1)
         self.cache = kv8.Kv8Cache(2, nq, nkv, d, self.B, max_seq, fmt, device=DEV)
         if paged:
             t = torch.randperm(self.cache.n_pages, generator=torch.Generator().manual_seed(seed)).to(torch.int32)
@@ -86,19 +88,21 @@ SHAPES = [(4, 2, 64), (32, 8, 128), (8, 1, 64), (6, 6, 128), (64, 8, 128), (64, 
 @pytest.mark.parametrize("fmt", ["e4m3", "int8"])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("nq,nkv,d", SHAPES)
-def test_lengths(fmt, dtype, nq, nkv, d):
+@pytest.mark.parametrize("long", [False, True])
+def test_lengths(fmt, dtype, nq, nkv, d, long):
     """From an empty context to several segments, ends inside and at blocks, ragged and padded."""
     for lens, n, counts, paged in (([0], 1, None, False), ([0, 1, 31, 32, 33], 2, [2, 1, 2, 0, 2], True), ([255, 256, 257, 7], 5, None, False),
                                    ([1000, 3, 4100], 9, [9, 7, 9], True), ([2047], 9, None, False), ([70, 600], 32, [32, 17], False)):
-        print(f"kv8 attention {fmt} {dtype} {nq}/{nkv}x{d} {lens} {n}", flush=True)
-        Batch(fmt, nq, nkv, d, lens, n, counts, paged).check(dtype)
+        print(f"kv8 attention {fmt} {dtype} {nq}/{nkv}x{d} {lens} {n} {long}", flush=True)
+        Batch(fmt, nq, nkv, d, lens, n, counts, paged, long=long).check(dtype)
 
 
 @pytest.mark.parametrize("nq,nkv,d", [(4, 2, 64), (32, 8, 128)])
 @pytest.mark.parametrize("fmt", ["e4m3", "int8"])
-def test_every_number_of_rows(fmt, nq, nkv, d):
+@pytest.mark.parametrize("long", [False, True])
+def test_every_number_of_rows(fmt, nq, nkv, d, long):
     """1 .. 32 new rows: row tiles and passes of every size, chains and trees."""
-    batch = Batch(fmt, nq, nkv, d, [37, 300], 32, seed=2)
+    batch = Batch(fmt, nq, nkv, d, [37, 300], 32, seed=2, long=long)
     full, held = batch.q, batch.held
     for n in range(1, 33):
         batch.n, batch.counts, batch.q = n, [n] * 2, full[:, :n].contiguous()
@@ -115,6 +119,13 @@ def test_windows(window, sinks, tree):
         batch = Batch(fmt, nq, nkv, d, lens, n, [13, 13, 12, 13, 5], paged=True, seed=3)
         print(f"kv8 window {window} {sinks} {fmt} {dtype}", flush=True)
         batch.check(dtype, [random_parents(n, b) for b in range(5)] if tree else None, window, sinks)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_wide_windows(dtype):
+    """Windows of many blocks over several sequences, whose queries go through the cache several tiles at a time."""
+    for nq, n, window, sinks in ((32, 9, 6000, 4), (64, 13, 5999, 100)):
+        Batch("int8", nq, 8, 128, [9000, 6003, 7777], n, [n, n, 3], seed=18).check(dtype, [random_parents(n, b) for b in range(3)], window, sinks)
 
 
 def test_rows_outside_the_window_are_not_read():
@@ -252,8 +263,9 @@ def test_strides_and_neighbours():
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
-def test_the_other_sequences_change_no_bit(dtype):
-    a = Batch("e4m3", 32, 8, 128, [1500, 90, 3000], 5, seed=11)
+@pytest.mark.parametrize("long", [False, True])
+def test_the_other_sequences_change_no_bit(dtype, long):
+    a = Batch("e4m3", 32, 8, 128, [1500, 90, 3000], 5, seed=11, long=long)
     first = a.check(dtype)
     k = torch.randn(1, 60, 8, 128, device=DEV)
     for b in (1, 2):
@@ -332,12 +344,13 @@ def test_pages_behind_four_gib():
     (32, 8, 128, 4, 9), (32, 8, 128, 2, 32), (64, 8, 128, 2, 9), (64, 8, 128, 7, 13), (64, 8, 128, 1, 1), (32, 8, 128, 33, 5),   # one pass and several, four and eight waves
     (64, 8, 64, 3, 9), (16, 2, 64, 1, 7), (16, 2, 128, 3, 7), (24, 8, 128, 5, 5), (48, 8, 64, 20, 6)])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
-def test_plans(nq, nkv, d, B, n, dtype):
+@pytest.mark.parametrize("long", [False, True])
+def test_plans(nq, nkv, d, B, n, dtype, long):
     """Passes, row tiles, waves and segments of every kind, segments joined inside the launch and by a second one; those joined without waiting give
     the same bits."""
     lens = [(1700 * (b + 1)) % 2300 + (b == 0) * 1500 for b in range(B)]
-    batch = Batch("int8" if n % 2 else "e4m3", nq, nkv, d, lens, n, paged=True, seed=n)
-    print(f"kv8 plan {nq}/{nkv}x{d} B {B} n {n} {dtype}", flush=True)
+    batch = Batch("int8" if n % 2 else "e4m3", nq, nkv, d, lens, n, paged=True, seed=n, long=long)
+    print(f"kv8 plan {nq}/{nkv}x{d} B {B} n {n} {dtype} {long}", flush=True)
     want = batch.check(dtype)
     batch.cache.args.flags = 2       # SSSD_NO_WAIT
     for _ in range(3):
