@@ -1,4 +1,25 @@
-// Attention of a step's new rows over a KV cache in 8 bits.
+// Attention of a step's new rows over a KV cache in 8 bits: softmax(q . k / sqrt(d)) over what a row sees, times v.
+//
+// Mathematics.  One pass over the cache with, per row, a reference m of the exponents, l = sum of p and o = sum of p v for p = 2^(score * log2(e) - m);
+// when m moves, l and o are multiplied by 2^(old - new).  m is not the running maximum but follows it lazily (REF_BELOW, REF_MOST), so that hardly any block
+// pays for it.  Sums over waves and segments are brought to one m at the end.
+//
+// Products are float16 matrix instructions (16 x 16 x 32) with 32-bit sums: an 8-bit code is a float16 exactly, in either format, at one conversion per two
+// codes.  The other operand is rounded to 11 bits or, for float32 queries, split into hi + lo with 22: queries after their row's largest has been
+// brought below 2^15 by a power of two, probabilities as they are.  K's scales join the factor of the exponent; V's go into the conversion of its codes, relative
+// to the largest one so far.
+//
+// Layout and split.  A score product gives a lane four positions of one query row, twice a block: just what the second product takes from it as an operand (V is
+// stored for that), so probabilities stay in registers.  Queries lie in LDS as operands.  A workgroup is four or eight waves on the
+// blocks of one (sequence, kv head) in turn; a wave requests a block's K and V as soon as it has used those before.  Sequences are cut into segments by the
+// plan (kv8_plan, cut_of), joined inside the launch where one die can hold them.
+//
+// What bounds it: from some thousands of positions a chip's worth of workgroups on the stream of the cache.  8B, B = 4, n = 9, 32768 bf16 269 MB in 54.6 us,
+// 4.9 TB/s, of which some 45 stream at 6 TB/s, as fast as the blocks are read by a kernel that does nothing else (46 us), around them 5 us until K is there
+// and the queries are operands and 3 for the sums of waves and segments; float32 queries 64 (twice the products).  B = 32, n = 5, 1024..4096 173 MB in
+// 41 us: one workgroup per head and sequence, so the longest decides; all of 2500 35.6.  Short ones on the chain of round trips: arguments, lens, page,
+// block, sums of waves, partial results, their arrival: B = 1, n = 9, 2048 8.7 us (as a launch 9.5: request of K at 2.2, loop from 3.1 to 5.3,
+// joined at 9).
 #include "kv8.h"
 
 #include <algorithm>

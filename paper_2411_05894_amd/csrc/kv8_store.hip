@@ -1,6 +1,12 @@
 // Rotary positions, and writing, reading back and committing rows of a KV cache in 8 bits.
 //
-// All of it is bound by memory for prompts and by a launch and two or three dependent round trips for a step's few rows.
+// All of it is bound by memory for prompts and by a launch and two or three dependent round trips for a step's few rows.  Captured, inputs in memory: a
+// rotation of 9 rows 3.3 us (the launch alone 3), of 8191 rows of 40 heads of 128 in bf16 38.9 (168 MB, 4.3 TB/s); an append of 9 rows in 8 heads 4.95, with
+// 32 heads of queries the same, of 100001 rows 121 (614 MB, 5.1 TB/s; a copy of 1 GiB 5.2), with the queries 433 (5.2 TB/s); reading 9 rows back 3.7, 32768 45
+// (4.5 TB/s); committing trees of 9 rows of 16 sequences in 32 layers 45.
+//
+// A block's scale needs all of its live rows, so a workgroup takes whole blocks: 32 rows of a head, sixteen values a thread, in the order of K's records.
+// Rows that were there before are taken out of their codes and go through the new scale like new ones.
 #include "kv8.h"
 
 namespace {
