@@ -158,8 +158,8 @@ int sssd_kv8_attention(const sssd_kv8 *kv, int32_t layer, int32_t B, int32_t n, 
  * Commit a step of n = k+1 <= 32 rows, all layers at once, as sssd_kv_commit_tree does: the rows of the accepted nodes
  * accepted_path[b][1..a], a = accepted_len[b], move to lens[b]+1 .. lens[b]+a; then lens[b] += a + 1 (device int32 [B],
  * in-out).  accepted_path [B][n], or NULL for chains: only lens advances.  A path that is not strictly increasing within
- * 1..n-1, a outside 0..n-1, lens[b] that does not fit n rows, or a page outside the pool leaves that sequence untouched and
- * raises the status.
+ * 1..n-1 or whose last row lies at or beyond max_seq, a outside 0..n-1, lens[b] < 0, or a page outside the pool for a block of
+ * the path leaves that sequence untouched and raises the status.
  */
 int sssd_kv8_commit_tree(const sssd_kv8 *kv, int32_t B, int32_t n, int32_t *lens, const int32_t *accepted_len,
                          const int32_t *accepted_path, void *stream);

@@ -564,17 +564,19 @@ __device__ __forceinline__ bool commit_ok(const Kv8StoreArgs &g, const int32_t *
     len = g.lens[b];
     acc = accepted[b];
     node = lane;
-    if (len < 0 || (int64_t)len + g.n > g.g.max_seq || acc < 0 || acc >= g.n) return false;
-    bool ok = true;
+    if (len < 0 || acc < 0 || acc >= g.n) return false;
     if (path) {
         if (lane > 0 && lane <= acc) node = path[(size_t)b * g.n + lane];
         const int before = __shfl_up(node, 1);
-        ok = lane == 0 || lane > acc || (node > before && node < g.n);
+        if (!__all(lane == 0 || lane > acc || (node > before && node < g.n))) return false;
     }
+    const int farthest = __shfl(node, acc);   // the path's last row
+    if ((int64_t)len + farthest >= g.g.max_seq) return false;
     const int blk = (len >> 5) + lane;
-    if (blk <= (len + g.n - 1) >> 5) {
+    bool ok = true;
+    if (blk <= (len + farthest) >> 5) {
         const int page = kv8_entry(g.g, b, blk);
-        ok = ok && page >= 0 && page < g.g.n_pages;
+        ok = page >= 0 && page < g.g.n_pages;
     }
     return __all(ok);
 }

@@ -310,7 +310,7 @@ PATHS = [list(range(1, 32)), [2, 3, 4, 5, 6, 7, 8, 9, 10, 11], [1, 2, 3, 30, 31]
 def test_commit_moves_the_path(fmt, d, paged):
     g = torch.Generator(device=DEV).manual_seed(13)
     n, max_seq, L, nkv = 32, 160, 2, 2
-    bad = [([2, 1], 2, 5), ([3, 3], 2, 5), ([1, 32], 2, 5), ([1, 2], 32, 5), ([1, 2], -1, 5), ([2, 4], 2, 129), ([2, 4], 2, -3)]
+    bad = [([2, 1], 2, 5), ([3, 3], 2, 5), ([1, 32], 2, 5), ([1, 2], 32, 5), ([1, 2], -1, 5), ([2, 4], 2, 156), ([2, 4], 2, -3)]
     paths, lens = PATHS + [p for p, _, _ in bad], [0, 1, 31, 20, 64, 100, 33] + [l for _, _, l in bad]
     B = len(paths)
     cache = kv8.Kv8Cache(L, 4, nkv, d, B, max_seq, fmt, device=DEV)
@@ -404,3 +404,27 @@ def test_nothing_to_do():
     lens = ints([3, 7])
     cache.sssd_kv8_commit_tree(5, lens, ints([0, 0]), ints([[0, -1, -1, -1, -1]] * 2))
     assert lens.tolist() == [4, 8] and torch.equal(before, cache.cache) and cache.sssd_kv8_sync() == SSSD_OK
+
+
+@pytest.mark.parametrize("lens", [[95, 90], [0, 63]])
+def test_the_last_step_of_a_full_cache(lens):
+    """Fewer rows than the call's, up to the last position: what is accepted fits, whatever n would not."""
+    cache = kv8.Kv8Cache(1, 2, 2, 64, 2, 100, "int8", device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(21)
+    x, new = (torch.randn(2, r, 2, 64, generator=g, device=DEV) for r in (100, 9))
+    cache.sssd_kv8_append(0, x, x, ints([0, 0]), counts=ints(lens))
+    counts, path = [5, 9], [[0, 2, 4] + [-1] * 6, [0, 1, 3, 5, 8] + [-1] * 4]
+    cache.sssd_kv8_append(0, new, new, ints(lens), counts=ints(counts))
+    now = ints(lens)
+    cache.sssd_kv8_commit_tree(9, now, ints([2, 4]), ints(path))
+    assert cache.sssd_kv8_sync() == SSSD_OK and now.tolist() == [lens[0] + 3, lens[1] + 5]
+    got = read_all(cache, 0, now.tolist(), 100)
+    for b in range(2):
+        c = Cache(2, 64, "int8", DEV)
+        c.append(0, x[b, :lens[b]])
+        c.append(lens[b], new[b, :counts[b]])
+        c.commit(lens[b], path[b][1:3 + 2 * b])
+        assert torch.equal(got[0][b, :now[b]].double(), c.x) and torch.equal(got[1][b, :now[b]].double(), c.x)
+    now = ints([95, 96])
+    cache.sssd_kv8_commit_tree(9, now, ints([2, 1]), ints([[0, 2, 5] + [-1] * 6, [0, 3] + [-1] * 7]))
+    assert cache.sssd_kv8_sync() == SSSD_ENOSPACE and now.tolist() == [95, 98]
