@@ -702,8 +702,9 @@ template <int HD> hipError_t launch_hd(const Kv8AttnArgs &a, int fmt, int rt, hi
 // their workgroups have more to set up, to add over their waves and to join.
 //  - Short sequences (as long as they can be: `blocks`): a tile a pass, while its workgroups fit on the chip together.  us, one tile / as few passes as
 //    can be, of 9 rows of 8B: float32 B = 1, 300 8.2 / 11.4, 2048 9.2 / 11.5, 8192 13.9 / 16.2, 16384 18.8 / 19.3, 32768 29.0 / 26.6; B = 8, 2048
-//    19.5 / 20.0, 4096 30.6 / 26.9; bf16 B = 1, 8192 13.5 / 14.8, 16384 18.2 / 17.2; 70B float32 B = 5, 300 7.4 / 13.5; sixteen
-//    tiles, B = 2, n = 32, 4000 25.9 / 20.9; more workgroups than fit, 8B B = 16, n = 32, 500 18.5 / 13.8.
+//    19.5 / 20.0, 4096 30.6 / 26.9; bf16 B = 1, 8192 13.5 / 14.8, 16384 18.2 / 17.2; two
+//    tiles, n = 5, bf16 B = 5, 1000 10.1 / 10.4, 2048 13.3 / 12.1; 70B float32 B = 5, 300 7.4 / 13.5; B = 6, 1500 15.5 / 22.3; sixteen tiles, n = 32,
+//    B = 3, 1000 16.6 / 21.6, B = 1, 4000 21.0 / 17.6, bf16 B = 2, 4000 25.9 / 20.9; more workgroups than fit, 8B B = 16, n = 32, 500 18.5 / 13.8.
 //  - Else by rounds of 256 workgroups and what a block costs a pass of one, two and three tiles.  us, by that / fewest passes / one tile: 70B float32
 //    B = 7, n = 13, 700..1500 21.4 / 26.8 / 21.0; B = 2, n = 32, 4000 bf16 20.9 / 24.9 / 25.8; 8B B = 16, n = 32, 500 13.8 / 16.9 / 18.5;
 //    B = 4, n = 9, 32768 57.4 / 57.7 / 76.8.
@@ -714,7 +715,7 @@ Kv8Plan kv8_plan(int B, int n, int gq, int nkv, int blocks, bool f32)
     const int tiles = (n * gq + 15) / 16;
     const int64_t heads = (int64_t)B * nkv;
     Kv8Plan p;
-    const bool brief = heads * blocks <= (f32 ? 3500 : 2300) && heads * blocks * tiles <= (f32 ? 20000 : 13000) && heads * tiles <= 512;
+    const bool brief = heads * blocks <= (f32 ? 3500 : tiles > 2 ? 2750 : 2000) && heads * blocks * tiles <= 15000 && heads * tiles <= 512;
     if (brief) p.passes = tiles;
     double best = 0;
     for (int rt = KV8_MAX_TILES; rt >= 1 && !brief; --rt) {
