@@ -18,8 +18,8 @@
 // 4.9 TB/s, of which some 45 stream at 6 TB/s, as fast as the blocks are read by a kernel that does nothing else (46 us), around them 5 us until K is there
 // and the queries are operands and 3 for the sums of waves and segments; float32 queries 64 (twice the products).  B = 32, n = 5, 1024..4096 173 MB in
 // 41 us: one workgroup per head and sequence, so the longest decides; all of 2500 35.6.  Short ones on the chain of round trips: arguments, lens, page,
-// block, sums of waves, partial results, their arrival: B = 1, n = 9, 2048 8.7 us (as a launch 9.5: request of K at 2.2, loop from 3.1 to 5.3,
-// joined at 9).
+// block, sums of waves, partial results, their arrival: B = 1, n = 9, 2048 8.8 us, of which K is requested after 2.2 and the rows are joined in the
+// last 2.
 #include "kv8.h"
 
 #include <algorithm>
