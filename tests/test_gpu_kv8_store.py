@@ -428,3 +428,39 @@ def test_the_last_step_of_a_full_cache(lens):
     now = ints([95, 96])
     cache.sssd_kv8_commit_tree(9, now, ints([2, 1]), ints([[0, 2, 5] + [-1] * 6, [0, 3] + [-1] * 7]))
     assert cache.sssd_kv8_sync() == SSSD_ENOSPACE and now.tolist() == [95, 98]
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("nkv,d,dtype", [(8, 128, torch.bfloat16), (5, 64, torch.float32), (7, 128, torch.float32), (16, 64, torch.bfloat16)])
+@pytest.mark.parametrize("rotary,interleaved", [(0, False), (None, False), (None, True), (32, False), (10, False), (22, True)])
+def test_several_heads_to_a_workgroup(fmt, nkv, d, dtype, rotary, interleaved):
+    """A batch so large that workgroups take several heads leaves the same bytes as its sequences one by one: blocks with older rows, ragged counts,
+    rows that are no numbers, addresses that are and are not multiples of 16 bytes; and reads back the same."""
+    g = torch.Generator(device=DEV).manual_seed(31)
+    B, n, max_seq = 48, 150, 256
+    lens = [(37 * b) % 100 for b in range(B)]
+    counts = [n - (11 * b) % 60 if b % 7 else 0 for b in range(B)]
+    old = rows(g, B, 100, nkv, d)
+    flat = torch.randn(B * n * 3 * nkv * d + 1, generator=g, device=DEV).to(dtype)
+    flat[::50021] = float("nan")
+    rope = kv8.Rope(rotary or d, 10000.0, interleaved=interleaved, device=DEV) if rotary != 0 else None
+    for shift in (0, 1):
+        qkv = flat[shift:shift + B * n * 3 * nkv * d].view(B, n, 3 * nkv, d)
+        q, k, v = qkv.split(nkv, 2)
+        caches = [kv8.Kv8Cache(1, nkv, nkv, d, B, max_seq, fmt, device=DEV) for _ in range(2)]
+        outs = [torch.full((B, n, nkv, d), 3.5, dtype=dtype, device=DEV) for _ in range(2)]
+        for cache, out, at in zip(caches, outs, ([(0, B)], [(b, b + 1) for b in range(B)])):
+            cache.sssd_kv8_set_block_table(table(cache))
+            for a, z in at:
+                turn = dict(rope=rope, q=q[a:z], q_out=out[a:z]) if rope else {}
+                cache.sssd_kv8_append(0, old[a:z], old[a:z], ints([0] * (z - a)), counts=ints(lens[a:z]), first=a)
+                cache.sssd_kv8_append(0, k[a:z], v[a:z], ints(lens[a:z]), counts=ints(counts[a:z]), first=a, **turn)
+            assert cache.sssd_kv8_sync() == SSSD_EINVAL      # the rows that are no numbers
+        assert torch.equal(caches[0].cache, caches[1].cache)
+        assert torch.equal(outs[0].nan_to_num(7.0), outs[1].nan_to_num(7.0))
+        got = []
+        for cache, at in zip(caches, ([(0, B)], [(b, b + 1) for b in range(B)])):
+            got.append([torch.full((B, n, nkv, d), 7.25, dtype=torch.bfloat16, device=DEV) for _ in range(2)])
+            for a, z in at:
+                cache.sssd_kv8_read(0, ints(lens[a:z]), ints(counts[a:z]), *(x[a:z] for x in got[-1]), first=a)
+        assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
