@@ -7,7 +7,7 @@
 // Products are float16 matrix instructions (16 x 16 x 32) with 32-bit sums: an 8-bit code is a float16 exactly, in either format, at one conversion per two
 // codes.  The other operand is rounded to 11 bits or, for float32 queries, split into hi + lo with 22: queries after their row's largest has been
 // brought below 2^15 by a power of two, probabilities as they are.  K's scales join the factor of the exponent; V's go into the conversion of its codes, relative
-// to the largest one so far.
+// to the largest one so far, where float16 holds that (V_ABOVE, V_BELOW).
 //
 // Layout and split.  A score product gives a lane four positions of one query row, twice a block: just what the second product takes from it as an operand (V is
 // stored for that), so probabilities stay in registers.  Queries lie in LDS as operands.  A workgroup is four or eight waves on the
@@ -36,6 +36,13 @@ constexpr float REF_BELOW = 7.f, REF_MOST = 15.f;
 // From scores of this size on they are rounded before the reference is subtracted: unrounded products of the row's largest could lie above a
 // reference made of a rounded one by more than float16 holds.
 constexpr float HUGE_SCORE = 0x1p20f;
+// V's codes are converted in units of a scale that follows the largest, V_ABOVE octaves late.  A block is taken as it comes while its own scale is at most
+// that far above the unit and V_BELOW below it, where float16 holds code * ratio exactly (it would down to 2^-15 for 8-bit floats and 2^-24 for integers), and
+// at most both together above the smallest one met: what its probabilities lose (2^-32 of the row's largest) is then worth no more than 2^-20 of that one's
+// values.  Other blocks are far: multiplied as they are, with probabilities relative to the block's own maximum (or REF_FAR below the row's reference, where
+// that is higher), and added in 32 bits.
+constexpr int V_ABOVE = 4, V_BELOW = 8;
+constexpr float REF_FAR = 96.f;
 
 // max / sum over the four lanes 16 apart that share a query row
 __device__ __forceinline__ float rows_max(float x)
@@ -425,7 +432,15 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
 
     f32x4 o[RT][DT], l_run[RT];   // l_run: sums of probabilities, by a product with ones: the same in every register of a lane's column
     float m_run[RT];
-    int v_ref = -256;   // biased exponent of a scale; below all of them: none yet
+    // Biased exponents of V's scales: the sums' and the smallest of all, beyond all of them while there is none, and those of blocks that are taken as they come,
+    // v_from .. v_from + v_span.
+    int v_ref = -256, v_low = 256, v_from = 512;
+    uint32_t v_span = V_ABOVE + V_BELOW;
+    const int v_first = __builtin_amdgcn_readlane((int)f32_bits(now.scale.y), 0) >> 23 & 255;
+    if (n_it > 0 && v_first != 127) {   // no block of zeros
+        v_ref = v_first;
+        v_from = v_ref - V_BELOW;
+    }
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
 #pragma unroll
@@ -445,7 +460,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
         }
         const int t0 = span.block(first + wave + NW * i) * 32;
         const float k_scale = bits_f32((uint32_t)__builtin_amdgcn_readlane((int)f32_bits(now.scale.x), i & 63));
-        const int v_e = __builtin_amdgcn_readlane((int)f32_bits(now.scale.y), i & 63) >> 23 & 255;
+        int v_e = __builtin_amdgcn_readlane((int)f32_bits(now.scale.y), i & 63) >> 23 & 255;
         int ql = lane;
         if (RT * PARTS > 2) asm volatile("" : "+v"(ql));   // the query operands are read again for every block: hoisted, they would not fit the registers
         f32x4 s[RT][2];   // s[t][u][r]: position t0 + 16u + 4q + r for query row c of tile t
@@ -514,23 +529,12 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
                     sc[t] = mine ? 1.f : sc[t];
                 }
         }
-        // The sums are in units of 2^(v_ref - 127), a V scale: they move to a larger one only when a block's outgrows it by 2^4.
-        if (v_e > v_ref + 4) {
-            const float down = bits_f32((uint32_t)max(v_ref - v_e + 127, 0) << 23);
-#pragma unroll
-            for (int t = 0; t < RT; ++t)
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt) o[t][dt] *= down;
-            v_ref = v_e;
-        }
-        const float ratio = bits_f32((uint32_t)max(v_e - v_ref + 127, 0) << 23);
         u32x4 pk[RT][PARTS];
-#pragma unroll
-        for (int t = 0; t < RT; ++t)
+        auto weigh = [&](int t, float ref) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e >> 1][2 * (e & 1)], sc[t], -m_run[t]));
-                const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e >> 1][2 * (e & 1) + 1], sc[t], -m_run[t]));
+                const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e >> 1][2 * (e & 1)], sc[t], -ref));
+                const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e >> 1][2 * (e & 1) + 1], sc[t], -ref));
                 uint32_t hi, lo;
                 if (PARTS == 2) {
                     split_half2(p0, p1, hi, lo);
@@ -540,18 +544,78 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
                 }
                 pk[t][0][e] = hi;
             }
+        };
+        auto codes = [&](int dt, float ratio) {
+            const u32x4 &w = v[dt >> 1];
+            return dt & 1 ? codes_half8<FMT>(w[2], w[3], ratio) : codes_half8<FMT>(w[0], w[1], ratio);
+        };
+        auto times = [&](const half8_t &x, int t, f32x4 sum) {
 #pragma unroll
-        for (int t = 0; t < RT; ++t)
+            for (int part = 0; part < PARTS; ++part) sum = mfma16(x, __builtin_bit_cast(half8_t, pk[t][part]), sum);
+            return sum;
+        };
+        // The sums are in units of 2^(v_ref - 127), a V scale: they move to a larger one only when a block's outgrows it, and not for a block of zeros, whose
+        // scale says nothing.
+        const int low_was = v_low;
+        v_low = min(v_low, v_e);
+        if (__builtin_expect((uint32_t)(v_e - v_from) > v_span, false)) {
+            uint32_t any = 0;
 #pragma unroll
-            for (int part = 0; part < PARTS; ++part) l_run[t] = mfma16(ones, __builtin_bit_cast(half8_t, pk[t][part]), l_run[t]);
+            for (int x = 0; x < VR; ++x)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) any |= FMT == SSSD_KV8_E4M3 ? v[x][e] & 0x7F7F7F7Fu : v[x][e] ^ 0x80808080u;
+            const bool some = __any(any != 0), far = some && v_ref >= 0;
+            if (some) {
+                const float down = bits_f32((uint32_t)max(v_ref - v_e + 127, 0) << 23);
+                if (v_e > v_ref) {
+#pragma unroll
+                    for (int t = 0; t < RT; ++t)
+#pragma unroll
+                        for (int dt = 0; dt < DT; ++dt) o[t][dt] *= down;
+                }
+                v_ref = max(v_ref, v_e);
+                const int top = min(v_ref + V_ABOVE, v_low + V_ABOVE + V_BELOW);
+                v_from = top < v_ref - V_BELOW ? 512 : v_ref - V_BELOW;   // 512: beyond all
+                v_span = (uint32_t)(top - v_from) & 31u;
+            }
+            if (far) {
+                const f32x4 none = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY}, zero = f32x4{0.f, 0.f, 0.f, 0.f};
+                const float down = bits_f32((uint32_t)max(v_e - v_ref + 127, 0) << 23);
+                float back[RT];   // from the block's reference and scale to the row's reference and the unit
+#pragma unroll
+                for (int t = 0; t < RT; ++t) {
+                    const float m = rows_max(max3(max3(s[t][0][0], s[t][0][1], s[t][0][2]), max3(s[t][0][3], s[t][1][0], s[t][1][1]), max3(s[t][1][2], s[t][1][3], s[t][1][3])));
+                    const float ref = fmaxf(above(m, sc[t], REF_BELOW), m_run[t] - REF_FAR);
+                    weigh(t, ref);
+                    s[t][0] = s[t][1] = none;   // then there is nothing left of the block
+                    back[t] = __builtin_amdgcn_exp2f(ref - m_run[t]);
+                    l_run[t] += times(ones, t, zero) * back[t];
+                    back[t] *= down;
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) {
+                    const half8_t vv = codes(dt, 1.f);
+#pragma unroll
+                    for (int t = 0; t < RT; ++t) o[t][dt] += times(vv, t, zero) * back[t];
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            if (!some) v_low = low_was;
+            v_e = v_ref;
+#pragma unroll
+            for (int x = 0; x < VR; ++x) asm volatile("" : "+v"(v[x]));   // its codes as halves are not kept for what follows: 32 registers
+        }
+        const float ratio = bits_f32((uint32_t)(v_e - v_ref + 127) << 23);   // 2^-V_BELOW .. 2^V_ABOVE
+#pragma unroll
+        for (int t = 0; t < RT; ++t) weigh(t, m_run[t]);
+#pragma unroll
+        for (int t = 0; t < RT; ++t) l_run[t] = times(ones, t, l_run[t]);
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) {
-            const u32x4 &w = v[dt >> 1];
-            const half8_t vv = dt & 1 ? codes_half8<FMT>(w[2], w[3], ratio) : codes_half8<FMT>(w[0], w[1], ratio);
+            const half8_t vv = codes(dt, ratio);
 #pragma unroll
-            for (int t = 0; t < RT; ++t)
-#pragma unroll
-                for (int part = 0; part < PARTS; ++part) o[t][dt] = mfma16(vv, __builtin_bit_cast(half8_t, pk[t][part]), o[t][dt]);
+            for (int t = 0; t < RT; ++t) o[t][dt] = times(vv, t, o[t][dt]);
         }
         load_v(i + 1);
     }
