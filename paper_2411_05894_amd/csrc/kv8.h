@@ -239,7 +239,7 @@ struct Kv8AttnArgs {
     const int32_t *lens, *counts, *parents;
     int window, sinks;       // window 0: all positions
     float *part_o;           // [sequence][kv head][segment][rows_pad][d] sums
-    float2 *part_ml;         // ... reference of the exponents (log2), sum of probabilities
+    f32x4 *part_ml;          // ... reference of the exponents (log2), sum of probabilities, biased exponent of the sums' unit
     int rows_pad;            // rows of a (sequence, kv head) in whole tiles
     Kv8Plan plan;
     Hand hand;               // words for segments merged inside the launch, or none

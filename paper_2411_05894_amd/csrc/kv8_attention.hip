@@ -177,23 +177,27 @@ __device__ __forceinline__ void merge_rows(const Kv8AttnArgs &a, int b, int kvh,
     const int sg = lane >> 4, cl = lane & 15;
     const size_t slot0 = ((size_t)b * a.g.nkv + kvh) * a.plan.share * a.rows_pad;
     const float *part_o = a.part_o + slot0 * HD;
-    const float2 *part_ml = a.part_ml + slot0;
-    const DieBuffer die_o(part_o, (size_t)n_seg * a.rows_pad * HD * sizeof(float)), die_ml(part_ml, (size_t)n_seg * a.rows_pad * sizeof(float2));
+    const f32x4 *part_ml = a.part_ml + slot0;
+    const DieBuffer die_o(part_o, (size_t)n_seg * a.rows_pad * HD * sizeof(float)), die_ml(part_ml, (size_t)n_seg * a.rows_pad * sizeof(f32x4));
     auto row = [&](int i) { return min(r0 + i * step, r_end - 1); };
-    auto stats = [&](int s, int r) { return DIE ? die_ml.load2((s * a.rows_pad + r) * 8) : part_ml[s * a.rows_pad + r]; };
-    float num[ROWS][E], den[ROWS], m_all[ROWS];
+    auto stats = [&](int s, int r) { return DIE ? die_ml.load4((s * a.rows_pad + r) * 16) : part_ml[s * a.rows_pad + r]; };
+    float num[ROWS][E], den[ROWS], m_all[ROWS], v_all[ROWS];   // v_all: the unit of the sums, that of the segment with the largest
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
-        m_all[i] = NONE;
+        m_all[i] = v_all[i] = NONE;
         if (MANY)
-            for (int s = lane; s < n_seg; s += 64) m_all[i] = fmaxf(m_all[i], stats(s, row(i)).x);
+            for (int s = lane; s < n_seg; s += 64) {
+                const f32x4 x = stats(s, row(i));
+                m_all[i] = fmaxf(m_all[i], x[0]);
+                v_all[i] = fmaxf(v_all[i], x[2]);
+            }
         den[i] = 0.f;
 #pragma unroll
         for (int e = 0; e < E; ++e) num[i][e] = 0.f;
     }
     for (int base = 0; base < (MANY ? n_seg : 1); base += 4 * U) {
         f32x4 pv[ROWS][U][E / 4];
-        float2 ml[ROWS][U];
+        f32x4 ml[ROWS][U];
 #pragma unroll
         for (int i = 0; i < ROWS; ++i)
 #pragma unroll
@@ -208,11 +212,18 @@ __device__ __forceinline__ void merge_rows(const Kv8AttnArgs &a, int b, int kvh,
             for (int i = 0; i < ROWS; ++i) {
                 if (!MANY) {
 #pragma unroll
-                    for (int u = 0; u < U; ++u) m_all[i] = fmaxf(m_all[i], ml[i][u].x);
+                    for (int u = 0; u < U; ++u) {
+                        m_all[i] = fmaxf(m_all[i], ml[i][u][0]);
+                        v_all[i] = fmaxf(v_all[i], ml[i][u][2]);
+                    }
                     m_all[i] = rows_max(m_all[i]);
+                    v_all[i] = rows_max(v_all[i]);
                 } else {
 #pragma unroll
-                    for (int x = 32; x > 0; x >>= 1) m_all[i] = fmaxf(m_all[i], __shfl_xor(m_all[i], x));
+                    for (int x = 32; x > 0; x >>= 1) {
+                        m_all[i] = fmaxf(m_all[i], __shfl_xor(m_all[i], x));
+                        v_all[i] = fmaxf(v_all[i], __shfl_xor(v_all[i], x));
+                    }
                 }
             }
         }
@@ -221,10 +232,10 @@ __device__ __forceinline__ void merge_rows(const Kv8AttnArgs &a, int b, int kvh,
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const bool on = base + 4 * u + sg < n_seg;
-                const float w = on ? __builtin_amdgcn_exp2f(ml[i][u].x - m_all[i]) : 0.f;
-                den[i] = on ? __builtin_fmaf(w, ml[i][u].y, den[i]) : den[i];
+                const float w = on ? __builtin_amdgcn_exp2f(ml[i][u][0] - m_all[i]) : 0.f, wv = __builtin_ldexpf(w, (int)(ml[i][u][2] - v_all[i]));
+                den[i] = on ? __builtin_fmaf(w, ml[i][u][1], den[i]) : den[i];
 #pragma unroll
-                for (int e = 0; e < E; ++e) num[i][e] = on ? __builtin_fmaf(w, pv[i][u][e / 4][e % 4], num[i][e]) : num[i][e];
+                for (int e = 0; e < E; ++e) num[i][e] = on ? __builtin_fmaf(wv, pv[i][u][e / 4][e % 4], num[i][e]) : num[i][e];
             }
     }
 #pragma unroll
@@ -239,7 +250,7 @@ __device__ __forceinline__ void merge_rows(const Kv8AttnArgs &a, int b, int kvh,
         for (int e = 0; e < E; e += 4) {
             f32x4 y;
 #pragma unroll
-            for (int x = 0; x < 4; ++x) y[x] = rows_sum(num[i][e + x]) * inv;
+            for (int x = 0; x < 4; ++x) y[x] = __builtin_ldexpf(rows_sum(num[i][e + x]) * inv, (int)v_all[i] - 127);
             if (sg == e / 4) store4(a.out, to, cl * E + e, y);
         }
     }
@@ -267,7 +278,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
     __shared__ uint32_t word_s[RT * 16];
     __shared__ int low_s[RT * 16], way_s;
     __shared__ float2 ml_s[NW][RT * 16];
-    __shared__ float vref_s[NW];
+    __shared__ int vref_s[NW];
 
     const int passes = a.plan.passes, share = a.plan.share, nkv = a.g.nkv;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -628,7 +639,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
     for (int t = 0; t < RT; ++t)
         if (q == 0) ml_s[wave][t * 16 + c] = float2{m_run[t], l_run[t][0]};
-    if (lane == 0) vref_s[wave] = v_ref < 0 ? 0.f : bits_f32((uint32_t)v_ref << 23);
+    if (lane == 0) vref_s[wave] = v_ref;
 #pragma unroll
     for (int w = 0; w < NW; ++w)
         if (w == wave)
@@ -650,6 +661,9 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
                     for (int x = 0; x < QT; ++x) part(w, wave, t, x) = o[t][w * QT + x];
         __syncthreads();
+        int v_all = vref_s[0];
+#pragma unroll
+        for (int w = 1; w < NW; ++w) v_all = max(v_all, vref_s[w]);
 #pragma unroll
         for (int t = tt; t < tt + TR && t < RT; ++t) {
             const int row = (rt0 + t) * 16 + c;
@@ -661,13 +675,13 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
                 m_all = fmaxf(m_all, s4[i].x);
             }
             float l_all = 0.f;
-            f32x4 y[QT];
+            f32x4 y[QT];   // in units of the waves' largest
 #pragma unroll
             for (int x = 0; x < QT; ++x) y[x] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < NW; ++i) {
                 const int w = (wave + i) & (NW - 1);
-                const float f = __builtin_amdgcn_exp2f(s4[i].x - m_all), fv = f * vref_s[w];
+                const float f = __builtin_amdgcn_exp2f(s4[i].x - m_all), fv = __builtin_ldexpf(f, vref_s[w] - v_all);
                 l_all += s4[i].y * f;
 #pragma unroll
                 for (int x = 0; x < QT; ++x) y[x] += (i ? part(wave, w, t, x) : own[t][x]) * fv;
@@ -678,12 +692,17 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
                 const float inv = l_all != 0.f ? 1.f / l_all : 0.f;   // a row that sees nothing: 0
                 char *to = a.out.at(b, ro.j, ro.head);
 #pragma unroll
-                for (int x = 0; x < QT; ++x) store4(a.out, to, (dt0 + x) * 16 + 4 * q, y[x] * inv);
+                for (int x = 0; x < QT; ++x) {
+                    f32x4 z;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) z[e] = __builtin_ldexpf(y[x][e] * inv, v_all - 127);
+                    store4(a.out, to, (dt0 + x) * 16 + 4 * q, z);
+                }
             } else {
                 const size_t at = (((size_t)b * nkv + kvh) * share + segment) * a.rows_pad + row;
 #pragma unroll
                 for (int x = 0; x < QT; ++x) *reinterpret_cast<f32x4 *>(a.part_o + at * HD + (dt0 + x) * 16 + 4 * q) = y[x];
-                if (wave == 0 && q == 0) a.part_ml[at] = float2{m_all, l_all};
+                if (wave == 0 && q == 0) a.part_ml[at] = f32x4{m_all, l_all, (float)v_all, 0.f};
             }
         }
     }
@@ -800,7 +819,7 @@ Kv8Plan kv8_plan(int B, int n, int gq, int nkv, int blocks, bool f32)
     return p;
 }
 
-size_t kv8_attention_ws(int d) { return HAND_WORDS + (size_t)KV8_GROUPS * KV8_MAX_TILES * 16 * (d * sizeof(float) + sizeof(float2)); }
+size_t kv8_attention_ws(int d) { return HAND_WORDS + (size_t)KV8_GROUPS * KV8_MAX_TILES * 16 * (d * sizeof(float) + sizeof(f32x4)); }
 
 hipError_t launch_kv8_attention(Kv8AttnArgs a, int fmt, int d, void *ws, hipStream_t s)
 {
@@ -812,6 +831,6 @@ hipError_t launch_kv8_attention(Kv8AttnArgs a, int fmt, int d, void *ws, hipStre
     a.rows_pad = tiles * 16;
     a.hand.words = a.plan.share > 1 && a.plan.in_die ? (uint64_t *)ws : nullptr;
     a.part_o = reinterpret_cast<float *>((char *)ws + HAND_WORDS);
-    a.part_ml = reinterpret_cast<float2 *>(a.part_o + (size_t)KV8_GROUPS * KV8_MAX_TILES * 16 * d);
+    a.part_ml = reinterpret_cast<f32x4 *>(a.part_o + (size_t)KV8_GROUPS * KV8_MAX_TILES * 16 * d);
     return d == 128 ? launch_hd<128>(a, fmt, rt, s) : launch_hd<64>(a, fmt, rt, s);
 }

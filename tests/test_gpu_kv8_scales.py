@@ -21,13 +21,15 @@ def ints(v):
     return torch.tensor(v, dtype=torch.int32, device=DEV)
 
 
-def check(fmt, dtype, nq, nkv, d, lens, n, sign, size, q0, room=0, parents=None, window=0, sinks=0, close=False, seed=1):
-    """sign, size [B][positions]: of each position's key, and of its V."""
+def check(fmt, dtype, nq, nkv, d, lens, n, sign, size, q0, room=0, parents=None, window=0, sinks=0, close=False, seed=1, uniform=False, least=0.0):
+    """sign, size [B][positions]: of each position's key, and of its V (uniform: up to that size); least: half a step of the smallest results."""
     g = torch.Generator(device=DEV).manual_seed(seed)
     B, rows = size.shape
     cache = kv8.Kv8Cache(1, nq, nkv, d, B, rows + room, fmt, device=DEV)
     k, v = torch.zeros(B, rows, nkv, d, device=DEV), torch.randn(B, rows, nkv, d, generator=g, device=DEV)
     k[..., 0] = sign.float().to(DEV)[..., None]
+    if uniform:
+        v = torch.rand(v.shape, generator=g, device=DEV) * 2 - 1
     v = (v.double() * size.to(DEV)[..., None, None]).float()
     cache.sssd_kv8_append(0, k, v, ints([0] * B), counts=ints([a + n for a in lens]))
     kk, vv = torch.empty_like(k), torch.empty_like(v)
@@ -42,7 +44,7 @@ def check(fmt, dtype, nq, nkv, d, lens, n, sign, size, q0, room=0, parents=None,
         total = lens[b] + n
         assert torch.equal(kk[b, :total], k[b, :total])
         want, mass, most = attend(q[b], kk[b, :total].double(), vv[b, :total].double(), lens[b], parents[b] if parents else None, window, sinks)
-        bound = mass * (8 * most * 2.0 ** -24 + 2.0 ** -20)
+        bound = mass * (8 * most * 2.0 ** -24 + 2.0 ** -20) + least
         if close:
             bound = bound + 2.0 ** -32 * vv[b, :total].double().abs().sum(0).repeat_interleave(nq // nkv, 0)
         if dtype == torch.bfloat16:
@@ -117,3 +119,21 @@ def test_a_sequence_of_ever_larger_blocks(fmt):
         for e in (at, 9 - at, (at * 7) % 10):
             size = torch.exp2(e.double() * step)[None]
             check(fmt, torch.float32, 4, 2, 64, [blocks * 32 - 1], 1, torch.where(at[None] % 2 == 0, 1.0, -1.0), size, 24.0, room=8000)
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("nq,nkv,d,B,n,blocks,room", PLANS + [(4, 2, 64, 1, 3, 40, 0), (6, 3, 128, 2, 2, 90, 0)])
+def test_values_at_the_ends_of_the_range(fmt, dtype, nq, nkv, d, B, n, blocks, room):
+    """Up to 2^127, the largest that the cache takes as finite, with every other block 2^30 smaller or not, and down to subnormal numbers, where results are
+    rounded to multiples of 2^-149, or in bf16 of 2^-133.  Segments of one sequence, joined inside the launch or by a second one, among them."""
+    for q0 in (0.0, 3.0):
+        for top in (127, 124, 120, -100, -118, -126):
+            for gap in (0, 30):
+                if top - gap < -126:
+                    continue
+                print(f"kv8 ends {fmt} {dtype} {nq}/{nkv}x{d} B {B} n {n} 2^{top} - {gap} q {q0}", flush=True)
+                large = large_blocks("mixed", B, blocks, blocks + 7).repeat_interleave(32, 1)
+                size = torch.where(large, 2.0 ** top, 2.0 ** (top - gap)).double()
+                check(fmt, dtype, nq, nkv, d, [blocks * 32 - n] * B, n, torch.where(large, -1.0, 1.0), size, q0, room, uniform=True,
+                      least=2.0 ** -149 if dtype == torch.float32 else 2.0 ** -149 + 2.0 ** -134)
