@@ -24,8 +24,9 @@ template <int FMT> __device__ __forceinline__ float block_scale(float most)
     return bits == 0 ? 1.f : bits_f32((uint32_t)max(x, 1) << 23);
 }
 
-// Magnitudes above 2^127 are taken as infinite: rounded up, they would stand for 2^128.
-__device__ __forceinline__ bool finite(float x) { return fabsf(x) <= 0x1p127f; }
+// Magnitudes of new rows above LARGEST are taken as infinite: rounded up, they would stand for 2^128.  What the cache holds is finite; the largest code, in place of
+// an infinite value beside one of 2^127, stands for more.
+constexpr float LARGEST = 0x1p127f, LARGEST_HELD = 0x1.fffffep127f;
 
 // Four codes of values already divided by the scale.
 template <int FMT> __device__ __forceinline__ uint32_t to_codes(float a, float b, float c, float d)
@@ -490,6 +491,8 @@ template <int HD, int FMT, bool MANY> __global__ __launch_bounds__(2 * HD, LB) v
         if (MANY && h + 1 < h1) fetch(h + 1, row + next);
         float most = 0.f;
         bool odd = false;
+        const float largest = j < 0 ? LARGEST_HELD : LARGEST;
+        auto finite = [&](float x) { return fabsf(x) <= largest; };
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             most = fmaxf(most, fmaxf(finite(x[i]) ? fabsf(x[i]) : 0.f, finite(y[i]) ? fabsf(y[i]) : 0.f));

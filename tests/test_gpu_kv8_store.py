@@ -464,3 +464,21 @@ def test_several_heads_to_a_workgroup(fmt, nkv, d, dtype, rotary, interleaved):
             for a, z in at:
                 cache.sssd_kv8_read(0, ints(lens[a:z]), ints(counts[a:z]), *(x[a:z] for x in got[-1]), first=a)
         assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_infinite_values_beside_the_largest_are_reported_once(fmt):
+    """An infinite value is held as the block's largest code; beside one of 2^127 that stands for more than 2^127, but is a number from then on: later rows
+    in its block raise nothing and change none of its bits."""
+    x = torch.randn(1, 9, 2, 64, device=DEV)
+    x[0, 2, 0, 5], x[0, 3, 0, 6], x[0, 4, 0, 7] = 2.0 ** 127, float("inf"), -float("inf")
+    cache = kv8.Kv8Cache(1, 2, 2, 64, 1, 64, fmt, device=DEV)
+    cache.sssd_kv8_append(0, x, x, ints([0]), counts=ints([5]))
+    assert cache.sssd_kv8_sync() == SSSD_EINVAL
+    before = read_all(cache, 0, [5], 5, torch.float32)
+    want, s = held(x[0, :5], fmt)
+    assert torch.equal(before[0][0].double(), want) and before[0][0, 3, 0, 6] == LIMIT[fmt] * s[0] > 2.0 ** 127
+    cache.sssd_kv8_append(0, x[:, 5:].contiguous(), x[:, 5:].contiguous(), ints([5]))
+    assert cache.sssd_kv8_sync() == SSSD_OK
+    for a, b in zip(before, read_all(cache, 0, [9], 9, torch.float32)):
+        assert torch.equal(a[0], b[0, :5])
