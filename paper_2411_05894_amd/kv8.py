@@ -156,8 +156,8 @@ class Kv8Cache:
         if rope is not None:
             assert rope.device == self.device
             turn = rope.ref
+        assert (q is None) == (q_out is None), "q and q_out come together"
         if q is not None:
-            assert q_out is not None
             of_q = (B, n, self.n_q_heads, self.head_dim)
             qq, to = self._heads(q, q, of_q), self._heads(q_out, q, of_q)
         _enqueue(_lib().sssd_kv8_append, self.device, self._ref, layer, first, B, n, self._heads(k, k, shape), self._heads(v, k, shape),

@@ -161,3 +161,12 @@ def test_the_binding_checks_tensors():
     with pytest.raises(AssertionError):
         kv8._ints(torch.zeros(3, dtype=torch.int32), (2,), -1)
     assert kv8._rows(x[:, :, 1:], -1) == kv8.ROWS(x.data_ptr() + 256, 0, 384, 128, 64) and len(kv8.ROWS(0, 0, 0, 0, 0)) == 40   # sssd_rows
+
+
+def test_queries_come_with_a_place_for_them():
+    c = kv8.Kv8Cache.__new__(kv8.Kv8Cache)      # without device buffers: the check comes first
+    c.n_q_heads, c.n_kv_heads, c.head_dim, c.device = 2, 2, 64, -1
+    x, lens = torch.zeros(1, 3, 2, 64), torch.zeros(1, dtype=torch.int32)
+    for more in (dict(q=x), dict(q_out=x)):
+        with pytest.raises(AssertionError, match="together"):
+            c.sssd_kv8_append(0, x, x, lens, **more)
