@@ -40,7 +40,6 @@ __device__ __forceinline__ int kv8_entry(const Kv8Geom &g, int b, int blk)
     const size_t at = (size_t)b * g.blocks_per_seq + blk;
     return g.table ? g.table[at] : (int)at;
 }
-__device__ __forceinline__ int kv8_page(const Kv8Geom &g, int b, int blk) { return min(max(kv8_entry(g, b, blk), 0), g.n_pages - 1); }
 
 // Rows of heads as a kernel takes them (sssd_rows); `vec`: 16 bytes at a time.
 struct Rows8 {

@@ -11,9 +11,6 @@
 
 namespace {
 
-#ifndef LB
-#define LB 1
-#endif
 // ------------------------------------------------------------------------------------------------ codes ----
 // The scale of a block of largest finite magnitude `most`: the smallest power of two with most <= 448 s or 127 s, at least 2^-126; 1 for
 // none.  From the bits: most = 1.m * 2^(E-127), and 448 = 1.75 * 2^8, 127 = 1.984375 * 2^6.
@@ -147,8 +144,8 @@ template <int HD> __device__ __forceinline__ u32x4 *block_record(uint8_t *codes,
 }
 
 // ------------------------------------------------------------------------------------------------- rope ----
-// Both runs of a Place rotated, of a head that is rotated as a whole: by halves they are each other's partners, and neighbours lie in a run.  own: cos
-// and sin of two of the thread's eight angles, T apart.
+// Both runs of a Place rotated, of a head that is rotated as a whole: by halves they are each other's partners, and neighbours lie in a run.  angle(i): cos
+// and sin of the thread's i-th of eight.
 template <typename Angle> __device__ __forceinline__ void rotate_whole(bool neighbours, Angle angle, float (&x)[8], float (&y)[8])
 {
 #pragma unroll
@@ -351,7 +348,7 @@ template <int T> __device__ __forceinline__ int touched_page(const Kv8StoreArgs 
 
 // ----------------------------------------------------------------------------------------------- append ----
 // Workgroup = (sequence, touched block, `per` kv heads, K or V), MANY: more than one; behind them the workgroups that rotate queries.
-template <int HD, int FMT, bool MANY> __global__ __launch_bounds__(2 * HD, LB) void append_kernel(Kv8StoreArgs a, int storing)
+template <int HD, int FMT, bool MANY> __global__ __launch_bounds__(2 * HD) void append_kernel(Kv8StoreArgs a, int storing)
 {
     constexpr int T = 2 * HD, PITCH = HD / 2 + 2;
     __shared__ float most_s[2][HD / 32];
