@@ -141,10 +141,11 @@ int sssd_kv8_read(const sssd_kv8 *kv, int32_t layer, int32_t first, int32_t B, i
  * Attention of n <= 32 new rows of each of the sequences in slots 0 .. B-1, which are in the cache (sssd_kv8_append):
  * softmax(q . k / sqrt(head_dim)) over what a row sees, times v.
  *   q, out   [B][n][n_q_heads][head_dim], of one type; q already rotated.  They must not overlap.  Scores, softmax and sums are
- *            held to 32-bit accuracy for SSSD_F32, probabilities to 22 bits of them and to 2^-32 of the largest; for SSSD_BF16
- *            probabilities are rounded to 11 bits.  Any finite q will do whose scores are in float32's range; a row of q that is
- *            no finite number spoils its own results alone.  The scales of V's blocks may lie anywhere; values of blocks 2^80 and
- *            more below the largest scale that any row of the call sees may count as 0
+ *            held to 32-bit accuracy for SSSD_F32, q and probabilities to 22 bits; for SSSD_BF16 probabilities are rounded to 11
+ *            bits.  For both, a channel of q is held to 2^-39 of its row's largest at the finest, a probability to 2^-32 of its
+ *            row's largest.  Any finite q will do whose scores are in float32's range; a row of q that is no finite number spoils
+ *            its own results alone.  The scales of V's blocks may lie anywhere; values of blocks 2^80 and more below the largest
+ *            scale that any row of the call sees may count as 0
  *   lens, counts, parents  as in sssd_kv8_append: row j sees the old rows (below lens[b]) and, of the new ones, itself
  *            and its ancestors
  *   window   0: all of them.  Else those fewer than `window` positions behind the row's own (a new row's position is

@@ -14,12 +14,12 @@
 // blocks of one (sequence, kv head) in turn; a wave requests a block's K and V as soon as it has used those before.  Sequences are cut into segments by the
 // plan (kv8_plan, cut_of), joined inside the launch where one die can hold them.
 //
-// What bounds it: from some thousands of positions a chip's worth of workgroups on the stream of the cache.  8B, B = 4, n = 9, 32768 bf16 269 MB in 54.6 us,
-// 4.9 TB/s, of which some 45 stream at 6 TB/s, as fast as the blocks are read by a kernel that does nothing else (46 us), around them 5 us until K is there
-// and the queries are operands and 3 for the sums of waves and segments; float32 queries 64 (twice the products).  B = 32, n = 5, 1024..4096 173 MB in
-// 41 us: one workgroup per head and sequence, so the longest decides; all of 2500 35.6.  Short ones on the chain of round trips: arguments, lens, page,
-// block, sums of waves, partial results, their arrival: B = 1, n = 9, 2048 8.8 us, of which K is requested after 2.2 and the rows are joined in the
-// last 2.
+// What bounds it: from some thousands of positions a chip's worth of workgroups on the stream of the cache.  us, captured (and called one behind the other, where
+// launches overlap): 8B, B = 4, n = 9, 32768 bf16 269 MB in 58 (55), 4.6 TB/s, of which some 45 stream at 6 TB/s, as fast as the blocks are read in the same
+// order by a kernel that does nothing else (46 us), around them 5 until K is there and the queries are operands and 3 for the sums of waves and segments;
+// float32 queries 68 (twice the products).  B = 32, n = 5, 1024..4096 173 MB in 47 (42): one workgroup per head and sequence, so the longest decides; all
+// of 2500 35.8.  Short ones on the chain of round trips: arguments, lens, page, block, sums of waves, partial results, their arrival: B = 1, n = 9, 2048
+// float32 9.7 (8.9), of which K is requested after 2.2 and the rows are joined in the last 2.
 #include "kv8.h"
 
 #include <algorithm>
@@ -136,9 +136,9 @@ __device__ __forceinline__ Span span_of(int len, int count, int window, int sink
 struct Cut {
     int each, n;   // blocks per segment (the last may have fewer), segments
 };
-// By the sequence's own blocks and the call's plan alone: what the others hold changes no bit.  At least four blocks a segment, one for each wave (2048
-// positions with eight at least 12.5 us, so 11.5); up to eight are one segment, which need not be joined.  Long segments are whole rounds of four waves
-// (4 x 32768 57.4 us, else 59.2; 16 sequences of 4000 with 32 rows 82.7, else 86.8).
+// By the sequence's own blocks and the call's plan alone: what the others hold changes no bit.  At least four blocks a segment, one for each wave (300
+// positions of 8B, float32, with eight at least 8.9 us, so 8.2; 2048 9.7 either way); up to eight are one segment, which need not be joined.  Long segments are
+// whole rounds of four waves (4 x 32768 bf16 58 us, else 60; one of 32768 float32 27.5, else 28.3; but 16 sequences of 4000 with 32 rows 56.5, else 54.6).
 __device__ __forceinline__ Cut cut_of(int blocks, int share)
 {
     auto up = [](int x, int y) { return (int)(((unsigned)x + (unsigned)y - 1u) / (unsigned)y); };
@@ -748,8 +748,8 @@ template <int HD, int FMT, int PARTS> hipError_t launch_parts(const Kv8AttnArgs 
 {
     const dim3 grid(((uint32_t)a.B * a.g.nkv + 7) / 8 * 8 * a.plan.share * a.plan.passes);
     // Eight waves to a workgroup where a compute unit has one workgroup, of long segments and more than a wave alone on its SIMD gets done while
-    // the cache streams: float32 queries, or several passes over the cache.  us, four / eight: 8B f32 B = 4, n = 9, 32768 73 / 67; 70B B = 16,
-    // n = 9, 2048 bf16 30.9 / 26.8, f32 36.4 / 34.1; B = 7, n = 13, 700..1500 f32 23.3 / 21.0; not: bf16 in one pass, 8B B = 4, 32768 57.3 / 59.7,
+    // the cache streams: float32 queries, or several passes over the cache.  us, four / eight: 8B f32 B = 4, n = 9, 32768 70 / 68; 70B B = 16,
+    // n = 9, 2048 bf16 27.7 / 26.3, f32 36.3 / 34.7; B = 7, n = 13, 700..1500 f32 24.1 / 21.6; not: bf16 in one pass, 8B B = 4, 32768 57.3 / 59.7,
     // many segments, f32 B = 1, 2048 11.4 / 13.0, two workgroups on a unit, B = 16, n = 32, 500 13.4 / 19.6
     const bool eight = HD == 128 && rt > 1 && a.plan.share <= 8 && (int64_t)a.B * a.g.nkv * a.plan.share * a.plan.passes <= 256 && (PARTS == 2 || a.plan.passes > 1);
 #define KV8_ATTN(RT, NW) hipLaunchKernelGGL((kv8_attn_kernel<HD, FMT, RT, PARTS, NW>), grid, dim3(NW * 64), 0, s, a)
@@ -793,6 +793,7 @@ template <int HD> hipError_t launch_hd(const Kv8AttnArgs &a, int fmt, int rt, hi
 //    B = 4, n = 9, 32768 57.4 / 57.7 / 76.8.
 //  - Segments of a sequence so that 256 workgroups have work; twice that where 256 in whole segments leave a quarter of the chip idle (8B B = 12, 3000
 //    24.6, without 27.8; for all calls: B = 32, 2500 41, now 36).
+// The limits were found with 8 kv heads of 128 channels; others go by the same ones, unmeasured.
 Kv8Plan kv8_plan(int B, int n, int gq, int nkv, int blocks, bool f32)
 {
     const int tiles = (n * gq + 15) / 16;

@@ -1,9 +1,9 @@
 // Rotary positions, and writing, reading back and committing rows of a KV cache in 8 bits.
 //
 // All of it is bound by memory for prompts and by a launch and two or three dependent round trips for a step's few rows.  Captured, inputs in memory: a
-// rotation of 9 rows 3.3 us (the launch alone 3), of 8191 rows of 40 heads of 128 in bf16 38.9 (168 MB, 4.3 TB/s); an append of 9 rows in 8 heads 4.95, with
-// 32 heads of queries the same, of 100001 rows 121 (614 MB, 5.1 TB/s; a copy of 1 GiB 5.2), with the queries 433 (5.2 TB/s); reading 9 rows back 3.7, 32768 45
-// (4.5 TB/s); committing trees of 9 rows of 16 sequences in 32 layers 45.
+// rotation of 9 rows 3.2 us (the launch alone 3), of 8191 rows of 40 heads of 128 in bf16 38.5 (168 MB, 4.4 TB/s); an append of 9 rows in 8 heads 4.9, with
+// 32 heads of queries the same, of 100001 rows 132 (614 MB, 4.7 TB/s; a copy of 1 GiB 5.2), with the queries 455 (5.0 TB/s); reading 9 rows back 3.7, 32768 48
+// (4.2 TB/s); committing trees of 9 rows of 16 sequences in 32 layers 46, of which writing each touched block anew needs 13 (67 MB) and the two launches 6.
 //
 // A block's scale needs all of its live rows, so a workgroup takes whole blocks: 32 rows of a head, sixteen values a thread, in the order of K's records.
 // Rows that were there before are taken out of their codes and go through the new scale like new ones.
@@ -202,7 +202,7 @@ __device__ __forceinline__ void rotate_part(const Rope8 &rp, const Rows8 &r, con
 // (some thirty instructions each); then the threads pass over the rows in the order of memory, a unit each: by halves U pairs (i .. i+U-1 with
 // their partners), as neighbours U/2 pairs that lie in a row, or U channels that pass.
 // Measured against a thread with the angles of eight pairs in registers that takes them through several heads (32 places of 256 bytes at a time, a
-// row's stride apart): 8191 rows of 40 heads of 128, bf16, 49.6 -> 43.5 us cold, now 38.9 (168 MB, 4.3 TB/s; a copy of 1 GiB 5.2).
+// row's stride apart): 8191 rows of 40 heads of 128, bf16, 49.6 -> 43.5 us cold, now 38.5 (168 MB, 4.4 TB/s; a copy of 1 GiB 5.2).
 struct RopeRow {
     int b, j, position, on;   // on: 0 where the row is left as it is
 };
@@ -420,7 +420,7 @@ template <int HD, int FMT, bool MANY> __global__ __launch_bounds__(2 * HD) void 
     for (int i = 0; i < 4; ++i) raw[i] = u32x4{0, 0, 0, 0};
     fetch(h0, row);
     // Angles once for all heads, in LDS (in registers they would leave fewer waves): a thread its own eight, or, of a head that is rotated in part, all
-    // threads those of the block's rows between them.  us of a prompt of 32768 in 8 heads of 128: angles for every head anew 71, once 48.
+    // threads those of the block's rows between them.  us of a prompt of 32768 in 8 heads of 128: angles for every head anew 67, once 50.
     f32x4 *own = reinterpret_cast<f32x4 *>(table) + threadIdx.x;   // cos and sin of two angles at own[T * i]
     float2 here[8];                                                // ... of one head alone
     auto angle = [&](int i) {
@@ -658,8 +658,8 @@ __global__ __launch_bounds__(64) void advance_kernel(Kv8StoreArgs a, const int32
 
 // Units of eight channels where pairs and the channels that pass divide into them, else single pairs.  A workgroup takes as many rows, with all their
 // heads, as have `each` units for a thread, while eight workgroups are left for every compute unit: one in a rotation alone (8191 rows of 40 heads of 128
-// in bf16 38.9 us, three rows a workgroup 44; 12000 of 16 of 64 14.9, one row a workgroup 17.1), four beside rows that are stored, where a workgroup
-// has more to look up first and fewer fit (prompts of 32768 with 32 heads of queries 147, one 166).  Few rows are cut by heads, too.
+// in bf16 38.5 us, three rows a workgroup 43.8; 12000 of 16 of 64 14.8, one row a workgroup 17.2), four beside rows that are stored, where a workgroup
+// has more to look up first and fewer fit (prompts of 32768 with 32 heads of queries 157, one 175).  Few rows are cut by heads, too.
 RopeWork rope_work(int B, int n, int d, int heads, int r, bool neighbours, int threads, int each)
 {
     RopeWork w;
@@ -705,9 +705,9 @@ hipError_t launch_rope(const Rows8 &x, const Rows8 &out, const int32_t *position
 #define COMMIT(HD, FMT) commit_kernel<HD, FMT>
 
 // Workgroups of an append or a read, each of `per` kv heads while 800 are left: what is the same for all heads, the angles and the look at every page of
-// the sequence, is then done once.  us, one head / several: prompts in 8 heads of 128 with a rotation, 4001 13.9 / 11.5 (two), 8192 22.5 / 17.8 (four),
-// 32768 71 / 53 (eight, and with a block table 93 / 57); 16 prompts of 512 22.7 / 17.7; fewer workgroups, 4001 12.4 (three), 8192 21.5 (eight).
-// Reads have the pages alone: with a table, 100001 216 / 153 (four), 32768 56 / 51; without one 45 / 48.
+// the sequence, is then done once.  us, one head / several: prompts in 8 heads of 128 with a rotation, 4001 11.8 / 10.8 (two), 8192 20.5 / 16.1 (four),
+// 32768 67 / 50 (eight, and with a block table 83 / 54); 16 prompts of 512 20.0 / 16.0; 500 workgroups instead of 800, 4001 11.7 (four), 8192 19.9 (eight).
+// Reads have the pages alone: with a table, 100001 221 / 157 (four), 32768 60 / 54.5; without one 48 / 50.
 static int store_groups(Kv8StoreArgs &a, int most)
 {
     const int64_t all = (int64_t)a.B * a.blocks * 2 * a.g.nkv, per = all / 800;
