@@ -341,7 +341,7 @@ def prepare(case, seed):
         book.sssd_kv8_reserve(K.shape[1], lens, fill)
         cache.sssd_kv8_append(0, K, V, lens, counts=fill)
         state.update(cache=cache, book=book, starts=_int(starts + [at]), shared=_int(prefix),
-                     workspace=cache.sssd_kv8_shared_workspace(B, n, len(sizes)))
+                     workspace=cache.sssd_kv8_shared_workspace(B, n))
     else:
         live = _below(_int([a + c for a, c in zip(rows, counts)]), K.shape[1])
         state.update(rows=_int(rows), held=[_quantised(x, live, case["fmt"]) for x in (K, V)],
