@@ -37,9 +37,6 @@ extern "C" {
 #define SSSD_KV8_E4M3 0 /* 8-bit floats: 1 sign, 4 exponent, 3 mantissa bits, largest 448 */
 #define SSSD_KV8_INT8 1 /* 8-bit integers -127 .. 127 */
 
-#define SSSD_F32 0
-#define SSSD_BF16 1
-
 /* head_dim 64 or 128; n_q_heads a multiple of n_kv_heads, at most 64 times as many; n_pages: pages of a layer's pool, 0 for
  * max_batch * ceil(max_seq / 32). */
 typedef struct {
@@ -166,6 +163,73 @@ int sssd_kv8_attention(const sssd_kv8 *kv, int32_t layer, int32_t B, int32_t n, 
  */
 int sssd_kv8_commit_tree(const sssd_kv8 *kv, int32_t B, int32_t n, int32_t *lens, const int32_t *accepted_len,
                          const int32_t *accepted_path, void *stream);
+
+/* ----------------------------------------------------------------- prefixes that sequences share -- */
+/*
+ * sssd_kv8_attention for a batch whose sequences share prefixes: the same rows and results (but for the order of sums), without a window,
+ * each prefix read once for all rows of its group.  Sequences of a group lie next to each other: group g is the slots starts[g] ..
+ * starts[g+1]-1 below B, and the first shared[g] positions of all of them are the same rows.  They are read, in whole blocks
+ * (shared[g] / 32 of them), through the block table's row of the group's first sequence, whose other state plays no part.
+ *   groups      0 .. B; sequences in no group, groups of one and empty groups share nothing
+ *   starts      device int32 [groups + 1], ascending from >= 0 to <= B
+ *   shared      device int32 [groups], 0 .. max_seq
+ *   workspace   device, 256-byte aligned, any contents, at least what sssd_kv8_shared_sizes asks for this B and n (a larger B or n asks
+ *               for more); calls that share it must be ordered.  kv's own workspace is not used
+ * starts or shared out of range raise the status, and nothing is shared in that call.  A sequence shorter than its group's shared blocks is rejected
+ * like the others (sssd_kv8_attention).  Pages outside the pool among a prefix's blocks raise the status and spoil the rows of the group.
+ */
+int sssd_kv8_shared_sizes(const sssd_kv8_config *cfg, int32_t B, int32_t n, size_t *ws_bytes);
+int sssd_kv8_attention_shared(const sssd_kv8 *kv, int32_t layer, int32_t B, int32_t n, const sssd_rows *q, const sssd_rows *out,
+                              const int32_t *lens, const int32_t *counts, const int32_t *parents, int32_t groups,
+                              const int32_t *starts, const int32_t *shared, void *workspace, size_t ws_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------------- pages of the pool -- */
+/*
+ * Who has which pages.  refs[p] counts the entries of the table that name page p, and whatever else the caller holds it for; pages of count 0
+ * are free.  A new pool has a table of -1 and counts of 0.  Entries behind a sequence's pages are -1.  The three calls change table, counts
+ * and pages on the device, in all layers, and each either does all of what it says or, where it cannot, nothing but raise the status.  Pages
+ * are taken from the lowest free ones, in the order of slots and blocks.
+ */
+typedef struct {
+    int32_t *table;   /* device int32 [max_batch][blocks_per_seq]: the cache's block_table, which has to point at it */
+    int32_t *refs;    /* device int32 [n_pages] */
+    void *workspace;  /* device, 256-byte aligned, at least ws_bytes; zero-filled once by the caller; calls that share it must be ordered */
+    size_t ws_bytes;
+} sssd_kv8_pages;
+
+int sssd_kv8_pages_sizes(const sssd_kv8_config *cfg, size_t *ws_bytes);
+
+/*
+ * All slots 0 .. max_batch-1 at once: slot b becomes a continuation of what slot origins[b] was before the call (b: stays itself; -1:
+ * empty, its length 0), with lens[b] = lens[origins[b]].  Its whole blocks are shared with all who continue the same slot; of its last block, where
+ * that is partly filled, one has the page (the origin itself if it stays, else the lowest slot) and the others get copies.  Pages behind the new length,
+ * and pages that nobody names any more, are free afterwards.
+ *   origins, lens   device int32 [max_batch]; lens in-out
+ * Nothing is done where an origin is outside -1 .. max_batch-1, the length of one outside 0 .. max_seq, an entry of the table outside
+ * -1 .. n_pages-1 or of a page that counts 0, a live block without a page, or where there are too few free pages.  max_batch <= 65535.
+ */
+int sssd_kv8_fork(const sssd_kv8 *kv, const sssd_kv8_pages *pages, const int32_t *origins, int32_t *lens, void *stream);
+
+/*
+ * Room for rows lens[b] .. lens[b]+counts[b]-1 (counts NULL: n) of the sequences in slots first .. first+B-1: every block of these rows gets a page that no
+ * other entry names.  Missing pages are taken; a page that others share is replaced, by a copy where live rows (below lens[b]) are in it.  Where all
+ * who share a page ask for it in this call, the first of them (by slot and block) keeps it.  lens is not changed.
+ * Nothing is done where lens[b], counts[b] or lens[b] + counts[b] is out of range as for sssd_kv8_append, an entry that is looked at is outside
+ * -1 .. n_pages-1 or of a page that counts 0, or where there are too few free pages.
+ */
+int sssd_kv8_reserve(const sssd_kv8 *kv, const sssd_kv8_pages *pages, int32_t first, int32_t B, int32_t n, const int32_t *lens,
+                     const int32_t *counts, void *stream);
+
+/*
+ * A pool without holes.  With U pages in use (counts above 0), to NULL: the i-th of those in use at or behind U moves into the i-th free one in front
+ * of it; the others stay.  Else the i-th page in use goes to page i of another cache (the same format, layers, kv heads, head_dim, max_batch and
+ * blocks per sequence, any n_pages >= U), whose table and counts are written whole; kv and its pages stay as they were.
+ *   moved    device int32 [n_pages] or NULL: where each page is now, -1 for free ones
+ *   in_use   device int32 [1] or NULL: U, written also where nothing else is done
+ * Nothing is done where the table has an entry outside -1 .. n_pages-1 or of a page that counts 0, or U is above the other's n_pages.  The status is kv's.
+ */
+int sssd_kv8_compact(const sssd_kv8 *kv, const sssd_kv8_pages *pages, const sssd_kv8 *to, const sssd_kv8_pages *to_pages, int32_t *moved,
+                     int32_t *in_use, void *stream);
 
 /* Wait for `stream`, then clear the status and return SSSD_ENOSPACE if a call raised it for a sequence, page, count,
  * path or parent out of range, else SSSD_EINVAL if it was raised for rows that are no finite numbers, SSSD_EHIP if the

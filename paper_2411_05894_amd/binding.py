@@ -103,6 +103,9 @@ def lib() -> C.CDLL:
         l.sssd_op_gemm_scratch_bytes.argtypes = [i32, i32, i32]
         l.sssd_op_gemm_scratch_bytes.restype = C.c_size_t
         l.sssd_op_gemm.argtypes = [vp, vp, vp, i32, i32, i32, vp, vp, C.c_size_t, vp]
+        l.sssd_op_logprobs_scratch_bytes.argtypes = [i32] * 5
+        l.sssd_op_logprobs_scratch_bytes.restype = sz
+        l.sssd_op_logprobs.argtypes = [vp, i32, i32, i32, C.c_int64, C.c_float, vp, i32, vp, vp, vp, i32, vp, vp, vp, sz, vp]
         l.sssd_op_attention.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp]
         _lib = l
     return _lib
@@ -341,6 +344,28 @@ def sssd_op_sample_wide(logits: torch.Tensor, sampling: SamplingParams, uniforms
     _check(lib().sssd_op_sample_wide(_ptr(logits), rows, vocab, C.byref(sampling), _ptr(uniforms), _ptr(out), _ptr(scratch),
                                      nbytes, _stream()), "sssd_op_sample_wide")
     return out
+
+
+def sssd_op_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, n_top: int = 0, temperature: float = 1.0):
+    """logits [rows][vocab], float32 or bfloat16, any distance between rows; tokens int32 [rows][m] or None -> (logprobs [rows][m], ranks [rows][m],
+    entropy [rows], top_ids [rows][n_top], top_logprobs [rows][n_top]).  Outputs and scratch are allocated here."""
+    rows, vocab = logits.shape
+    device = logits.device
+    kind = {torch.float32: 0, torch.bfloat16: 1}.get(logits.dtype)
+    assert kind is not None and device.type == "cuda" and (logits.stride(1) == 1 or vocab == 1), "float32 or bfloat16 rows on a GPU"
+    m = 0
+    if tokens is not None:
+        assert tokens.dtype == torch.int32 and tokens.dim() == 2 and tokens.shape[0] == rows and tokens.device == device and tokens.is_contiguous()
+        m = tokens.shape[1]
+    with torch.cuda.device(device):
+        logprobs, entropy = torch.empty(rows, m, device=device), torch.empty(rows, device=device)
+        top_logprobs = torch.empty(rows, n_top, device=device)
+        ranks, top_ids = (torch.empty(rows, k, dtype=torch.int32, device=device) for k in (m, n_top))
+        nbytes = lib().sssd_op_logprobs_scratch_bytes(kind, rows, vocab, m, n_top)
+        scratch = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=device)
+        _check(lib().sssd_op_logprobs(logits.data_ptr(), kind, rows, vocab, logits.stride(0), temperature, _ptr(tokens), m, _ptr(logprobs), _ptr(ranks),
+                                      _ptr(entropy), n_top, _ptr(top_ids), _ptr(top_logprobs), _ptr(scratch), nbytes, _stream()), "sssd_op_logprobs")
+    return logprobs, ranks, entropy, top_ids, top_logprobs
 
 
 def sssd_op_gemm_small_step_rows() -> int:

@@ -244,6 +244,20 @@ struct Kv8AttnArgs {
     Hand hand;               // words for segments merged inside the launch, or none
     int32_t *status;
 };
+struct Kv8SharedArgs : Kv8AttnArgs {   // of a batch whose sequences share prefixes in groups
+    int groups;
+    const int32_t *starts, *shared;
+    int tiles;             // workgroups' row tiles of all groups at most
+    int wave_rows;         // waves of a workgroup on row tiles of their own (1, 2 or 4), the others on other segments
+    int prefix_share;      // workgroups on a prefix at most
+    int prefix_segments;   // segments of a prefix at most: prefix_share * 4 / wave_rows
+    int rows_all;          // B * n * gq
+};
 Kv8Plan kv8_plan(int B, int n, int gq, int nkv, int blocks, bool f32);   // blocks: of a sequence at most
+struct Kv8SharedPlan {
+    int rt, wave_rows, tiles, share, segments;   // row tiles of a wave; the others as in Kv8SharedArgs
+};
+Kv8SharedPlan kv8_shared_plan(int B, int n, int gq, int nkv, int groups);
+size_t kv8_shared_ws(int B, int n, int gq, int nkv, int d);
 size_t kv8_attention_ws(int d);   // bytes behind the workspace that any call's partial results take
 hipError_t launch_kv8_attention(Kv8AttnArgs a, int fmt, int d, void *ws, hipStream_t s);

@@ -33,6 +33,10 @@ class RopeArgs(C.Structure):
     _fields_ = [("turns", C.c_void_p), ("rotary_dims", C.c_int32), ("pairs", C.c_int32), ("magnitude", C.c_float)]
 
 
+class Kv8PagesArgs(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("refs", C.c_void_p), ("workspace", C.c_void_p), ("ws_bytes", C.c_size_t)]
+
+
 ROWS = struct.Struct("@Piqqq").pack      # sssd_rows as bytes: half the time of a ctypes structure
 _bound = None
 
@@ -50,6 +54,12 @@ def _lib() -> C.CDLL:
         l.sssd_kv8_read.argtypes = [p(Kv8), i32, i32, i32, i32, vp, vp, rows, rows, vp]
         l.sssd_kv8_attention.argtypes = [p(Kv8), i32, i32, i32, rows, rows, vp, vp, vp, i32, i32, vp]
         l.sssd_kv8_commit_tree.argtypes = [p(Kv8), i32, i32, vp, vp, vp, vp]
+        l.sssd_kv8_shared_sizes.argtypes = [p(Kv8Config), i32, i32, p(C.c_size_t)]
+        l.sssd_kv8_attention_shared.argtypes = [p(Kv8), i32, i32, i32, rows, rows, vp, vp, vp, i32, vp, vp, vp, C.c_size_t, vp]
+        l.sssd_kv8_pages_sizes.argtypes = [p(Kv8Config), p(C.c_size_t)]
+        l.sssd_kv8_fork.argtypes = [p(Kv8), p(Kv8PagesArgs), vp, vp, vp]
+        l.sssd_kv8_reserve.argtypes = [p(Kv8), p(Kv8PagesArgs), i32, i32, i32, vp, vp, vp]
+        l.sssd_kv8_compact.argtypes = [p(Kv8), p(Kv8PagesArgs), p(Kv8), p(Kv8PagesArgs), vp, vp, vp]
         l.sssd_kv8_sync.argtypes = [p(Kv8), vp]
         _bound = l
     return _bound
@@ -177,6 +187,24 @@ class Kv8Cache:
         _enqueue(_lib().sssd_kv8_attention, self.device, self._ref, layer, B, n, self._heads(q, q, shape), self._heads(out, q, shape),
                  _ints(lens, (B,), self.device), _ints(counts, (B,), self.device), _ints(parents, (B, n), self.device), window, sinks)
 
+    def sssd_kv8_shared_workspace(self, B: int, n: int) -> torch.Tensor:
+        """What sssd_kv8_attention_shared takes for up to B sequences of up to n rows."""
+        size = C.c_size_t()
+        _check(_lib().sssd_kv8_shared_sizes(C.byref(self.cfg), B, n, C.byref(size)), "sssd_kv8_shared_sizes")
+        return torch.empty(size.value, dtype=torch.uint8, device=self.cache.device)
+
+    def sssd_kv8_attention_shared(self, layer: int, q: torch.Tensor, lens: torch.Tensor, out: torch.Tensor, starts: torch.Tensor, shared: torch.Tensor,
+                                  workspace: torch.Tensor, counts: Optional[torch.Tensor] = None, parents: Optional[torch.Tensor] = None) -> None:
+        """Groups are sequences starts[g] .. starts[g+1]-1, whose first shared[g] positions are the same."""
+        B, n = q.shape[:2]
+        shape = (B, n, self.n_q_heads, self.head_dim)
+        groups = shared.shape[0]
+        assert workspace.get_device() == self.device and workspace.is_contiguous()
+        _enqueue(_lib().sssd_kv8_attention_shared, self.device, self._ref, layer, B, n, self._heads(q, q, shape), self._heads(out, q, shape),
+                 _ints(lens, (B,), self.device), _ints(counts, (B,), self.device), _ints(parents, (B, n), self.device), groups,
+                 _ints(starts, (groups + 1,), self.device), _ints(shared, (groups,), self.device), workspace.data_ptr(),
+                 workspace.numel() * workspace.element_size())
+
     def sssd_kv8_commit_tree(self, n: int, lens: torch.Tensor, accepted_len: torch.Tensor, accepted_path: Optional[torch.Tensor] = None) -> None:
         """n: rows of the step (accepted_path [B][n]); lens advances."""
         B = lens.numel()
@@ -186,3 +214,35 @@ class Kv8Cache:
     def sssd_kv8_sync(self) -> int:
         with torch.cuda.device(self.device):
             return _lib().sssd_kv8_sync(self._ref, torch.cuda.current_stream().cuda_stream)
+
+
+class Kv8Pages:
+    """Who has which pages of a cache's pool: owns the block table (set as the cache's), the pages' counts and the calls' workspace."""
+
+    def __init__(self, cache: Kv8Cache):
+        size = C.c_size_t()
+        _check(_lib().sssd_kv8_pages_sizes(C.byref(cache.cfg), C.byref(size)), "sssd_kv8_pages_sizes")
+        self.cache, where = cache, cache.cache.device
+        self.table = torch.full((cache.cfg.max_batch, cache.blocks_per_seq), -1, dtype=torch.int32, device=where)
+        self.refs = torch.zeros(cache.n_pages, dtype=torch.int32, device=where)
+        self.workspace = torch.zeros(size.value, dtype=torch.uint8, device=where)
+        self.args = Kv8PagesArgs(self.table.data_ptr(), self.refs.data_ptr(), self.workspace.data_ptr(), size.value)
+        self._ref = C.byref(self.args)
+        cache.sssd_kv8_set_block_table(self.table)
+
+    def sssd_kv8_fork(self, origins: torch.Tensor, lens: torch.Tensor) -> None:
+        """Slot b goes on from what slot origins[b] was (-1: empty); lens changes with it."""
+        c, slots = self.cache, (self.cache.cfg.max_batch,)
+        _enqueue(_lib().sssd_kv8_fork, c.device, c._ref, self._ref, _ints(origins, slots, c.device), _ints(lens, slots, c.device))
+
+    def sssd_kv8_reserve(self, n: int, lens: torch.Tensor, counts: Optional[torch.Tensor] = None, first: int = 0) -> None:
+        """Pages of their own for the next n (or counts[b]) rows of the sequences from slot `first` on."""
+        c, B = self.cache, lens.numel()
+        _enqueue(_lib().sssd_kv8_reserve, c.device, c._ref, self._ref, first, B, n, _ints(lens, (B,), c.device), _ints(counts, (B,), c.device))
+
+    def sssd_kv8_compact(self, to: Optional["Kv8Pages"] = None, moved: Optional[torch.Tensor] = None, in_use: Optional[torch.Tensor] = None) -> None:
+        """Pages in use to the front of the pool, or into another cache's."""
+        c = self.cache
+        assert to is None or to.cache.device == c.device
+        _enqueue(_lib().sssd_kv8_compact, c.device, c._ref, self._ref, None if to is None else to.cache._ref, None if to is None else to._ref,
+                 _ints(moved, (c.n_pages,), c.device), _ints(in_use, (1,), c.device))
