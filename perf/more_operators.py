@@ -296,7 +296,7 @@ def prepare(case, seed):
             s = SHAPES[case["shape"]]
 
             def paged(pages, data):
-                cache = kv8.Kv8Cache(case["layers"], s["nq"], s["nkv"], s["d"], case["slots"], h["per"] * BLOCK, "e4m3", n_pages=pages, device=DEV)
+                cache = kv8.Kv8Cache(case["layers"], s["nq"], s["nkv"], s["d"], case["slots"], table.shape[1] * BLOCK, "e4m3", n_pages=pages, device=DEV)
                 cache.cache.copy_(data.view(-1))
                 return kv8.Kv8Pages(cache)
             state["book"] = paged(h["pages"], pool)
