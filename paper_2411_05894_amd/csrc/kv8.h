@@ -248,7 +248,7 @@ struct Kv8SharedArgs : Kv8AttnArgs {   // of a batch whose sequences share prefi
     int groups;
     const int32_t *starts, *shared;
     int tiles;             // workgroups' row tiles of all groups at most
-    int wave_rows;         // waves of a workgroup on row tiles of their own (1, 2 or 4), the others on other segments
+    int wave_rows;         // waves of a workgroup on row tiles of their own: 4, or 1 with the others on other segments
     int prefix_share;      // workgroups on a prefix at most
     int prefix_segments;   // segments of a prefix at most: prefix_share * 4 / wave_rows
     int rows_all;          // B * n * gq
@@ -257,7 +257,7 @@ Kv8Plan kv8_plan(int B, int n, int gq, int nkv, int blocks, bool f32);   // bloc
 struct Kv8SharedPlan {
     int rt, wave_rows, tiles, share, segments;   // row tiles of a wave; the others as in Kv8SharedArgs
 };
-Kv8SharedPlan kv8_shared_plan(int B, int n, int gq, int nkv, int groups);
+Kv8SharedPlan kv8_shared_plan(int B, int n, int gq, int nkv, int groups, bool f32);
 size_t kv8_shared_ws(int B, int n, int gq, int nkv, int d);
 size_t kv8_attention_ws(int d);   // bytes behind the workspace that any call's partial results take
 hipError_t launch_kv8_attention(Kv8AttnArgs a, int fmt, int d, void *ws, hipStream_t s);

@@ -347,9 +347,9 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
     int pass, segment, b, kvh;
     int skip = 0, n_rows = 0;   // blocks that are another workgroup's; rows of a group
     if constexpr (PRE) {
-        // workgroups of one (kv head, segment) on one die, next to each other: they read the same blocks
-        const uint32_t slot = blockIdx.x >> 3, x = slot / (uint32_t)a.tiles, pair = x * 8 + (blockIdx.x & 7);
-        int tile = (int)(slot - x * a.tiles);
+        // workgroups of one (kv head, segment) on one die: they read the same blocks; tiles that no group has come last
+        const uint32_t slot = blockIdx.x >> 3, pairs = ((uint32_t)nkv * a.prefix_share + 7) >> 3, x = slot / pairs, pair = (slot - x * pairs) * 8 + (blockIdx.x & 7);
+        int tile = (int)x;
         segment = (int)(pair / (uint32_t)nkv);
         kvh = (int)pair - segment * nkv;
         if (segment >= a.prefix_share) return;

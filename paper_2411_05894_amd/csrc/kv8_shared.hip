@@ -9,7 +9,316 @@
 #include "kv8_attention.h"
 #include "kv8_host.h"
 
+#include <algorithm>
+
 namespace {
+
+// Many rows: four waves of a workgroup with up to three row tiles each on the same blocks.  A block's codes are requested two blocks ahead, a quarter by each wave,
+// turned into float16 operands once for all four and handed round in LDS (two blocks of room, one barrier a block); queries stay in registers.
+//
+// V's scales: the unit of the sums is the largest of the segment, known before the first block.  Where all of them lie within V_SPAN octaves, codes are converted in that unit, which
+// float16 holds exactly (down to 2^-21 for 8-bit floats, 2^-12 for integers); else blocks are multiplied as they are, with probabilities relative to the
+// block's own maximum (or REF_FAR below the row's reference, where that is higher), and added in 32 bits.
+constexpr int V_SPAN = V_ABOVE + V_BELOW;
+constexpr int prefix_waves(int rt, int parts) { return rt * parts <= 2 ? 2 : 1; }   // waves of a SIMD that the registers leave room for
+
+template <int HD, int FMT, int RT, int PARTS>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(prefix_waves(RT, PARTS), prefix_waves(RT, PARTS)))) void kv8_prefix_kernel(Kv8SharedArgs a)
+{
+    constexpr int KS = HD / 32, DT = HD / 16, REC = HD / 16, MINE = REC / 4;   // 16-byte records of a lane: of a block (K's, V's), of a wave
+    constexpr int BLOCK_OPS = 2 * REC * 64;   // operands of a block
+    __shared__ u32x4 ring[2][2 * BLOCK_OPS];
+    const int nkv = a.g.nkv;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, q = lane >> 4, c = lane & 15;
+    // Workgroups of one (kv head, segment) on one die: they read the same blocks.  Tiles that no group has come last: in between, workgroups that end at once
+    // had some compute units get three of those that do not, and others one.
+    const uint32_t slot = blockIdx.x >> 3, pairs = ((uint32_t)nkv * a.prefix_share + 7) >> 3, x0 = slot / pairs, pair = (slot - x0 * pairs) * 8 + (blockIdx.x & 7);
+    int tile = (int)x0;
+    const int segment = (int)(pair / (uint32_t)nkv), kvh = (int)pair - segment * nkv;
+    if (segment >= a.prefix_share) return;
+    const Group g = group_of_tile(a, tile, 4 * RT * 16, lane);
+    if (g.n == 0) return;
+    const int each = a.n * a.gq, rows = g.n * each, row0 = (tile * 4 + wave) * RT * 16;
+    const Cut cut = prefix_cut(g.blocks, a.prefix_segments);
+    if (segment >= cut.n) return;
+    const int first = segment * cut.each, n_it = min(cut.each, g.blocks - first);
+    const bool mine = row0 < rows;
+
+    struct Ahead {
+        int record;
+        float2 scale;
+    };
+    auto look = [&](int chunk) {   // lane l: block 64 * chunk + l of the segment
+        const int i = first + min(64 * chunk + lane, n_it - 1);
+        Ahead x;
+        const int entry = kv8_entry(a.g, g.first, i);
+        const int page = min(max(entry, 0), a.g.n_pages - 1);
+        if (entry != page && kvh == 0 && tile == 0) atomicOr(a.status, KV8_RANGE);
+        x.record = page * nkv + kvh;
+        x.scale = a.scales[(uint32_t)x.record];
+        return x;
+    };
+    int chunk = 0;
+    Ahead now = look(0), next = now;
+
+    // Query operands: row c of tile t, channels 32 ks + 8 q .. + 7, times a power of two that brings the row's largest below 2^15.
+    u32x4 qq[RT][KS][PARTS];
+    float row_scale[RT];
+    const float soft = 1.4426950408889634f * rsqrtf((float)HD);   // log2(e) / sqrt(d)
+    {
+        u32x4 lo[RT][KS], hi[RT][KS];
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            const int r = min(row0 + t * 16 + c, rows - 1), of = (int)((unsigned)r / (unsigned)each);   // past the last: that one again, used by no row
+            const RowOut o(r - of * each, a.gq, kvh);
+            const char *row = a.q.at(g.first + of, o.j, o.head);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) fetch8(a.q, row, 32 * ks + 8 * q, lo[t][ks], hi[t][ks]);
+        }
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            float most = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                float v[8];
+                decode8(a.q, lo[t][ks], hi[t][ks], v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(v[i]));
+            }
+            most = rows_max(most);
+            const int e = (int)(f32_bits(most) >> 23);   // 2^(e-127) <= most < 2^(e-126)
+            const int to = e == 0 || e == 255 ? 127 : min(268 - e, 253);   // biased exponent of the factor, 2^(141-e)
+            const float f = bits_f32((uint32_t)to << 23);
+            row_scale[t] = bits_f32((uint32_t)(254 - to) << 23) * soft;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                float v[8];
+                decode8(a.q, lo[t][ks], hi[t][ks], v);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    uint32_t h, l = 0;
+                    if (PARTS == 2) split_half2(v[2 * i] * f, v[2 * i + 1] * f, h, l);
+                    else h = pack_half2(v[2 * i] * f, v[2 * i + 1] * f);
+                    qq[t][ks][0][i] = h;
+                    if (PARTS == 2) qq[t][ks][PARTS - 1][i] = l;
+                }
+            }
+        }
+    }
+
+    // The segment's largest and smallest scale of V (biased exponents).
+    int v_ref = (int)(f32_bits(now.scale.y) >> 23 & 255), v_low = v_ref;
+    for (int i = 1; i * 64 < n_it; ++i) {
+        const int e = (int)(f32_bits(look(i).scale.y) >> 23 & 255);
+        v_ref = max(v_ref, e);
+        v_low = min(v_low, e);
+    }
+#pragma unroll
+    for (int i = 32; i > 0; i >>= 1) {
+        v_ref = max(v_ref, __shfl_xor(v_ref, i));
+        v_low = min(v_low, __shfl_xor(v_low, i));
+    }
+    v_ref = __builtin_amdgcn_readfirstlane(v_ref);
+    const bool wide = __builtin_amdgcn_readfirstlane(v_ref - v_low) > V_SPAN;
+    if (n_it > 64) next = look(1);
+
+    // A wave's records of a block: K's are those below REC / 2, then V's.  Blocks go in pairs; where block i is multiplied, scores are made of block i + 1 already, so K's
+    // pairs are one block ahead of V's.
+    u32x4 raw[2][MINE];
+    auto is_v = [&](int x) { return wave + 4 * x >= REC / 2; };
+    auto request = [&](int i) {   // V's records of blocks i and i + 1, K's of i + 1 and i + 2 (behind the last: that one again)
+#pragma unroll
+        for (int two = 0; two < 2; ++two)
+#pragma unroll
+            for (int x = 0; x < MINE; ++x) {
+                const int at = min(i + two + (is_v(x) ? 0 : 1), n_it - 1);
+                const uint32_t record = (uint32_t)__builtin_amdgcn_readlane(at >> 6 == chunk ? now.record : next.record, at & 63);
+                const auto p = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(a.codes) + (size_t)record * (64 * HD), 0, 64 * HD, 0x00027000);
+                raw[two][x] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(p, lane * 16, (wave + 4 * x) * 1024, 0));
+            }
+    };
+    // Operand tiles in LDS: of a pair, K's [u][ks] and then V's [dt].
+    auto hand = [&](int i, u32x4 *to) {
+#pragma unroll
+        for (int two = 0; two < 2; ++two) {
+            const int at = min(i + two, n_it - 1);
+            const int e = __builtin_amdgcn_readlane((int)f32_bits(at >> 6 == chunk ? now.scale.y : next.scale.y), at & 63) >> 23 & 255;
+            const float v_ratio = wide ? 1.f : bits_f32((uint32_t)(e - v_ref + 127) << 23);
+#pragma unroll
+            for (int x = 0; x < MINE; ++x) {
+                const int rec = wave + 4 * x, p = is_v(x) ? rec - REC / 2 : rec % (KS / 2);
+                const float ratio = is_v(x) ? v_ratio : 1.f;
+                const u32x4 &w = raw[two][x];
+                u32x4 *tile_at = to + two * BLOCK_OPS + (is_v(x) ? REC + 2 * p : rec / (KS / 2) * KS + p) * 64 + lane;
+                tile_at[0] = __builtin_bit_cast(u32x4, codes_half8<FMT>(w[0], w[1], ratio));
+                tile_at[(is_v(x) ? 1 : KS / 2) * 64] = __builtin_bit_cast(u32x4, codes_half8<FMT>(w[2], w[3], ratio));
+            }
+        }
+    };
+
+    f32x4 o[RT][DT], l_run[RT];   // l_run: sums of probabilities, by a product with ones: the same in every register of a lane's column
+    float m_run[RT], sc[RT];
+    f32x4 s[RT][2];   // s[t][u][r]: position 16u + 4q + r of the block for query row c of tile t
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[t][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        l_run[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        m_run[t] = NONE;
+    }
+    const half8_t ones = __builtin_bit_cast(half8_t, u32x4{0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u});
+    bool huge = false;   // some row's reference has been HUGE_SCORE
+
+    auto scores = [&](const u32x4 *at, f32x4 (&to)[RT][2]) {
+#pragma unroll
+        for (int t = 0; t < RT; ++t) to[t][0] = to[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const half8_t kk = __builtin_bit_cast(half8_t, at[(u * KS + ks) * 64 + lane]);
+#pragma unroll
+                for (int part = 0; part < PARTS; ++part)
+#pragma unroll
+                    for (int t = 0; t < RT; ++t) to[t][u] = mfma16(kk, __builtin_bit_cast(half8_t, qq[t][ks][part]), to[t][u]);
+            }
+    };
+    auto lane_most = [&](int t) { return max3(max3(s[t][0][0], s[t][0][1], s[t][0][2]), max3(s[t][0][3], s[t][1][0], s[t][1][1]), max3(s[t][1][2], s[t][1][3], s[t][1][3])); };
+    // The references of the rows, for the block whose scores are in s.
+    auto refer = [&](int i) {
+        const float k_scale = bits_f32((uint32_t)__builtin_amdgcn_readlane((int)f32_bits(i >> 6 == chunk ? now.scale.x : next.scale.x), i & 63));
+        float mx[RT];   // of the lane's own eight positions
+        bool grow = huge;
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            sc[t] = __builtin_amdgcn_fmed3f(row_scale[t] * k_scale, 0x1p-126f, 0x1p127f);   // neither 0 nor infinite: times -INFINITY or 0
+            mx[t] = lane_most(t);
+            grow = grow || above(mx[t], sc[t], m_run[t]) > REF_MOST;
+        }
+        if (__any(grow)) {
+#pragma unroll
+            for (int t = 0; t < RT; ++t) {
+                const float m = rows_max(mx[t]);
+                const float m_new = above(m, sc[t], m_run[t]) > REF_MOST ? above(m, sc[t], REF_BELOW) : m_run[t], alpha = __builtin_amdgcn_exp2f(m_run[t] - m_new);
+                m_run[t] = m_new;
+                huge = huge || __any(fabsf(m_new) >= HUGE_SCORE && m_new != NONE);
+                l_run[t] *= alpha;
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) o[t][dt] *= alpha;
+            }
+            if (huge)
+#pragma unroll
+                for (int t = 0; t < RT; ++t) {
+                    const bool own = fabsf(m_run[t]) >= HUGE_SCORE;   // by the row alone: the others change none of its bits
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) s[t][u] = own ? s[t][u] * sc[t] : s[t][u];
+                    sc[t] = own ? 1.f : sc[t];
+                }
+        }
+    };
+    u32x4 pk[RT][PARTS];
+    auto weigh = [&](int t, float ref) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e >> 1][2 * (e & 1)], sc[t], -ref));
+            const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e >> 1][2 * (e & 1) + 1], sc[t], -ref));
+            uint32_t hi, lo;
+            if (PARTS == 2) {
+                split_half2(p0, p1, hi, lo);
+                pk[t][PARTS - 1][e] = lo;
+            } else {
+                hi = pack_half2(p0, p1);
+            }
+            pk[t][0][e] = hi;
+        }
+    };
+    auto times = [&](const half8_t &x, int t, f32x4 sum) {
+#pragma unroll
+        for (int part = 0; part < PARTS; ++part) sum = mfma16(x, __builtin_bit_cast(half8_t, pk[t][part]), sum);
+        return sum;
+    };
+    auto value = [&](const u32x4 *at, int dt) { return __builtin_bit_cast(half8_t, at[(REC + dt) * 64 + lane]); };
+    // Block i, whose scores are in s, times its values; the scores of block i + 1 instead.  at: the operands.  One tile's probabilities are made while
+    // another's are multiplied.
+    auto attend = [&](int i, const u32x4 *at) {
+        f32x4 ahead[RT][2];
+        half8_t vv[DT];
+        weigh(0, m_run[0]);
+        scores(at, ahead);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) vv[dt] = value(at, dt);
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            if (t + 1 < RT) weigh(t + 1, m_run[t + 1]);
+            l_run[t] = times(ones, t, l_run[t]);
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) o[t][dt] = times(vv[dt], t, o[t][dt]);
+        }
+#pragma unroll
+        for (int t = 0; t < RT; ++t) s[t][0] = ahead[t][0], s[t][1] = ahead[t][1];
+        if (i + 1 < n_it) refer(i + 1);
+    };
+    auto attend_wide = [&](int i, const u32x4 *at) {
+        const f32x4 zero = f32x4{0.f, 0.f, 0.f, 0.f};
+        const int e = __builtin_amdgcn_readlane((int)f32_bits(now.scale.y), i & 63) >> 23 & 255;
+        const float down = bits_f32((uint32_t)max(e - v_ref + 127, 0) << 23);
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            const float ref = fmaxf(above(rows_max(lane_most(t)), sc[t], REF_BELOW), m_run[t] - REF_FAR);
+            weigh(t, ref);
+            float back = __builtin_amdgcn_exp2f(ref - m_run[t]);   // from the block's reference and scale to the row's reference and the unit
+            l_run[t] += times(ones, t, zero) * back;
+            back *= down;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+                o[t][dt] += times(value(at, dt), t, zero) * back;
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        scores(at, s);
+        if (i + 1 < n_it) refer(i + 1);
+    };
+
+    request(-1);   // K of block 0 (and what is not used)
+    hand(-1, ring[1]);
+    request(0);
+    __syncthreads();
+    if (mine) {
+        scores(ring[1], s);
+        refer(0);
+    }
+    hand(0, ring[0]);
+    request(2);
+    auto all = [&](auto step) {
+        for (int i = 0; i < n_it; i += 2) {
+            if (i >> 6 != chunk) {
+                chunk = i >> 6;
+                now = next;
+                next = look(chunk + 1);
+            }
+            const int half = i >> 1 & 1;
+            __syncthreads();   // the operands of this turn are there, those of the one before have been read
+            __builtin_amdgcn_sched_barrier(0);
+            hand(i + 2, ring[half ^ 1]);
+            request(i + 4);
+            if (!mine) continue;
+            step(i, ring[half]);
+            if (i + 1 < n_it) step(i + 1, ring[half] + BLOCK_OPS);
+        }
+    };
+    if (__builtin_expect(wide, false)) all(attend_wide);
+    else all(attend);
+
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        const int row = row0 + t * 16 + c;
+        if (row >= rows) continue;
+        const size_t at = shared_slot(a, segment, kvh, g.first * each + row);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4 *>(a.part_o + at * HD + dt * 16 + 4 * q) = o[t][dt];
+        if (q == 0) a.part_ml[at] = f32x4{m_run[t], l_run[t][0], (float)v_ref, 0.f};
+    }
+}
 
 // A wave per row of the batch.
 template <int HD> __global__ __launch_bounds__(256) void kv8_shared_merge_kernel(Kv8SharedArgs a)
@@ -95,13 +404,24 @@ template <int HD, int FMT, int PARTS> hipError_t launch_shared(const Kv8SharedAr
     if (a.groups > 0) {
         const uint32_t pairs = (uint32_t)a.g.nkv * a.prefix_share;
         const dim3 grid((pairs + 7) / 8 * 8 * a.tiles);
-#define KV8_PRE(RT) hipLaunchKernelGGL((kv8_attn_kernel<HD, FMT, RT, PARTS, 4, KV8_PREFIX>), grid, dim3(256), 0, s, a)
-        switch (rt_prefix) {
-        case 1: KV8_PRE(1); break;
-        case 2: KV8_PRE(2); break;
-        default: KV8_PRE(3); break;
+#define KV8_FEW(RT) hipLaunchKernelGGL((kv8_attn_kernel<HD, FMT, RT, PARTS, 4, KV8_PREFIX>), grid, dim3(256), 0, s, a)
+#define KV8_MANY(RT) hipLaunchKernelGGL((kv8_prefix_kernel<HD, FMT, RT, PARTS>), grid, dim3(256), 0, s, a)
+        if (a.wave_rows == 4) {
+            switch (rt_prefix) {
+            case 1: KV8_MANY(1); break;
+            case 2: KV8_MANY(2); break;
+            case 3: KV8_MANY(3); break;
+            default: KV8_MANY(4); break;
+            }
+        } else {
+            switch (rt_prefix) {
+            case 1: KV8_FEW(1); break;
+            case 2: KV8_FEW(2); break;
+            default: KV8_FEW(3); break;
+            }
         }
-#undef KV8_PRE
+#undef KV8_FEW
+#undef KV8_MANY
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -126,17 +446,29 @@ template <int HD> hipError_t launch_format(const Kv8SharedArgs &a, int fmt, int 
 
 }  // namespace
 
-Kv8SharedPlan kv8_shared_plan(int B, int n, int gq, int nkv, int groups)
+Kv8SharedPlan kv8_shared_plan(int B, int n, int gq, int nkv, int groups, bool f32)
 {
     Kv8SharedPlan p{};
     const int64_t rows = (int64_t)B * n * gq, each = groups > 0 ? (rows + groups - 1) / groups : rows;   // rows of a group, if they are all alike
-    const int tiles = (int)((each + 15) / 16);
-    p.rt = tiles < KV8_MAX_TILES ? tiles : KV8_MAX_TILES;
-    p.wave_rows = tiles <= p.rt ? 1 : tiles <= 2 * p.rt ? 2 : 4;
+    const int64_t tiles = (each + 15) / 16;
+    if (tiles <= KV8_MAX_TILES) {
+        p.rt = (int)tiles;
+        p.wave_rows = 1;
+    } else {   // as few row tiles as can be that are nobody's
+        p.wave_rows = 4;
+        int64_t best = INT64_MAX;
+        for (int rt = 4; rt >= 1; --rt) {
+            const int64_t cost = (tiles + 4 * rt - 1) / (4 * rt) * (rt + 1);
+            if (cost < best) {
+                best = cost;
+                p.rt = rt;
+            }
+        }
+    }
     const int64_t per = p.wave_rows * p.rt * 16;
-    p.tiles = (int)(rows / per + groups);
+    p.tiles = (int)((rows + per - 1) / per + std::max(groups, 1) - 1);
     const int64_t units = (each + per - 1) / per * (groups > 0 ? groups : 1) * nkv;
-    const int64_t share = KV8_GROUPS / units;
+    const int64_t share = (p.wave_rows == 4 && p.rt * (f32 ? 2 : 1) > 2 ? 256 : KV8_GROUPS) / units;
     p.share = share < 1 ? 1 : share > 64 ? 64 : (int)share;
     p.segments = p.share * 4 / p.wave_rows;
     return p;
@@ -186,7 +518,7 @@ int sssd_kv8_attention_shared(const sssd_kv8 *kv, int32_t layer, int32_t B, int3
     a.plan = kv8_plan(B, n, a.gq, c.n_kv_heads, S.blocks_per_seq, !a.q.bf16);
     const int tiles = (n * a.gq + 15) / 16;
     a.rows_pad = tiles * 16;
-    const Kv8SharedPlan p = kv8_shared_plan(B, n, a.gq, c.n_kv_heads, groups);
+    const Kv8SharedPlan p = kv8_shared_plan(B, n, a.gq, c.n_kv_heads, groups, !a.q.bf16);
     a.groups = groups; a.starts = starts; a.shared = shared;
     a.tiles = p.tiles; a.wave_rows = p.wave_rows; a.prefix_share = p.share; a.prefix_segments = p.segments;
     a.rows_all = B * n * a.gq;

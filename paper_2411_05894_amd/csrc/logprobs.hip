@@ -4,23 +4,25 @@
 //   log p_i = x_i - log(1 + s),   H = log(1 + s) - t / (1 + s)
 // so that what is nearly certain keeps its digits: log p of the likeliest token is -log1p(s), however small s is.
 //
-// Split.  A row is cut into tiles that a workgroup holds in registers: every logit is loaded once, all loads of a thread at once, and the maximum is known before
-// anything is summed.  A tile leaves (M, s, t), how many of its logits come before each given token, and its own most probable tokens in order; a wave per row joins
-// the tiles.  Sums are taken over tiles in a fixed order.
+// Split.  A workgroup goes over a row, or a part of one where there are few rows, a chunk of 1024 16-byte loads at a time, the next one under way; its waves know nothing of each other until
+// the end.  A wave keeps the largest logit M so far and how many there were of it, per lane s and t of the others relative to a logit r near M (so that hardly any chunk
+// changes it), how many come before each given token, and a list of its most probable tokens: what is above the last of n in a list that was full, at first above the n-th largest of its lanes'
+// largest logits.  Parts leave all that in memory, and a second launch joins them.  The order of sums is fixed.
 //
-// The most probable tokens of a tile: the n-th largest of the threads' own largest logits, or less (the smallest over waves of the ceil(n / waves)-th largest of a wave's),
-// bounds them from below: what is at or above it is listed, and its place counted against the rest of the list.  Where the list would overflow (equal logits), they are
-// taken out one by one.
+// What bounds it: reading the logits, and nearly as much nine instructions a logit, an exponential among them.
 #include "../../include/sssd_ops.h"
 #include "common.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace {
 
-constexpr int LT = 512, LWAVES = LT / 64;   // threads of a tile's workgroup
-constexpr int LIST = 1024;                  // tokens listed at most
+constexpr int LT = 256, LWAVES = LT / 64;   // threads of a workgroup
+constexpr int LIST = 192;                   // a wave's list of tokens: two rounds of its lanes behind a list that has been cut
 constexpr int MOST_TOKENS = SSSD_LOGPROBS_MAX_TOKENS, MOST_TOP = SSSD_LOGPROBS_MAX_TOP;
+static_assert(LIST >= MOST_TOP + 64);
+constexpr float FAR = 4.f;                  // octaves of probability that M may be away from r
 
 // Order of tokens: larger logit first, then the lower id; what is no number counts as -infinity.  As one word, larger first: keys of logits ascend with
 // them (-0 is 0), ids are inverted.
@@ -30,34 +32,47 @@ __device__ __forceinline__ uint32_t logit_key(float z)
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 __device__ __forceinline__ float key_logit(uint32_t k) { return bits_f32(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k); }
+__device__ __forceinline__ float next_below(float z)   // a finite or infinite one above the lowest; the same for both zeros
+{
+    const int u = (int)f32_bits(z + 0.f);
+    return bits_f32((uint32_t)(u == 0 ? (int)0x80000001u : u > 0 ? u - 1 : u + 1));
+}
 __device__ __forceinline__ float ordered(float z) { return fmaxf(z, -INFINITY); }
 __device__ __forceinline__ uint64_t token_key(float z, int id) { return (uint64_t)logit_key(ordered(z)) << 32 | (uint32_t)~id; }
 
 struct LogArgs {
     const char *logits;
     int64_t stride;      // elements
-    int rows, vocab, tile, tiles, n_tokens, n_top;
+    int rows, vocab, part, parts, n_tokens, n_top;   // part: logits of a part
     float k, inv_t;      // log2(e) / T, 1 / T
     const int32_t *tokens;
     float *logprobs, *entropy, *top_logprobs;
     int32_t *ranks, *top_ids;
-    f32x4 *stats;        // [row][tile] M, s, t, -
-    int32_t *before;     // [row][tile][token]
-    uint64_t *best;      // [row][tile][top]
+    f32x4 *stats;        // [row][part] M, s, t, -
+    int32_t *before;     // [row][part][token]
+    uint64_t *best;      // [row][part][top]
 };
 
-// Sum, largest of a workgroup; red: LWAVES words.
+// Over a wave, the same in every lane: neighbours, then eights, sixteens and halves of the wave.
+template <typename F> __device__ __forceinline__ float wave_all(float x, F f)
+{
+    auto dpp = [&](auto ctrl) { return bits_f32((uint32_t)__builtin_amdgcn_mov_dpp((int)f32_bits(x), decltype(ctrl)::value, 0xF, 0xF, true)); };
+    x = f(x, dpp(std::integral_constant<int, 0xB1>()));    // lane ^ 1
+    x = f(x, dpp(std::integral_constant<int, 0x4E>()));    // lane ^ 2
+    x = f(x, dpp(std::integral_constant<int, 0x141>()));   // mirrored within eight
+    x = f(x, dpp(std::integral_constant<int, 0x140>()));   // ... within sixteen
+    auto h = __builtin_amdgcn_permlane16_swap(f32_bits(x), f32_bits(x), false, false);
+    x = f(bits_f32(h[0]), bits_f32(h[1]));
+    h = __builtin_amdgcn_permlane32_swap(f32_bits(x), f32_bits(x), false, false);
+    return f(bits_f32(h[0]), bits_f32(h[1]));
+}
 __device__ __forceinline__ float wave_max(float x)
 {
-#pragma unroll
-    for (int i = 32; i > 0; i >>= 1) x = fmaxf(x, __shfl_xor(x, i));
-    return x;
+    return wave_all(x, [](float a, float b) { return fmaxf(a, b); });
 }
 __device__ __forceinline__ float wave_add(float x)
 {
-#pragma unroll
-    for (int i = 32; i > 0; i >>= 1) x += __shfl_xor(x, i);
-    return x;
+    return wave_all(x, [](float a, float b) { return a + b; });
 }
 __device__ __forceinline__ uint64_t wave_max64(uint64_t x)
 {
@@ -69,171 +84,17 @@ __device__ __forceinline__ uint64_t wave_max64(uint64_t x)
     return x;
 }
 
-// V: 16-byte loads of a thread; a tile is at most LT * V * 16 bytes of logits.  grid: tiles of a row next to each other
-template <int V, bool BF16> __global__ __launch_bounds__(LT) void logprob_tile_kernel(LogArgs a)
+// How many lanes.
+__device__ __forceinline__ int lanes_of(bool x) { return (int)__popcll(__ballot(x)); }
+
+// What lanes of a wave stored in LDS is there for the others.
+__device__ __forceinline__ void wave_sync()
 {
-    constexpr int PER = BF16 ? 8 : 4, SIZE = BF16 ? 2 : 4, N = V * PER + 1;   // logits of a load; of a thread: one of the ends besides
-    __shared__ float red_s[LWAVES], sum_s[LWAVES], turn_s[LWAVES];
-    __shared__ uint32_t bound_s[LWAVES], listed_s;
-    __shared__ uint64_t list_s[LIST];
-    __shared__ int count_s[LWAVES];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint32_t row_of = blockIdx.x / (uint32_t)a.tiles;
-    const int tile = (int)(blockIdx.x - row_of * a.tiles);
-    const int64_t row = row_of;
-    const int lo = tile * a.tile, hi = min(a.vocab, lo + a.tile);
-    const char *base = a.logits + row * a.stride * SIZE;
-    // ids lo .. lo+head-1 and those behind the last whole 16 bytes: one a thread
-    const int head = min((int)((16 - (uintptr_t)(base + (int64_t)lo * SIZE) % 16) % 16 / SIZE), hi - lo);
-    const int vecs = (hi - lo - head) / PER, rest = lo + head + vecs * PER, ends = head + hi - rest;
-    const u32x4 *at = reinterpret_cast<const u32x4 *>(base + (int64_t)(lo + head) * SIZE);
-    u32x4 raw[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-        if (i * LT + (int)threadIdx.x < vecs) raw[i] = at[i * LT + threadIdx.x];
-    auto load = [&](int id) { return BF16 ? bf16_to_f32(reinterpret_cast<const uint16_t *>(base)[id]) : reinterpret_cast<const float *>(base)[id]; };
-    const int end_id = (int)threadIdx.x < head ? lo + (int)threadIdx.x : rest + (int)threadIdx.x - head;
-    float z[N];
-    z[N - 1] = (int)threadIdx.x < ends ? load(end_id) : -INFINITY;
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const bool on = i * LT + (int)threadIdx.x < vecs;
-#pragma unroll
-        for (int e = 0; e < PER; ++e)
-            z[i * PER + e] = !on ? -INFINITY : BF16 ? bits_f32(e & 1 ? raw[i][e / 2] & 0xFFFF0000u : raw[i][e / 2] << 16) : bits_f32(raw[i][e % 4]);
-    }
-    auto id_of = [&](int i) { return i == N - 1 ? end_id : lo + head + ((i / PER) * LT + (int)threadIdx.x) * PER + i % PER; };
-    auto live = [&](int i) { return i == N - 1 ? (int)threadIdx.x < ends : (i / PER) * LT + (int)threadIdx.x < vecs; };
-
-    float top = -INFINITY;   // not counting what is no number
-#pragma unroll
-    for (int i = 0; i < N; ++i) top = fmaxf(top, z[i]);
-    const float wave_top = wave_max(top);
-    if (lane == 0) red_s[wave] = wave_top;
-    if (threadIdx.x == 0) listed_s = 0;
-    __syncthreads();
-    float most = red_s[0];
-#pragma unroll
-    for (int w = 1; w < LWAVES; ++w) most = fmaxf(most, red_s[w]);
-
-    // The thread that holds the first of the largest leaves it out of its sum.
-    uint64_t holders = __ballot(top == most);
-    int first_wave = 0;
-#pragma unroll
-    for (int w = LWAVES - 1; w >= 0; --w) first_wave = red_s[w] == most ? w : first_wave;
-    bool skip = wave == first_wave && lane == __ffsll((long long)holders) - 1;
-    const float ref = most == -INFINITY ? 0.f : most;   // a tile of nothing: sums of 0
-    float s = 0.f, t = 0.f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const float x = (z[i] - ref) * a.k, e = __builtin_amdgcn_exp2f(x);
-        t = __builtin_fmaf(e, fmaxf(x, -16384.f), t);   // 0 * -infinity is 0 here
-        const bool out = skip && z[i] == most;
-        s += out ? 0.f : e;
-        skip = skip && !out;
-    }
-    s = wave_add(s);
-    t = wave_add(t);
-    if (lane == 0) {
-        sum_s[wave] = s;
-        turn_s[wave] = t;
-    }
-    const int64_t slot = row * a.tiles + tile;
-    // ranks
-    for (int j = 0; j < a.n_tokens; ++j) {
-        const int token = a.tokens[row * a.n_tokens + j];
-        int n = 0;
-        if (token >= 0 && token < a.vocab) {
-            const float v = ordered(load(token));
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const float o = ordered(z[i]);
-                n += live(i) && (o > v || (o == v && id_of(i) < token)) ? 1 : 0;
-            }
-        }
-#pragma unroll
-        for (int i = 32; i > 0; i >>= 1) n += __shfl_xor(n, i);
-        __syncthreads();   // the counts before have been read
-        if (lane == 0) count_s[wave] = n;
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            n = 0;
-#pragma unroll
-            for (int w = 0; w < LWAVES; ++w) n += count_s[w];
-            a.before[slot * a.n_tokens + j] = n;
-        }
-    }
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        s = t = 0.f;
-#pragma unroll
-        for (int w = 0; w < LWAVES; ++w) {
-            s += sum_s[w];
-            t += turn_s[w];
-        }
-        a.stats[slot] = f32x4{most, s, t, 0.f};
-    }
-    const int n_top = min(a.n_top, hi - lo);
-    if (a.n_top == 0) return;
-    uint64_t *best = a.best + slot * a.n_top;
-    if ((int)threadIdx.x >= n_top && (int)threadIdx.x < a.n_top) best[threadIdx.x] = 0;   // behind every token's
-
-    // a bound: the nth-largest of a wave's lanes, the smallest of the waves all of whose lanes have logits
-    const int whole = max(min(vecs >> 6, LWAVES), 1), nth = (n_top + whole - 1) / whole;
-    {
-        float left = top, bound = top;
-        for (int i = 0; i < nth; ++i) {
-            bound = wave_max(left);
-            const uint64_t has = __ballot(left == bound);
-            if (lane == __ffsll((long long)has) - 1) left = -INFINITY;
-        }
-        if (lane == 0) bound_s[wave] = logit_key(bound);
-    }
-    __syncthreads();
-    uint32_t bound_k = bound_s[0];
-#pragma unroll
-    for (int w = 1; w < LWAVES; ++w) bound_k = w < whole ? min(bound_k, bound_s[w]) : bound_k;
-    const float bound = key_logit(bound_k);
-    if (top >= bound)
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const float o = ordered(z[i]);
-            if (live(i) && o >= bound) {
-                const uint32_t k = atomicAdd(&listed_s, 1u);
-                if (k < LIST) list_s[k] = token_key(o, id_of(i));
-            }
-        }
-    __syncthreads();
-    const int listed = (int)listed_s;
-    if (listed <= LIST) {
-        for (int i = threadIdx.x; i < listed; i += LT) {
-            const uint64_t mine = list_s[i];
-            int place = 0;
-            for (int j = 0; j < listed; ++j) place += list_s[j] > mine;
-            if (place < n_top) best[place] = mine;
-        }
-        return;
-    }
-    uint64_t below = ~0ull;   // taken so far
-    for (int k = 0; k < n_top; ++k) {
-        uint64_t mine = 0;
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const uint64_t key = live(i) ? token_key(z[i], id_of(i)) : 0;
-            mine = key < below && key > mine ? key : mine;
-        }
-        mine = wave_max64(mine);
-        __syncthreads();
-        if (lane == 0) list_s[wave] = mine;
-        __syncthreads();
-        below = list_s[0];
-#pragma unroll
-        for (int w = 1; w < LWAVES; ++w) below = list_s[w] > below ? list_s[w] : below;
-        if (threadIdx.x == 0) best[k] = below;
-    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
 }
 
-// (M, s, t) of two parts; k: log2(e) / T.  t is in units of log2.
+// (M, s, t): the largest logit, and the sums of the others relative to it, t in units of log2.
 struct Part {
     float m, s, t;
 };
@@ -246,21 +107,307 @@ __device__ __forceinline__ Part join(const Part &a, const Part &b, float k)
     return Part{x.m, __builtin_fmaf(w, n, x.s), x.t + w * __builtin_fmaf(n, fmaxf(d, -16384.f), y.t)};
 }
 
+struct Row {   // what comes out of one
+    const LogArgs &a;
+    int64_t row;
+    float m, log_s;
+    __device__ __forceinline__ Row(const LogArgs &a, int64_t row, const Part &p, bool writes) : a(a), row(row), m(p.m)
+    {
+        const bool none = !(fabsf(p.m) < INFINITY);   // no finite logit, or an infinite one: no distribution
+        log_s = none ? NAN : log1pf(p.s);
+        if (writes && a.entropy) a.entropy[row] = log_s - p.t * 0.69314718056f / (1.f + p.s);
+    }
+    __device__ __forceinline__ float logprob(float z) const { return (z - m) * a.inv_t - log_s; }
+    __device__ __forceinline__ void token(int j, bool there, float z, int before) const
+    {
+        a.logprobs[row * a.n_tokens + j] = there ? logprob(z) : -INFINITY;
+        if (a.ranks) a.ranks[row * a.n_tokens + j] = there ? before : -1;
+    }
+    __device__ __forceinline__ void top(int k, uint64_t key) const
+    {
+        a.top_ids[row * a.n_top + k] = (int)~(uint32_t)key;
+        a.top_logprobs[row * a.n_top + k] = logprob(key_logit((uint32_t)(key >> 32)));
+    }
+};
+
+// WHOLE: a workgroup has a whole row.  grid: parts of a row next to each other
+template <bool BF16, bool WHOLE> __global__ __launch_bounds__(LT) __attribute__((amdgpu_waves_per_eu(6))) void logprob_kernel(LogArgs a)
+{
+    constexpr int V = BF16 ? 2 : 4, PER = BF16 ? 8 : 4, SIZE = BF16 ? 2 : 4;   // 16-byte loads of a thread and chunk, logits of a load
+    __shared__ float token_z_s[MOST_TOKENS];
+    __shared__ int token_s[MOST_TOKENS], before_s[LWAVES][MOST_TOKENS], listed_s[LWAVES];
+    __shared__ Part part_s[LWAVES];
+    __shared__ uint64_t list_s[LWAVES][LIST];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t row_of = WHOLE ? blockIdx.x : blockIdx.x / (uint32_t)a.parts;
+    const int part = WHOLE ? 0 : (int)(blockIdx.x - row_of * a.parts);
+    const int64_t row = row_of;
+    const int lo = part * a.part, hi = min(a.vocab, lo + a.part);
+    const char *base = a.logits + row * a.stride * SIZE;
+    auto load = [&](int id) { return BF16 ? bf16_to_f32(reinterpret_cast<const uint16_t *>(base)[id]) : reinterpret_cast<const float *>(base)[id]; };
+    // ids lo .. lo+head-1 and those behind the last whole 16 bytes: one a thread
+    const int head = min((int)((16 - (uintptr_t)(base + (int64_t)lo * SIZE) % 16) % 16 / SIZE), hi - lo);
+    const int vecs = (hi - lo - head) / PER, rest = lo + head + vecs * PER, ends = head + hi - rest;
+    const u32x4 *from = reinterpret_cast<const u32x4 *>(base + (int64_t)(lo + head) * SIZE);
+    const uint32_t empty = BF16 ? 0xFF80FF80u : 0xFF800000u;   // -infinity
+    u32x4 raw[V];
+    auto request = [&](int first) {   // vectors from there on
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            raw[i] = u32x4{empty, empty, empty, empty};
+            if (first + i * LT + (int)threadIdx.x < vecs) raw[i] = from[first + i * LT + threadIdx.x];
+        }
+    };
+    request(0);
+    const int end_id = (int)threadIdx.x < head ? lo + (int)threadIdx.x : rest + (int)threadIdx.x - head;
+    const float z_end = (int)threadIdx.x < ends ? load(end_id) : -INFINITY;
+    if ((int)threadIdx.x < a.n_tokens) {
+        const int token = a.tokens[row * a.n_tokens + threadIdx.x];
+        const bool there = token >= 0 && token < a.vocab;
+        token_s[threadIdx.x] = there ? token : -1;
+        token_z_s[threadIdx.x] = there ? load(token) : INFINITY;
+    }
+    for (int j = lane; j < a.n_tokens; j += 64) before_s[wave][j] = 0;
+    __syncthreads();
+    const int n_tokens = a.ranks ? a.n_tokens : 0, n_top = min(a.n_top, hi - lo);
+    const int token0 = n_tokens > 0 ? token_s[0] : 0;
+    const float v0 = n_tokens > 0 ? ordered(token_z_s[0]) : INFINITY, below0 = next_below(v0);
+
+    float most = -INFINITY, ref = 0.f, s = 0.f, t = 0.f;   // most: the wave's largest so far; s, t: the lane's
+    int equal = 0, before0 = 0, listed = 0;
+    float least = -INFINITY;    // what is below it is not among the wave's n_top
+    uint64_t least_key = 0;
+    uint64_t *list = list_s[wave];
+
+    // The list's n_top first, in order.
+    auto cut = [&]() {
+        wave_sync();
+        uint64_t mine[LIST / 64];
+        int place[LIST / 64];
+        auto places = [&](auto rounds) {
+            constexpr int E = decltype(rounds)::value;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                mine[e] = lane + 64 * e < listed ? list[lane + 64 * e] : 0;
+                place[e] = 0;
+            }
+            for (int j = 0; j < listed; ++j) {
+                const uint64_t other = list[j];
+#pragma unroll
+                for (int e = 0; e < E; ++e) place[e] += other > mine[e];
+            }
+            wave_sync();
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (mine[e] && place[e] < n_top) list[place[e]] = mine[e];
+        };
+        if (listed <= 64) places(std::integral_constant<int, 1>());
+        else places(std::integral_constant<int, LIST / 64>());
+        wave_sync();
+        if (listed >= n_top) {
+            listed = n_top;
+            least_key = list[n_top - 1];
+            least = key_logit((uint32_t)(least_key >> 32));
+        }
+    };
+    // N logits a lane, z[i] of token first + i / PER * LT * PER + i % PER while that is below `end`: the others are -infinity.
+    auto chunk = [&](auto n_of, const auto &z, int first, int end) {
+        constexpr int N = decltype(n_of)::value, G = N == 1 ? 1 : PER;
+        float top = z[0];
+#pragma unroll
+        for (int i = 1; i + 1 < N; i += 2) top = __builtin_elementwise_maximum(__builtin_elementwise_maximum(z[i], z[i + 1]), top);
+        if (N % 2 == 0) top = __builtin_elementwise_maximum(top, z[N - 1]);
+        if (__any(top != top)) {   // not counting what is no number
+            top = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < N; ++i) top = fmaxf(top, z[i]);
+        }
+        const float here = bits_f32((uint32_t)__builtin_amdgcn_readfirstlane((int)f32_bits(wave_max(top))));
+        if (here > most) {
+            if (equal) {   // those that were the largest join the others
+                const float x = (most - ref) * a.k, e = __builtin_amdgcn_exp2f(x) * (float)equal;
+                s += lane == 0 ? e : 0.f;
+                t += lane == 0 ? e * x : 0.f;
+            }
+            const float d = (ref - here) * a.k;
+            if (!equal || !(d >= -FAR)) {
+                const float f = __builtin_amdgcn_exp2f(d);
+                if (equal) {
+                    t = __builtin_fmaf(fmaxf(d, -16384.f), s, t) * f;
+                    s *= f;
+                }
+                ref = here;
+            }
+            most = here;
+            equal = 0;
+        }
+        auto sums = [&](auto holding, auto counting) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float x = (z[i] - ref) * a.k;
+                float e = __builtin_amdgcn_exp2f(x);
+                if (decltype(holding)::value) {
+                    const bool is = z[i] == most;
+                    e = is ? 0.f : e;
+                    equal += lanes_of(is);
+                }
+                t = __builtin_fmaf(e, fmaxf(x, -16384.f), t);   // 0 * -infinity is 0 here
+                s += e;
+                if (decltype(counting)::value) before0 += lanes_of(z[i] > (first + i / PER * LT * PER + G <= token0 ? below0 : v0));
+            }
+        };
+        const bool counts = here >= v0 && v0 > -INFINITY;
+        if (here == most && most > -INFINITY) {
+            if (counts) sums(std::true_type(), std::true_type());
+            else sums(std::true_type(), std::false_type());
+        } else {
+            if (counts) sums(std::false_type(), std::true_type());
+            else sums(std::false_type(), std::false_type());
+        }
+        // Tokens that come before the given ones: larger logits, and of equal ones those of lower ids -- what is larger than the next number below.
+        auto id_of = [&](int i) { return first + i / PER * LT * PER + i % PER; };
+        for (int j = 0; j < n_tokens; ++j) {
+            const int token = token_s[j];
+            const float v = ordered(token_z_s[j]);
+            int n = 0;
+            if (v == -INFINITY) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const float o = ordered(z[i]);
+                    n += lanes_of(id_of(i) < end && (o > v || id_of(i) < token));
+                }
+            } else if (here >= v) {
+                if (j > 0) {
+                    const float below = next_below(v);
+#pragma unroll
+                    for (int i = 0; i < N; ++i) n += lanes_of(z[i] > (first + i / PER * LT * PER + G <= token ? below : v));
+                }
+                const int off = token - first;
+                bool has = false;   // the token is one of those of a load of the lane's, and not the first of them
+#pragma unroll
+                for (int l = 0; l < N / PER; ++l) has = has || (off > l * LT * PER && off < l * LT * PER + PER);
+                if (__any(has))
+#pragma unroll
+                    for (int i = 0; i < N; ++i) {
+                        const int within = off - i / PER * LT * PER;
+                        n += lanes_of(within > i % PER && within < PER && z[i] == v);
+                    }
+            }
+            if (n && lane == 0) before_s[wave][j] += n;
+        }
+        if (n_top == 0) return;
+        if (least == -INFINITY) {   // the wave's first logits
+            const int lanes = lanes_of(top > -INFINITY);
+            if (lanes >= n_top) {
+                float left = top;
+                for (int i = 0; i < n_top; ++i) {
+                    least = wave_max(left);
+                    const uint64_t has = __ballot(left == least);
+                    if (lane == __ffsll((long long)has) - 1) left = -INFINITY;
+                }
+            }
+        }
+        if (here >= least)
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                if (!__any(z[i] >= least || least == -INFINITY)) continue;
+                const uint64_t key = token_key(z[i], id_of(i));
+                bool take = ordered(z[i]) >= least && id_of(i) < end && key > least_key;
+                uint64_t who = __ballot(take);
+                if (listed + (int)__popcll(who) > LIST) {
+                    cut();
+                    take = take && key > least_key;
+                    who = __ballot(take);
+                }
+                if (take) list[listed + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0))] = key;
+                listed += (int)__popcll(who);
+            }
+        if (listed > n_top / 2 + 48) cut();   // so that the next chunks have fewer to list
+    };
+    {
+        // the ends are chunks of one logit a lane: before and behind the others
+        const float z[1] = {z_end};
+        if (ends > 0 && wave == 0) chunk(std::integral_constant<int, 1>(), z, end_id, (int)threadIdx.x < ends ? end_id + 1 : end_id);
+    }
+    for (int at = 0; at < vecs; at += V * LT) {
+        float z[V * PER];
+#pragma unroll
+        for (int i = 0; i < V * PER; ++i) {
+            const uint32_t w = BF16 ? raw[i / PER][i % PER / 2] : raw[i / PER][i % PER];
+            z[i] = bits_f32(!BF16 ? w : i & 1 ? w & 0xFFFF0000u : w << 16);
+        }
+        request(at + V * LT);
+        chunk(std::integral_constant<int, V * PER>(), z, lo + head + (at + (int)threadIdx.x) * PER, rest);
+    }
+    if (n_top > 0) cut();
+    // relative to the wave's largest
+    const float x = (most - ref) * a.k, f = equal ? __builtin_amdgcn_exp2f(-x) : 1.f;
+    t = wave_add(t);
+    s = wave_add(s);
+    if (equal) {
+        t = __builtin_fmaf(-x, s, t) * f;
+        s = __builtin_fmaf(s, f, (float)(equal - 1));
+    }
+    if (lane == 0) {
+        part_s[wave] = Part{most, s, t};
+        listed_s[wave] = listed;
+        if (n_tokens > 0) before_s[wave][0] += before0;
+    }
+    __syncthreads();
+    Part p = part_s[0];
+#pragma unroll
+    for (int w = 1; w < LWAVES; ++w) p = join(p, part_s[w], a.k);
+    const int64_t slot = row * a.parts + part;
+    const Row r(a, row, WHOLE ? p : Part{0.f, 0.f, 0.f}, WHOLE && threadIdx.x == 0);
+    if (!WHOLE && threadIdx.x == 0) a.stats[slot] = f32x4{p.m, p.s, p.t, 0.f};
+    if ((int)threadIdx.x < a.n_tokens) {
+        int n = 0;
+#pragma unroll
+        for (int w = 0; w < LWAVES; ++w) n += before_s[w][threadIdx.x];
+        if (WHOLE) r.token(threadIdx.x, token_s[threadIdx.x] >= 0, token_z_s[threadIdx.x], n);
+        else a.before[slot * a.n_tokens + threadIdx.x] = n;
+    }
+    // a token's place among the waves' lists, which are in order
+    uint64_t *best = a.best + slot * a.n_top;
+    int all = 0;
+#pragma unroll
+    for (int w = 0; w < LWAVES; ++w) all += listed_s[w];
+    for (int i = lane; i < listed; i += 64) {
+        const uint64_t mine = list[i];
+        int place = i;
+#pragma unroll
+        for (int w = 0; w < LWAVES; ++w)
+            if (w != wave)
+                for (int j = 0; j < listed_s[w] && place < n_top; ++j) place += list_s[w][j] > mine;
+        if (place >= n_top) continue;
+        if (WHOLE) r.top(place, mine);
+        else best[place] = mine;
+    }
+    if (!WHOLE)
+        for (int i = threadIdx.x; i < a.n_top; i += LT)
+            if (i >= all) best[i] = 0;   // behind every token's
+}
+
 constexpr int JT = 256, JLIST = 1024;   // threads of a row's workgroup, tokens listed at most
 
+// The parts of a row.
 template <bool BF16> __global__ __launch_bounds__(JT) void logprob_join_kernel(LogArgs a)
 {
-    __shared__ float all_s[2];   // M, log(1 + s)
+    __shared__ Part part_s;
     __shared__ uint64_t list_s[JLIST], bound_s;
     __shared__ uint32_t listed_s;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t row = blockIdx.x, slot = row * a.tiles;
+    const int64_t row = blockIdx.x, slot = row * a.parts;
     const char *base = a.logits + row * a.stride * (BF16 ? 2 : 4);
     auto load = [&](int id) { return BF16 ? bf16_to_f32(reinterpret_cast<const uint16_t *>(base)[id]) : reinterpret_cast<const float *>(base)[id]; };
     const uint64_t *best = a.best + slot * a.n_top;
+    // a given token's logit, requested ahead of everything
+    const int token = (int)threadIdx.x < a.n_tokens ? a.tokens[row * a.n_tokens + threadIdx.x] : -1;
+    const bool there = token >= 0 && token < a.vocab;
+    const float token_z = there ? load(token) : 0.f;
     if (wave == 0) {
         Part p{-INFINITY, 0.f, 0.f};
-        for (int i = lane; i < a.tiles; i += 64) {
+        for (int i = lane; i < a.parts; i += 64) {
             const f32x4 x = a.stats[slot + i];
             p = join(p, Part{x[0], x[1], x[2]}, a.k);
         }
@@ -269,18 +416,12 @@ template <bool BF16> __global__ __launch_bounds__(JT) void logprob_join_kernel(L
             const Part o{__shfl_xor(p.m, i), __shfl_xor(p.s, i), __shfl_xor(p.t, i)};
             p = lane & i ? join(o, p, a.k) : join(p, o, a.k);
         }
-        const bool none = !(fabsf(p.m) < INFINITY);   // no finite logit, or an infinite one: no distribution
-        const float log_s = none ? NAN : log1pf(p.s);
-        if (lane == 0) {
-            all_s[0] = p.m;
-            all_s[1] = log_s;
-            if (a.entropy) a.entropy[row] = log_s - p.t * 0.69314718056f / (1.f + p.s);
-        }
+        if (lane == 0) part_s = p;
     } else if (wave == 1 && a.n_top > 0) {
-        // The n_top-th largest of the row is no smaller than the last of any tile's list, nor than the smallest of the tiles' nth ones.
-        const int nth = (a.n_top + a.tiles - 1) / a.tiles;
+        // The n_top-th largest of the row is no smaller than the last of any part's list, nor than the smallest of the parts' nth ones.
+        const int nth = (a.n_top + a.parts - 1) / a.parts;
         uint64_t last = 0, least = 0;   // least: inverted
-        for (int i = lane; i < a.tiles; i += 64) {
+        for (int i = lane; i < a.parts; i += 64) {
             const uint64_t x = best[(int64_t)i * a.n_top + a.n_top - 1], y = ~best[(int64_t)i * a.n_top + nth - 1];
             last = x > last ? x : last;
             least = y > least ? y : least;
@@ -292,28 +433,14 @@ template <bool BF16> __global__ __launch_bounds__(JT) void logprob_join_kernel(L
             listed_s = 0;
         }
     }
+    int n = 0;
+    if (a.ranks && (int)threadIdx.x < a.n_tokens)
+        for (int i = 0; i < a.parts; ++i) n += a.before[(slot + i) * a.n_tokens + threadIdx.x];
     __syncthreads();
-    const float m = all_s[0], log_s = all_s[1];
-    auto logprob = [&](float z) { return (z - m) * a.inv_t - log_s; };
-    for (int j = wave; j < a.n_tokens; j += JT / 64) {
-        const int token = a.tokens[row * a.n_tokens + j];
-        const bool there = token >= 0 && token < a.vocab;
-        int n = 0;
-        for (int i = lane; i < a.tiles; i += 64) n += a.before[(slot + i) * a.n_tokens + j];
-#pragma unroll
-        for (int i = 32; i > 0; i >>= 1) n += __shfl_xor(n, i);
-        if (lane == 0) {
-            a.logprobs[row * a.n_tokens + j] = there ? logprob(load(token)) : -INFINITY;
-            if (a.ranks) a.ranks[row * a.n_tokens + j] = there ? n : -1;
-        }
-    }
+    const Row r(a, row, part_s, threadIdx.x == 0);
+    if ((int)threadIdx.x < a.n_tokens) r.token(threadIdx.x, there, token_z, n);
     if (a.n_top == 0) return;
-    auto put = [&](int k, uint64_t key) {
-        const int id = (int)~(uint32_t)key;
-        a.top_ids[row * a.n_top + k] = id;
-        a.top_logprobs[row * a.n_top + k] = logprob(load(id));
-    };
-    const int64_t all = (int64_t)a.tiles * a.n_top;
+    const int64_t all = (int64_t)a.parts * a.n_top;
     const uint64_t bound = bound_s;
     for (int64_t i = threadIdx.x; i < all; i += JT) {
         const uint64_t key = best[i];
@@ -329,7 +456,7 @@ template <bool BF16> __global__ __launch_bounds__(JT) void logprob_join_kernel(L
             const uint64_t mine = list_s[i];
             int place = 0;
             for (int j = 0; j < listed; ++j) place += list_s[j] > mine;
-            if (place < a.n_top) put(place, mine);
+            if (place < a.n_top) r.top(place, mine);
         }
         return;
     }
@@ -347,24 +474,21 @@ template <bool BF16> __global__ __launch_bounds__(JT) void logprob_join_kernel(L
         below = list_s[0];
 #pragma unroll
         for (int w = 1; w < JT / 64; ++w) below = list_s[w] > below ? list_s[w] : below;
-        if (threadIdx.x == 0) put(k, below);
+        if (threadIdx.x == 0) r.top(k, below);
     }
 }
 
-// Tiles: small while there are few rows, so that they spread over the chip.
+// Whole rows while there are enough of them to fill the chip, else parts.
 struct LogPlan {
-    int v, tile, tiles;
+    int part, parts;
 };
-LogPlan log_plan(int64_t rows, int vocab, bool bf16)
+LogPlan log_plan(int64_t rows, int vocab)
 {
+    const int64_t want = (1024 + rows - 1) / rows, most = (vocab + 2047) / 2048;   // parts of 2048 logits at least
     LogPlan p;
-    const int per = bf16 ? 8 : 4;
-    p.v = 8;
-    while (p.v > 2 && rows * (((int64_t)vocab + LT * p.v * per - 1) / (LT * p.v * per)) < 512) p.v /= 2;
-    const int64_t most = (int64_t)LT * p.v * per;
-    p.tiles = (int)((vocab + most - 1) / most);
-    p.tile = (int)((((int64_t)vocab + p.tiles - 1) / p.tiles + per - 1) / per * per);
-    p.tiles = (vocab + p.tile - 1) / p.tile;
+    p.parts = (int)std::max<int64_t>(1, std::min(want, most));
+    p.part = (int)(((int64_t)vocab + p.parts - 1) / p.parts + 7) / 8 * 8;
+    p.parts = (vocab + p.part - 1) / p.part;
     return p;
 }
 struct LogScratch {
@@ -373,7 +497,7 @@ struct LogScratch {
 LogScratch log_scratch(int64_t rows, const LogPlan &p, int n_tokens, int n_top)
 {
     LogScratch s;
-    const size_t slots = (size_t)rows * p.tiles;
+    const size_t slots = p.parts > 1 ? (size_t)rows * p.parts : 0;
     s.best = slots * sizeof(f32x4);
     s.before = s.best + slots * n_top * sizeof(uint64_t);
     s.bytes = (s.before + slots * n_tokens * sizeof(int32_t) + 255) / 256 * 256;
@@ -387,7 +511,7 @@ extern "C" {
 size_t sssd_op_logprobs_scratch_bytes(int32_t type, int32_t rows, int32_t vocab, int32_t n_tokens, int32_t n_top)
 {
     if ((type != SSSD_F32 && type != SSSD_BF16) || rows <= 0 || vocab <= 0 || n_tokens < 0 || n_tokens > MOST_TOKENS || n_top < 0 || n_top > MOST_TOP || n_top > vocab) return 0;
-    return log_scratch(rows, log_plan(rows, vocab, type == SSSD_BF16), n_tokens, n_top).bytes;
+    return log_scratch(rows, log_plan(rows, vocab), n_tokens, n_top).bytes;
 }
 
 int sssd_op_logprobs(const void *logits, int32_t type, int32_t rows, int32_t vocab, int64_t row_stride, float temperature, const int32_t *tokens,
@@ -401,14 +525,14 @@ int sssd_op_logprobs(const void *logits, int32_t type, int32_t rows, int32_t voc
     if ((uintptr_t)logits % (bf16 ? 2 : 4) || (rows > 1 && row_stride < 0)) return SSSD_EINVAL;
     const float k = 1.4426950408889634f / temperature;
     if (!(temperature > 0.f) || !(k > 0.f) || !(k <= 3.0e38f)) return SSSD_EINVAL;
-    const LogPlan p = log_plan(rows, vocab, bf16);
+    const LogPlan p = log_plan(rows, vocab);
     const LogScratch z = log_scratch(rows, p, n_tokens, n_top);
-    if (!scratch || (uintptr_t)scratch % 16) return SSSD_EINVAL;
-    if (scratch_bytes < z.bytes || (int64_t)rows * p.tiles > UINT32_MAX / LT) return SSSD_ECAPACITY;
+    if (z.bytes && (!scratch || (uintptr_t)scratch % 16)) return SSSD_EINVAL;
+    if (scratch_bytes < z.bytes || (int64_t)rows * p.parts > UINT32_MAX / LT) return SSSD_ECAPACITY;
     LogArgs a{};
     a.logits = (const char *)logits;
     a.stride = rows > 1 ? row_stride : 0;
-    a.rows = rows; a.vocab = vocab; a.tile = p.tile; a.tiles = p.tiles;
+    a.rows = rows; a.vocab = vocab; a.part = p.part; a.parts = p.parts;
     a.n_tokens = n_tokens; a.n_top = n_top;
     a.k = k;
     a.inv_t = 1.f / temperature;
@@ -417,18 +541,14 @@ int sssd_op_logprobs(const void *logits, int32_t type, int32_t rows, int32_t voc
     a.best = (uint64_t *)((char *)scratch + z.best);
     a.before = (int32_t *)((char *)scratch + z.before);
     hipStream_t s = (hipStream_t)stream;
-    const dim3 grid((uint32_t)rows * p.tiles);
-#define TILE(V)                                                                                          \
-    do {                                                                                                 \
-        if (bf16) hipLaunchKernelGGL((logprob_tile_kernel<V, true>), grid, dim3(LT), 0, s, a);           \
-        else hipLaunchKernelGGL((logprob_tile_kernel<V, false>), grid, dim3(LT), 0, s, a);               \
-    } while (0)
-    switch (p.v) {
-    case 2: TILE(2); break;
-    case 4: TILE(4); break;
-    default: TILE(8); break;
+    const dim3 grid((uint32_t)rows * p.parts);
+    if (p.parts == 1) {
+        if (bf16) hipLaunchKernelGGL((logprob_kernel<true, true>), grid, dim3(LT), 0, s, a);
+        else hipLaunchKernelGGL((logprob_kernel<false, true>), grid, dim3(LT), 0, s, a);
+        return hipGetLastError() == hipSuccess ? SSSD_OK : SSSD_EHIP;
     }
-#undef TILE
+    if (bf16) hipLaunchKernelGGL((logprob_kernel<true, false>), grid, dim3(LT), 0, s, a);
+    else hipLaunchKernelGGL((logprob_kernel<false, false>), grid, dim3(LT), 0, s, a);
     if (hipGetLastError() != hipSuccess) return SSSD_EHIP;
     if (bf16) hipLaunchKernelGGL(logprob_join_kernel<true>, dim3(rows), dim3(JT), 0, s, a);
     else hipLaunchKernelGGL(logprob_join_kernel<false>, dim3(rows), dim3(JT), 0, s, a);
