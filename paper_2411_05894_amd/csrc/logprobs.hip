@@ -133,7 +133,7 @@ struct Row {   // what comes out of one
 // WHOLE: a workgroup has a whole row.  grid: parts of a row next to each other
 template <bool BF16, bool WHOLE> __global__ __launch_bounds__(LT) __attribute__((amdgpu_waves_per_eu(6))) void logprob_kernel(LogArgs a)
 {
-    constexpr int V = BF16 ? 2 : 4, PER = BF16 ? 8 : 4, SIZE = BF16 ? 2 : 4;   // 16-byte loads of a thread and chunk, logits of a load
+    constexpr int PER = BF16 ? 8 : 4, SIZE = BF16 ? 2 : 4, V = (WHOLE ? 16 : 8) / PER;   // logits of a 16-byte load, loads of a thread and chunk
     __shared__ float token_z_s[MOST_TOKENS];
     __shared__ int token_s[MOST_TOKENS], before_s[LWAVES][MOST_TOKENS], listed_s[LWAVES];
     __shared__ Part part_s[LWAVES];
@@ -396,6 +396,7 @@ template <bool BF16> __global__ __launch_bounds__(JT) void logprob_join_kernel(L
     __shared__ Part part_s;
     __shared__ uint64_t list_s[JLIST], bound_s;
     __shared__ uint32_t listed_s;
+    __shared__ int before_s[MOST_TOKENS];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t row = blockIdx.x, slot = row * a.parts;
     const char *base = a.logits + row * a.stride * (BF16 ? 2 : 4);
@@ -405,6 +406,11 @@ template <bool BF16> __global__ __launch_bounds__(JT) void logprob_join_kernel(L
     const int token = (int)threadIdx.x < a.n_tokens ? a.tokens[row * a.n_tokens + threadIdx.x] : -1;
     const bool there = token >= 0 && token < a.vocab;
     const float token_z = there ? load(token) : 0.f;
+    constexpr int EARLY = 4;   // tokens of a thread that are requested before it is known which of them count
+    const int64_t all = (int64_t)a.parts * a.n_top;
+    uint64_t keys[EARLY];
+#pragma unroll
+    for (int e = 0; e < EARLY; ++e) keys[e] = (int)threadIdx.x + e * JT < all ? best[threadIdx.x + e * JT] : 0;
     if (wave == 0) {
         Part p{-INFINITY, 0.f, 0.f};
         for (int i = lane; i < a.parts; i += 64) {
@@ -433,22 +439,28 @@ template <bool BF16> __global__ __launch_bounds__(JT) void logprob_join_kernel(L
             listed_s = 0;
         }
     }
-    int n = 0;
-    if (a.ranks && (int)threadIdx.x < a.n_tokens)
-        for (int i = 0; i < a.parts; ++i) n += a.before[(slot + i) * a.n_tokens + threadIdx.x];
+    if (wave >= 2 && a.ranks)
+        for (int j = wave - 2; j < a.n_tokens; j += JT / 64 - 2) {
+            int n = 0;
+            for (int i = lane; i < a.parts; i += 64) n += a.before[(slot + i) * a.n_tokens + j];
+#pragma unroll
+            for (int i = 32; i > 0; i >>= 1) n += __shfl_xor(n, i);
+            if (lane == 0) before_s[j] = n;
+        }
     __syncthreads();
     const Row r(a, row, part_s, threadIdx.x == 0);
-    if ((int)threadIdx.x < a.n_tokens) r.token(threadIdx.x, there, token_z, n);
+    if ((int)threadIdx.x < a.n_tokens) r.token(threadIdx.x, there, token_z, before_s[threadIdx.x]);
     if (a.n_top == 0) return;
-    const int64_t all = (int64_t)a.parts * a.n_top;
     const uint64_t bound = bound_s;
-    for (int64_t i = threadIdx.x; i < all; i += JT) {
-        const uint64_t key = best[i];
+    auto list = [&](uint64_t key) {
         if (key && key >= bound) {
             const uint32_t k = atomicAdd(&listed_s, 1u);
             if (k < JLIST) list_s[k] = key;
         }
-    }
+    };
+#pragma unroll
+    for (int e = 0; e < EARLY; ++e) list(keys[e]);
+    for (int64_t i = threadIdx.x + EARLY * JT; i < all; i += JT) list(best[i]);
     __syncthreads();
     const int listed = (int)listed_s;
     if (listed <= JLIST) {
