@@ -83,7 +83,7 @@ __device__ __forceinline__ int scan_group(int x, int &total, int *lds)
     return before + upto - x;
 }
 
-// The lowest `n` pages for which free(page): take(i, page) for the i-th of them.  Whole workgroup; returns how many there are, at most n.
+// The lowest `n` pages for which free(page, which of its thread's): take(i, page) for the i-th of them.  Whole workgroup; returns how many there are, at most n.
 template <typename Free, typename Take> __device__ __forceinline__ int find_pages(int pages, int n, int *lds, Free free, Take take)
 {
     int found = 0;
@@ -93,7 +93,7 @@ template <typename Free, typename Take> __device__ __forceinline__ int find_page
 #pragma unroll
         for (int e = 0; e < PER; ++e) {
             const int p = base + (int)threadIdx.x * PER + e;
-            is[e] = p < pages && free(p);
+            is[e] = p < pages && free(p, e);
             mine += is[e];
         }
         int total, at = found + scan_group(mine, total, lds);
@@ -186,7 +186,7 @@ __global__ __launch_bounds__(PT) void fork_decide_kernel(PagesArgs a)
     __syncthreads();
     bool go = !fault && n <= a.g.n_pages;
     if (go && n > 0) {
-        const int found = find_pages(a.g.n_pages, n, lds, [&](int p) { return a.refs[p] + a.delta[p] == 0; }, [&](int i, int p) { a.copy[i].y = p; });
+        const int found = find_pages(a.g.n_pages, n, lds, [&](int p, int) { return a.refs[p] + a.delta[p] == 0; }, [&](int i, int p) { a.copy[i].y = p; });
         go = found == n;
         __syncthreads();
         if (go)
@@ -267,94 +267,115 @@ __global__ __launch_bounds__(256) void fork_write_kernel(PagesArgs a, CopyArgs c
 }
 
 // ---------------------------------------------------------------------------------------------------------- reserve ----
-// One workgroup: the blocks that the call's rows touch, slot by slot, a thread each.
+// One workgroup: the blocks that the call's rows touch, slot by slot, a thread each, in as many rounds as they take.  One round is the rule (a step's rows): then what a thread has
+// read stays with it.
+struct Asked {
+    bool on, bad, live;   // live: rows that live are in the block
+    int slot, blk, page, refs;
+};
 __global__ __launch_bounds__(PT) void reserve_kernel(PagesArgs a)
 {
-    __shared__ int off_s[PT + 1], first_s[PT], lds[PT / 64], fault_s;
+    __shared__ int off_s[PT], len_s[PT], lds[PT / 64], fault_s, shared_s;
     const int per = a.g.blocks_per_seq;
-    if (threadIdx.x == 0) fault_s = 0;
+    int early[PER];   // the front of the pool, in case pages are wanted
+#pragma unroll
+    for (int e = 0; e < PER; ++e) early[e] = (int)threadIdx.x * PER + e < a.g.n_pages ? a.refs[threadIdx.x * PER + e] : 1;
+    if (threadIdx.x == 0) fault_s = shared_s = 0;
     __syncthreads();
-    // f(slot, block, place, live) for all of them in order, at(i) of the i-th of a round, the same number of times in every thread
+    auto place = [&](int slot, int blk) { return (size_t)slot * per + blk; };
+    // Sequences base .. base + PT - 1: where their blocks begin among those of the round; how many there are.
+    auto sequences = [&](int base) {
+        const int i = base + (int)threadIdx.x;
+        int len = 0, n = 0, total;
+        if (i < a.B) {
+            const int count = a.counts ? a.counts[i] : a.n;
+            len = a.lens[i];
+            const bool ok = len >= 0 && count >= 0 && count <= a.n && (int64_t)len + count <= a.g.max_seq;
+            if (!ok) fault_s = 1;
+            n = ok && count > 0 ? blocks_of(len + count) - (len >> 5) : 0;
+            len = ok ? len : 0;
+        }
+        const int at = scan_group(n, total, lds);
+        off_s[threadIdx.x] = at;
+        len_s[threadIdx.x] = len;
+        __syncthreads();
+        return total;
+    };
+    auto block = [&](int base, int k, int total) {
+        Asked x{k < total, false, false, 0, 0, -1, 0};
+        if (!x.on) return x;
+        int lo = 0, hi = PT - 1;   // the last sequence that begins at or before k: it has blocks
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (off_s[mid] <= k) lo = mid;
+            else hi = mid - 1;
+        }
+        x.slot = a.first + base + lo;
+        x.blk = (len_s[lo] >> 5) + k - off_s[lo];
+        x.live = (int64_t)x.blk * 32 < len_s[lo];
+        x.page = a.table[place(x.slot, x.blk)];
+        x.bad = x.page < -1 || x.page >= a.g.n_pages;
+        x.refs = x.bad || x.page < 0 ? 0 : a.refs[x.page];
+        x.bad = x.bad || (x.page >= 0 && x.refs <= 0);
+        return x;
+    };
+    int total = a.B <= PT ? sequences(0) : 0;
+    const bool one = a.B <= PT && total <= PT;
+    const Asked mine = block(0, threadIdx.x, one ? total : 0);
+    // f(what is asked) for all blocks in order, the same number of times in every thread
     auto all = [&](auto f) {
+        if (one) {
+            f(mine);
+            return;
+        }
         for (int base = 0; base < a.B; base += PT) {
-            const int i = base + threadIdx.x;
-            int from = 0, n = 0;
-            if (i < a.B) {
-                const int len = a.lens[i], count = a.counts ? a.counts[i] : a.n;
-                const bool ok = len >= 0 && count >= 0 && count <= a.n && (int64_t)len + count <= a.g.max_seq;
-                if (!ok) fault_s = 1;
-                from = ok ? len >> 5 : 0;
-                n = ok && count > 0 ? blocks_of(len + count) - from : 0;
-            }
-            int total;
-            const int at = scan_group(n, total, lds);
-            off_s[threadIdx.x] = at;
-            first_s[threadIdx.x] = from;
-            __syncthreads();
-            for (int r = 0; r < total; r += PT) {
-                const int k = r + threadIdx.x;
-                int lo = 0, hi = PT - 1;   // the last slot that begins at or before k and has blocks
-                while (lo < hi) {
-                    const int mid = (lo + hi + 1) >> 1;
-                    if (off_s[mid] <= k) lo = mid;
-                    else hi = mid - 1;
-                }
-                f(k < total, a.first + base + lo, first_s[lo] + k - off_s[lo], base + lo);
-            }
+            if (a.B > PT) total = sequences(base);
+            for (int r = 0; r < total; r += PT) f(block(base, r + threadIdx.x, total));
             __syncthreads();
         }
     };
-    auto place = [&](int slot, int blk) { return (size_t)slot * per + blk; };
     // pages that several entries name: their counters
-    all([&](bool on, int slot, int blk, int) {
-        if (!on) return;
-        const int page = a.table[place(slot, blk)];
-        if (page < -1 || page >= a.g.n_pages || (page >= 0 && a.refs[page] <= 0)) {
+    all([&](const Asked &x) {
+        if (x.bad) {
             fault_s = 1;
-        } else if (page >= 0 && a.refs[page] > 1) {
-            __hip_atomic_store(&a.map[page], 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            __hip_atomic_store(&a.low[page], ~0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        } else if (x.refs > 1) {
+            shared_s = 1;
+            __hip_atomic_store(&a.map[x.page], 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __hip_atomic_store(&a.low[x.page], ~0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
     });
-    __threadfence();
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     const bool fault = fault_s != 0;
     int n = 0;
-    if (!fault) {
-        all([&](bool on, int slot, int blk, int) {
-            if (!on) return;
-            const int page = a.table[place(slot, blk)];
-            if (page >= 0 && a.refs[page] > 1) {
-                atomicAdd(&a.map[page], 1);
-                atomicMin(&a.low[page], (unsigned long long)place(slot, blk));
-            }
+    if (!fault && shared_s) {
+        all([&](const Asked &x) {
+            if (x.refs <= 1) return;
+            atomicAdd(&a.map[x.page], 1);
+            atomicMin(&a.low[x.page], (unsigned long long)place(x.slot, x.blk));
         });
-        __threadfence();
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        all([&](bool on, int slot, int blk, int i) {
-            bool wants = false;
-            int page = -1;
-            if (on) {
-                page = a.table[place(slot, blk)];
-                wants = page < 0;
-                if (page >= 0 && a.refs[page] > 1) {   // where all who share a page ask for it, the first one keeps it
-                    const unsigned long long low = __hip_atomic_load(&a.low[page], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                    wants = !(agent_load(&a.map[page]) == a.refs[page] && low == place(slot, blk));
-                }
-            }
-            int total;
-            const int at = n + scan_group(wants, total, lds);
-            if (wants && at < a.g.n_pages) {
-                a.need[at] = int3{slot, blk, page};
-                a.copy[at].x = page >= 0 && (int64_t)blk * 32 < a.lens[i] ? page : -1;
-            }
-            n += total;
-        });
     }
+    if (!fault)
+        all([&](const Asked &x) {
+            bool wants = x.on && x.page < 0;
+            if (x.refs > 1) {   // where all who share a page ask for it, the first one keeps it
+                const unsigned long long low = __hip_atomic_load(&a.low[x.page], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                wants = !(agent_load(&a.map[x.page]) == x.refs && low == place(x.slot, x.blk));
+            }
+            int sum;
+            const int at = n + scan_group(wants, sum, lds);
+            if (wants && at < a.g.n_pages) {
+                a.need[at] = int3{x.slot, x.blk, x.page};
+                a.copy[at].x = x.page >= 0 && x.live ? x.page : -1;
+            }
+            n += sum;
+        });
     __syncthreads();
     bool go = !fault && n <= a.g.n_pages;
     if (go && n > 0) {
-        const int found = find_pages(a.g.n_pages, n, lds, [&](int p) { return a.refs[p] == 0; }, [&](int i, int p) { a.copy[i].y = p; });
+        const int found = find_pages(a.g.n_pages, n, lds, [&](int p, int e) { return (p < PT * PER ? early[e] : a.refs[p]) == 0; }, [&](int i, int p) { a.copy[i].y = p; });
         go = found == n;
     }
     __syncthreads();
@@ -417,7 +438,7 @@ __global__ __launch_bounds__(PT) void compact_plan_kernel(PagesArgs a)
     if (go) {
         if (a.to_table) {   // all of them, in order
             copies = used;
-            find_pages(pages, used, lds, [&](int p) { return a.refs[p] > 0; }, [&](int i, int p) {
+            find_pages(pages, used, lds, [&](int p, int) { return a.refs[p] > 0; }, [&](int i, int p) {
                 a.map[p] = i;
                 a.copy[i] = int2{p, i};
             });
@@ -425,9 +446,9 @@ __global__ __launch_bounds__(PT) void compact_plan_kernel(PagesArgs a)
                 if (a.refs[p] <= 0) a.map[p] = -1;
         } else {   // the i-th in use behind the first `used` pages into the i-th hole among them
             for (int p = threadIdx.x; p < pages; p += PT) a.map[p] = a.refs[p] > 0 ? p : -1;
-            copies = find_pages(used, used, lds, [&](int p) { return a.refs[p] <= 0; }, [&](int i, int p) { a.copy[i].y = p; });
+            copies = find_pages(used, used, lds, [&](int p, int) { return a.refs[p] <= 0; }, [&](int i, int p) { a.copy[i].y = p; });
             __syncthreads();
-            find_pages(pages - used, copies, lds, [&](int p) { return a.refs[used + p] > 0; }, [&](int i, int p) { a.copy[i].x = used + p; });
+            find_pages(pages - used, copies, lds, [&](int p, int) { return a.refs[used + p] > 0; }, [&](int i, int p) { a.copy[i].x = used + p; });
             __syncthreads();
             for (int i = threadIdx.x; i < copies; i += PT) {
                 const int2 move = a.copy[i];
