@@ -250,6 +250,7 @@ struct Kv8SharedArgs : Kv8AttnArgs {   // of a batch whose sequences share prefi
     int tiles;             // workgroups' row tiles of all groups at most
     int wave_rows;         // waves of a workgroup on row tiles of their own: 4, or 1 with the others on other segments
     int prefix_share;      // workgroups on a prefix at most
+    int prefix_groups;     // workgroups of a launch that are on prefixes
     int prefix_segments;   // segments of a prefix at most: prefix_share * 4 / wave_rows
     int rows_all;          // B * n * gq
 };

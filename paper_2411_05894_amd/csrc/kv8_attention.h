@@ -328,18 +328,28 @@ template <int MODE> using Kv8Args = std::conditional_t<MODE == KV8_ALONE, Kv8Att
 // PARTS: the query operand is float16 (1: bf16 queries) or float16 hi + lo (2: float32 queries), and so are the probabilities.
 // grid: workgroups of one (sequence, kv head) have block indexes of one residue modulo 8: its segments, and their passes next to each other.
 // KV8_PREFIX: a wave has row tiles of its own (wave_rows of a workgroup's waves), the others of a tile are on other segments; its partial results are its own.
-template <int HD, int FMT, int RT, int PARTS, int NW, int MODE = KV8_ALONE>
-__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void kv8_attn_kernel(Kv8Args<MODE> a)
+template <int HD, int RT, int PARTS, int NW, int MODE> struct AttnShared {   // LDS of a workgroup
+    static constexpr int KS = HD / 32, DT = HD / 16, QT = DT / NW, TR = NW == 4 ? RT : RT <= 2 ? RT : 2;
+    static constexpr int QREC = RT * KS * PARTS * 64, RRED = NW * (NW - 1) * TR * QT * 64, QSETS = MODE == KV8_PREFIX ? NW : 1;
+    u32x4 lds[MODE == KV8_PREFIX ? QREC * NW : QREC > RRED ? QREC : RRED];
+    float row_scale_s[RT * 16 * QSETS];
+    uint32_t word_s[RT * 16];
+    int low_s[RT * 16], way_s;
+    float2 ml_s[NW][RT * 16];
+    int vref_s[NW];
+};
+// bid: the workgroup's number among those of this kind
+template <int HD, int FMT, int RT, int PARTS, int NW, int MODE>
+__device__ __forceinline__ void attend_group(const Kv8Args<MODE> &a, AttnShared<HD, RT, PARTS, NW, MODE> &sh, const uint32_t bid)
 {
-    constexpr int KS = HD / 32, DT = HD / 16, QT = DT / NW, TR = NW == 4 ? RT : RT <= 2 ? RT : 2;
+    using Shared = AttnShared<HD, RT, PARTS, NW, MODE>;
+    constexpr int KS = Shared::KS, DT = Shared::DT, QT = Shared::QT, TR = Shared::TR, QREC = Shared::QREC;
     constexpr bool PRE = MODE == KV8_PREFIX;
-    constexpr int QREC = RT * KS * PARTS * 64, RRED = NW * (NW - 1) * TR * QT * 64, QSETS = PRE ? NW : 1;
-    __shared__ u32x4 lds[PRE ? QREC * NW : QREC > RRED ? QREC : RRED];
-    __shared__ float row_scale_s[RT * 16 * QSETS];
-    __shared__ uint32_t word_s[RT * 16];
-    __shared__ int low_s[RT * 16], way_s;
-    __shared__ float2 ml_s[NW][RT * 16];
-    __shared__ int vref_s[NW];
+    u32x4 *lds = sh.lds;
+    float *row_scale_s = sh.row_scale_s;
+    uint32_t *word_s = sh.word_s;
+    int *low_s = sh.low_s, &way_s = sh.way_s, *vref_s = sh.vref_s;
+    auto &ml_s = sh.ml_s;
 
     const int passes = a.plan.passes, share = a.plan.share, nkv = a.g.nkv;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -348,7 +358,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
     int skip = 0, n_rows = 0;   // blocks that are another workgroup's; rows of a group
     if constexpr (PRE) {
         // workgroups of one (kv head, segment) on one die: they read the same blocks; tiles that no group has come last
-        const uint32_t slot = blockIdx.x >> 3, pairs = ((uint32_t)nkv * a.prefix_share + 7) >> 3, x = slot / pairs, pair = (slot - x * pairs) * 8 + (blockIdx.x & 7);
+        const uint32_t slot = bid >> 3, pairs = ((uint32_t)nkv * a.prefix_share + 7) >> 3, x = slot / pairs, pair = (slot - x * pairs) * 8 + (bid & 7);
         int tile = (int)x;
         segment = (int)(pair / (uint32_t)nkv);
         kvh = (int)pair - segment * nkv;
@@ -362,10 +372,10 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
         segment = segment * (NW / slabs) + wave / slabs;
         pass = tile * slabs + slab;
     } else {
-        const uint32_t slot = blockIdx.x >> 3, x = slot / (uint32_t)passes, row = x / (uint32_t)share;
+        const uint32_t slot = bid >> 3, x = slot / (uint32_t)passes, row = x / (uint32_t)share;
         pass = (int)(slot - x * passes);
         segment = (int)(x - row * share);
-        const uint32_t u = row * 8 + ((blockIdx.x - row) & 7);   // heads rotate over the dies
+        const uint32_t u = row * 8 + ((bid - row) & 7);   // heads rotate over the dies
         b = (int)(u / (uint32_t)nkv);
         kvh = (int)u - b * nkv;
     }
@@ -407,7 +417,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
     if constexpr (MODE == KV8_BEHIND) {
         bool sane;
         skip = group_of(a, b, lane, sane).blocks;
-        if (!sane && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(a.status, KV8_RANGE);
+        if (!sane && bid == 0 && threadIdx.x == 0) atomicOr(a.status, KV8_RANGE);
         if (len < skip * KV8_BLOCK) ok = false;   // shorter than what it is said to share
     }
 
@@ -848,6 +858,13 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
     }
     if (way != HAND_SHARE) left = hand_leave(a.hand, group);
     hand_clear(a.hand, group, cut.n, left);
+}
+
+template <int HD, int FMT, int RT, int PARTS, int NW>
+__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void kv8_attn_kernel(Kv8AttnArgs a)
+{
+    __shared__ AttnShared<HD, RT, PARTS, NW, KV8_ALONE> sh;
+    attend_group<HD, FMT, RT, PARTS, NW, KV8_ALONE>(a, sh, blockIdx.x);
 }
 
 }  // namespace

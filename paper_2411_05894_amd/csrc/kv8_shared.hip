@@ -20,19 +20,20 @@ namespace {
 // float16 holds exactly (down to 2^-21 for 8-bit floats, 2^-12 for integers); else blocks are multiplied as they are, with probabilities relative to the
 // block's own maximum (or REF_FAR below the row's reference, where that is higher), and added in 32 bits.
 constexpr int V_SPAN = V_ABOVE + V_BELOW;
-constexpr int prefix_waves(int rt, int parts) { return rt * parts <= 2 ? 2 : 1; }   // waves of a SIMD that the registers leave room for
 
-template <int HD, int FMT, int RT, int PARTS>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(prefix_waves(RT, PARTS), prefix_waves(RT, PARTS)))) void kv8_prefix_kernel(Kv8SharedArgs a)
+template <int HD> struct PrefixShared {   // LDS of a workgroup: operands of two pairs of blocks
+    u32x4 ring[2][2 * (HD / 8) * 64];
+};
+template <int HD, int FMT, int RT, int PARTS> __device__ __forceinline__ void prefix_group(const Kv8SharedArgs &a, PrefixShared<HD> &sh, const uint32_t bid)
 {
     constexpr int KS = HD / 32, DT = HD / 16, REC = HD / 16, MINE = REC / 4;   // 16-byte records of a lane: of a block (K's, V's), of a wave
     constexpr int BLOCK_OPS = 2 * REC * 64;   // operands of a block
-    __shared__ u32x4 ring[2][2 * BLOCK_OPS];
+    auto &ring = sh.ring;
     const int nkv = a.g.nkv;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, q = lane >> 4, c = lane & 15;
     // Workgroups of one (kv head, segment) on one die: they read the same blocks.  Tiles that no group has come last: in between, workgroups that end at once
     // had some compute units get three of those that do not, and others one.
-    const uint32_t slot = blockIdx.x >> 3, pairs = ((uint32_t)nkv * a.prefix_share + 7) >> 3, x0 = slot / pairs, pair = (slot - x0 * pairs) * 8 + (blockIdx.x & 7);
+    const uint32_t slot = bid >> 3, pairs = ((uint32_t)nkv * a.prefix_share + 7) >> 3, x0 = slot / pairs, pair = (slot - x0 * pairs) * 8 + (bid & 7);
     int tile = (int)x0;
     const int segment = (int)(pair / (uint32_t)nkv), kvh = (int)pair - segment * nkv;
     if (segment >= a.prefix_share) return;
@@ -106,6 +107,23 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(prefix_wave
         }
     }
 
+    // A wave's records of a block: K's are those below REC / 2, then V's.  Blocks go in pairs; where block i is multiplied, scores are made of block i + 1 already, so K's
+    // pairs are one block ahead of V's.
+    u32x4 raw[2][MINE];
+    auto is_v = [&](int x) { return wave + 4 * x >= REC / 2; };
+    auto request = [&](int i) {   // V's records of blocks i and i + 1, K's of i + 1 and i + 2 (behind the last: that one again)
+#pragma unroll
+        for (int two = 0; two < 2; ++two)
+#pragma unroll
+            for (int x = 0; x < MINE; ++x) {
+                const int at = min(i + two + (is_v(x) ? 0 : 1), n_it - 1);
+                const uint32_t record = (uint32_t)__builtin_amdgcn_readlane(at >> 6 == chunk ? now.record : next.record, at & 63);
+                const auto p = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(a.codes) + (size_t)record * (64 * HD), 0, 64 * HD, 0x00027000);
+                raw[two][x] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(p, lane * 16, (wave + 4 * x) * 1024, 0));
+            }
+    };
+    request(-1);   // K of block 0 (and what is not used)
+
     // The segment's largest and smallest scale of V (biased exponents).
     int v_ref = (int)(f32_bits(now.scale.y) >> 23 & 255), v_low = v_ref;
     for (int i = 1; i * 64 < n_it; ++i) {
@@ -122,21 +140,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(prefix_wave
     const bool wide = __builtin_amdgcn_readfirstlane(v_ref - v_low) > V_SPAN;
     if (n_it > 64) next = look(1);
 
-    // A wave's records of a block: K's are those below REC / 2, then V's.  Blocks go in pairs; where block i is multiplied, scores are made of block i + 1 already, so K's
-    // pairs are one block ahead of V's.
-    u32x4 raw[2][MINE];
-    auto is_v = [&](int x) { return wave + 4 * x >= REC / 2; };
-    auto request = [&](int i) {   // V's records of blocks i and i + 1, K's of i + 1 and i + 2 (behind the last: that one again)
-#pragma unroll
-        for (int two = 0; two < 2; ++two)
-#pragma unroll
-            for (int x = 0; x < MINE; ++x) {
-                const int at = min(i + two + (is_v(x) ? 0 : 1), n_it - 1);
-                const uint32_t record = (uint32_t)__builtin_amdgcn_readlane(at >> 6 == chunk ? now.record : next.record, at & 63);
-                const auto p = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(a.codes) + (size_t)record * (64 * HD), 0, 64 * HD, 0x00027000);
-                raw[two][x] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(p, lane * 16, (wave + 4 * x) * 1024, 0));
-            }
-    };
     // Operand tiles in LDS: of a pair, K's [u][ks] and then V's [dt].
     auto hand = [&](int i, u32x4 *to) {
 #pragma unroll
@@ -279,7 +282,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(prefix_wave
         if (i + 1 < n_it) refer(i + 1);
     };
 
-    request(-1);   // K of block 0 (and what is not used)
     hand(-1, ring[1]);
     request(0);
     __syncthreads();
@@ -399,40 +401,44 @@ template <int HD> __global__ __launch_bounds__(256) void kv8_shared_merge_kernel
     }
 }
 
-template <int HD, int FMT, int PARTS> hipError_t launch_shared(const Kv8SharedArgs &a, int rt_prefix, int rt, hipStream_t s)
+// Both kinds of workgroups in one launch, those of prefixes first: they take longest, and the others fill in behind them.  RTP: row tiles of a wave of a prefix; FEW: its waves
+// are on different segments.
+template <int HD, int FMT, int PARTS, int RTP, bool FEW, int RT>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void kv8_shared_kernel(Kv8SharedArgs a)
 {
-    if (a.groups > 0) {
-        const uint32_t pairs = (uint32_t)a.g.nkv * a.prefix_share;
-        const dim3 grid((pairs + 7) / 8 * 8 * a.tiles);
-#define KV8_FEW(RT) hipLaunchKernelGGL((kv8_attn_kernel<HD, FMT, RT, PARTS, 4, KV8_PREFIX>), grid, dim3(256), 0, s, a)
-#define KV8_MANY(RT) hipLaunchKernelGGL((kv8_prefix_kernel<HD, FMT, RT, PARTS>), grid, dim3(256), 0, s, a)
-        if (a.wave_rows == 4) {
-            switch (rt_prefix) {
-            case 1: KV8_MANY(1); break;
-            case 2: KV8_MANY(2); break;
-            case 3: KV8_MANY(3); break;
-            default: KV8_MANY(4); break;
-            }
-        } else {
-            switch (rt_prefix) {
-            case 1: KV8_FEW(1); break;
-            case 2: KV8_FEW(2); break;
-            default: KV8_FEW(3); break;
-            }
-        }
-#undef KV8_FEW
-#undef KV8_MANY
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
-    const dim3 grid(((uint32_t)a.B * a.g.nkv + 7) / 8 * 8 * a.plan.share * a.plan.passes);
-#define KV8_REST(RT) hipLaunchKernelGGL((kv8_attn_kernel<HD, FMT, RT, PARTS, 4, KV8_BEHIND>), grid, dim3(256), 0, s, a)
-    switch (rt) {
-    case 1: KV8_REST(1); break;
-    case 2: KV8_REST(2); break;
-    default: KV8_REST(3); break;
+    union Shared {
+        PrefixShared<HD> many;
+        AttnShared<HD, RTP, PARTS, 4, KV8_PREFIX> few;
+        AttnShared<HD, RT, PARTS, 4, KV8_BEHIND> rest;
+    };
+    constexpr size_t BYTES = std::max(FEW ? sizeof(Shared::few) : sizeof(Shared::many), sizeof(Shared::rest));
+    __shared__ __align__(16) char lds[BYTES];
+    if (blockIdx.x >= (uint32_t)a.prefix_groups) attend_group<HD, FMT, RT, PARTS, 4, KV8_BEHIND>(a, *reinterpret_cast<AttnShared<HD, RT, PARTS, 4, KV8_BEHIND> *>(lds), blockIdx.x - a.prefix_groups);
+    else if constexpr (FEW) attend_group<HD, FMT, RTP, PARTS, 4, KV8_PREFIX>(a, *reinterpret_cast<AttnShared<HD, RTP, PARTS, 4, KV8_PREFIX> *>(lds), blockIdx.x);
+    else prefix_group<HD, FMT, RTP, PARTS>(a, *reinterpret_cast<PrefixShared<HD> *>(lds), blockIdx.x);
+}
+
+template <int HD, int FMT, int PARTS> hipError_t launch_shared(Kv8SharedArgs a, int rt_prefix, int rt, hipStream_t s)
+{
+    a.prefix_groups = a.groups > 0 ? ((uint32_t)a.g.nkv * a.prefix_share + 7) / 8 * 8 * a.tiles : 0;
+    const dim3 grid(a.prefix_groups + ((uint32_t)a.B * a.g.nkv + 7) / 8 * 8 * a.plan.share * a.plan.passes);
+#define KV8_SHARED(RTP, FEW, RT) hipLaunchKernelGGL((kv8_shared_kernel<HD, FMT, PARTS, RTP, FEW, RT>), grid, dim3(256), 0, s, a)
+#define KV8_REST(RTP, FEW)                        \
+    do {                                          \
+        if (rt == 1) KV8_SHARED(RTP, FEW, 1);     \
+        else if (rt == 2) KV8_SHARED(RTP, FEW, 2); \
+        else KV8_SHARED(RTP, FEW, 3);             \
+    } while (0)
+    if (a.wave_rows == 1) {
+        if (rt_prefix == 1) KV8_REST(1, true);
+        else KV8_REST(2, true);
+    } else if (PARTS == 2 || rt_prefix == 1) {
+        KV8_REST(1, false);
+    } else {
+        KV8_REST(3 - PARTS, false);
     }
 #undef KV8_REST
+#undef KV8_SHARED
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kv8_shared_merge_kernel<HD>, dim3(((uint32_t)a.rows_all * a.g.nkv + 3) / 4), dim3(256), 0, s, a);
@@ -451,24 +457,17 @@ Kv8SharedPlan kv8_shared_plan(int B, int n, int gq, int nkv, int groups, bool f3
     Kv8SharedPlan p{};
     const int64_t rows = (int64_t)B * n * gq, each = groups > 0 ? (rows + groups - 1) / groups : rows;   // rows of a group, if they are all alike
     const int64_t tiles = (each + 15) / 16;
-    if (tiles <= KV8_MAX_TILES) {
+    if (tiles <= 2) {
         p.rt = (int)tiles;
         p.wave_rows = 1;
-    } else {   // as few row tiles as can be that are nobody's
+    } else {
+        p.rt = f32 || tiles <= 4 ? 1 : 2;
         p.wave_rows = 4;
-        int64_t best = INT64_MAX;
-        for (int rt = 4; rt >= 1; --rt) {
-            const int64_t cost = (tiles + 4 * rt - 1) / (4 * rt) * (rt + 1);
-            if (cost < best) {
-                best = cost;
-                p.rt = rt;
-            }
-        }
     }
     const int64_t per = p.wave_rows * p.rt * 16;
     p.tiles = (int)((rows + per - 1) / per + std::max(groups, 1) - 1);
     const int64_t units = (each + per - 1) / per * (groups > 0 ? groups : 1) * nkv;
-    const int64_t share = (p.wave_rows == 4 && p.rt * (f32 ? 2 : 1) > 2 ? 256 : KV8_GROUPS) / units;
+    const int64_t share = KV8_GROUPS / units;
     p.share = share < 1 ? 1 : share > 64 ? 64 : (int)share;
     p.segments = p.share * 4 / p.wave_rows;
     return p;
