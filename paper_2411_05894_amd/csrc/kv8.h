@@ -258,7 +258,7 @@ Kv8Plan kv8_plan(int B, int n, int gq, int nkv, int blocks, bool f32);   // bloc
 struct Kv8SharedPlan {
     int rt, wave_rows, tiles, share, segments;   // row tiles of a wave; the others as in Kv8SharedArgs
 };
-Kv8SharedPlan kv8_shared_plan(int B, int n, int gq, int nkv, int groups, bool f32);
+Kv8SharedPlan kv8_shared_plan(int B, int n, int gq, int nkv, int blocks, int groups, bool f32);   // blocks: of a sequence at most
 size_t kv8_shared_ws(int B, int n, int gq, int nkv, int d);
 size_t kv8_attention_ws(int d);   // bytes behind the workspace that any call's partial results take
 hipError_t launch_kv8_attention(Kv8AttnArgs a, int fmt, int d, void *ws, hipStream_t s);

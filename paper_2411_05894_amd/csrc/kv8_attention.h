@@ -312,10 +312,10 @@ __device__ __forceinline__ Group group_of_tile(const Kv8SharedArgs &a, int &tile
     tile = at;
     return ok ? mine : Group{0, 0, 0};
 }
-// The segments of a shared prefix, a wave each.
-__device__ __forceinline__ Cut prefix_cut(int blocks, int share)
+// The segments of a shared prefix, at least four blocks each.
+__device__ __forceinline__ Cut prefix_cut(const Kv8SharedArgs &a, int blocks)
 {
-    const int each = max((int)(((unsigned)blocks + (unsigned)share - 1u) / (unsigned)share), 4);
+    const int each = max((int)(((unsigned)blocks + (unsigned)a.prefix_segments - 1u) / (unsigned)a.prefix_segments), 4);
     return Cut{each, (int)(((unsigned)blocks + (unsigned)each - 1u) / (unsigned)each)};
 }
 // Where the partial result of a row of the batch lies: prefixes' segments first.
@@ -442,7 +442,7 @@ __device__ __forceinline__ void attend_group(const Kv8Args<MODE> &a, AttnShared<
     if constexpr (MODE == KV8_BEHIND) span = Span{0, skip, span.n - skip};
     if constexpr (PRE) span = Span{0, 0, skip};
     Cut cut = cut_of(span.n, share);
-    if constexpr (PRE) cut = prefix_cut(span.n, a.prefix_segments);
+    if constexpr (PRE) cut = prefix_cut(a, span.n);
     if (!PRE && segment >= cut.n) return;
     // blocks of a wave: first + off, and every STEP-th behind it
     constexpr int STEP = PRE ? 1 : NW;

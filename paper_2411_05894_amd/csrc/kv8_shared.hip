@@ -10,6 +10,7 @@
 #include "kv8_host.h"
 
 #include <algorithm>
+#include <cmath>
 
 namespace {
 
@@ -40,7 +41,7 @@ template <int HD, int FMT, int RT, int PARTS> __device__ __forceinline__ void pr
     const Group g = group_of_tile(a, tile, 4 * RT * 16, lane);
     if (g.n == 0) return;
     const int each = a.n * a.gq, rows = g.n * each, row0 = (tile * 4 + wave) * RT * 16;
-    const Cut cut = prefix_cut(g.blocks, a.prefix_segments);
+    const Cut cut = prefix_cut(a, g.blocks);
     if (segment >= cut.n) return;
     const int first = segment * cut.each, n_it = min(cut.each, g.blocks - first);
     const bool mine = row0 < rows;
@@ -345,7 +346,7 @@ template <int HD> __global__ __launch_bounds__(256) void kv8_shared_merge_kernel
         return;
     }
     if (r >= count * a.gq) return;
-    const int n_pre = g.blocks ? prefix_cut(g.blocks, a.prefix_segments).n : 0;
+    const int n_pre = g.blocks ? prefix_cut(a, g.blocks).n : 0;
     const int n_seg = n_pre + cut_of(((len + count + 31) >> 5) - g.blocks, a.plan.share).n;
     const int row = b * R + r;
     auto slot = [&](int s) { return shared_slot(a, s < n_pre ? s : a.prefix_segments + s - n_pre, kvh, row); };
@@ -452,10 +453,15 @@ template <int HD> hipError_t launch_format(const Kv8SharedArgs &a, int fmt, int 
 
 }  // namespace
 
-Kv8SharedPlan kv8_shared_plan(int B, int n, int gq, int nkv, int groups, bool f32)
+// Row tiles of a wave, and how many workgroups go over a prefix, for groups that are all alike.  Few rows: a workgroup's waves are on different segments.  Else, with s workgroups to
+// a row tile and prefix, about
+//     blocks / s * (0.65 us, or half as much again where compute units have two of them) + s * rows * nkv * 264 us, for 528 bytes of partial results a row, out and in, at 4 TB/s
+// us, by that / as many as the chip holds: best of eight with 9 rows on 2048 positions 31 / 37, two prompts of 70B 61 / 64, 32 sequences of 4 rows on 2000 of 70B 41 / 49, 64 of one on
+// 32768 and 16 of 9 on 4096 the same.  More workgroups than find something to do hold those that lie behind them up by some 3 us.
+Kv8SharedPlan kv8_shared_plan(int B, int n, int gq, int nkv, int blocks, int groups, bool f32)
 {
     Kv8SharedPlan p{};
-    const int64_t rows = (int64_t)B * n * gq, each = groups > 0 ? (rows + groups - 1) / groups : rows;   // rows of a group, if they are all alike
+    const int64_t rows = (int64_t)B * n * gq, each = groups > 0 ? (rows + groups - 1) / groups : rows;
     const int64_t tiles = (each + 15) / 16;
     if (tiles <= 2) {
         p.rt = (int)tiles;
@@ -467,9 +473,17 @@ Kv8SharedPlan kv8_shared_plan(int B, int n, int gq, int nkv, int groups, bool f3
     const int64_t per = p.wave_rows * p.rt * 16;
     p.tiles = (int)((rows + per - 1) / per + std::max(groups, 1) - 1);
     const int64_t units = (each + per - 1) / per * (groups > 0 ? groups : 1) * nkv;
-    const int64_t share = KV8_GROUPS / units;
-    p.share = share < 1 ? 1 : share > 64 ? 64 : (int)share;
-    p.segments = p.share * 4 / p.wave_rows;
+    const int sub = 4 / p.wave_rows;   // segments of a workgroup
+    double best = 0;
+    p.share = 1;
+    for (int64_t s = 1; s <= 64 && s * units <= KV8_GROUPS && (s - 1) * sub * 4 < blocks; ++s) {
+        const double cost = std::ceil((double)blocks / (s * sub)) * (s * units <= 256 ? 0.65 : 0.975) + s * sub * (double)rows * nkv * 2.64e-4;
+        if (s == 1 || cost < best) {
+            best = cost;
+            p.share = (int)s;
+        }
+    }
+    p.segments = p.share * sub;
     return p;
 }
 
@@ -517,7 +531,7 @@ int sssd_kv8_attention_shared(const sssd_kv8 *kv, int32_t layer, int32_t B, int3
     a.plan = kv8_plan(B, n, a.gq, c.n_kv_heads, S.blocks_per_seq, !a.q.bf16);
     const int tiles = (n * a.gq + 15) / 16;
     a.rows_pad = tiles * 16;
-    const Kv8SharedPlan p = kv8_shared_plan(B, n, a.gq, c.n_kv_heads, groups, !a.q.bf16);
+    const Kv8SharedPlan p = kv8_shared_plan(B, n, a.gq, c.n_kv_heads, S.blocks_per_seq, groups, !a.q.bf16);
     a.groups = groups; a.starts = starts; a.shared = shared;
     a.tiles = p.tiles; a.wave_rows = p.wave_rows; a.prefix_share = p.share; a.prefix_segments = p.segments;
     a.rows_all = B * n * a.gq;
