@@ -98,7 +98,7 @@ int sssd_op_sample_wide(const float *logits, int32_t rows, int32_t vocab, const 
 
 /*
  * Log-probabilities under softmax(logits / temperature), row by row, in one pass over the logits; natural logarithms, float32.
- *   logits     device [rows][vocab], SSSD_F32 or SSSD_BF16, rows row_stride >= 0 elements apart
+ *   logits     device [rows][vocab], SSSD_F32 or SSSD_BF16, rows row_stride >= 0 elements apart; vocab <= 2^30
  *   tokens     device int32 [rows][n_tokens], n_tokens <= SSSD_LOGPROBS_MAX_TOKENS; NULL for none
  *   logprobs   device out [rows][n_tokens]; -infinity for a token outside 0 .. vocab-1
  *   ranks      device int32 out [rows][n_tokens] or NULL: how many tokens come before it, by logit descending, then id ascending; -1
@@ -106,7 +106,8 @@ int sssd_op_sample_wide(const float *logits, int32_t rows, int32_t vocab, const 
  *   entropy    device out [rows] or NULL
  *   top_ids, top_logprobs   device int32 and float32 out [rows][n_top], the first n_top tokens in that order; n_top <= vocab and
  *              <= SSSD_LOGPROBS_MAX_TOP; NULL for n_top = 0
- *   scratch    device, 16-byte aligned, any contents, at least sssd_op_logprobs_scratch_bytes; calls that share it must be ordered
+ *   scratch    device, 16-byte aligned, any contents, at least sssd_op_logprobs_scratch_bytes (0: not needed, may be NULL); calls that share it must
+ *              be ordered
  * Logits of -infinity are probabilities of 0.  A row that has no finite logit, one of +infinity or one that is no number has no distribution:
  * its log-probabilities (of tokens within the vocabulary) and its entropy are no numbers; in the order, what is no number counts as -infinity.
  */

@@ -22,6 +22,7 @@ constexpr int LT = 256, LWAVES = LT / 64;   // threads of a workgroup
 constexpr int LIST = 192;                   // a wave's list of tokens: two rounds of its lanes behind a list that has been cut
 constexpr int MOST_TOKENS = SSSD_LOGPROBS_MAX_TOKENS, MOST_TOP = SSSD_LOGPROBS_MAX_TOP;
 static_assert(LIST >= MOST_TOP + 64);
+constexpr int MOST_VOCAB = 1 << 30;         // places behind the last token are numbers, too
 constexpr float FAR = 4.f;                  // octaves of probability that M may be away from r
 
 // Order of tokens: larger logit first, then the lower id; what is no number counts as -infinity.  As one word, larger first: keys of logits ascend with
@@ -496,11 +497,11 @@ struct LogPlan {
 };
 LogPlan log_plan(int64_t rows, int vocab)
 {
-    const int64_t want = (1024 + rows - 1) / rows, most = (vocab + 2047) / 2048;   // parts of 2048 logits at least
+    const int64_t want = (1024 + rows - 1) / rows, most = ((int64_t)vocab + 2047) / 2048;   // parts of 2048 logits at least
     LogPlan p;
     p.parts = (int)std::max<int64_t>(1, std::min(want, most));
-    p.part = (int)(((int64_t)vocab + p.parts - 1) / p.parts + 7) / 8 * 8;
-    p.parts = (vocab + p.part - 1) / p.part;
+    p.part = (int)((((int64_t)vocab + p.parts - 1) / p.parts + 7) / 8 * 8);
+    p.parts = (int)(((int64_t)vocab + p.part - 1) / p.part);
     return p;
 }
 struct LogScratch {
@@ -522,7 +523,7 @@ extern "C" {
 
 size_t sssd_op_logprobs_scratch_bytes(int32_t type, int32_t rows, int32_t vocab, int32_t n_tokens, int32_t n_top)
 {
-    if ((type != SSSD_F32 && type != SSSD_BF16) || rows <= 0 || vocab <= 0 || n_tokens < 0 || n_tokens > MOST_TOKENS || n_top < 0 || n_top > MOST_TOP || n_top > vocab) return 0;
+    if ((type != SSSD_F32 && type != SSSD_BF16) || rows <= 0 || vocab <= 0 || n_tokens < 0 || n_tokens > MOST_TOKENS || n_top < 0 || n_top > MOST_TOP || n_top > vocab || vocab > MOST_VOCAB) return 0;
     return log_scratch(rows, log_plan(rows, vocab), n_tokens, n_top).bytes;
 }
 
@@ -531,7 +532,7 @@ int sssd_op_logprobs(const void *logits, int32_t type, int32_t rows, int32_t voc
                      size_t scratch_bytes, void *stream)
 {
     if (!logits || (type != SSSD_F32 && type != SSSD_BF16) || rows <= 0 || vocab <= 0 || n_tokens < 0 || n_top < 0 || n_top > vocab) return SSSD_EINVAL;
-    if (n_tokens > MOST_TOKENS || n_top > MOST_TOP) return SSSD_ECAPACITY;
+    if (n_tokens > MOST_TOKENS || n_top > MOST_TOP || vocab > MOST_VOCAB) return SSSD_ECAPACITY;
     if ((n_tokens > 0 && (!tokens || !logprobs)) || (n_top > 0 && (!top_ids || !top_logprobs))) return SSSD_EINVAL;
     const bool bf16 = type == SSSD_BF16;
     if ((uintptr_t)logits % (bf16 ? 2 : 4) || (rows > 1 && row_stride < 0)) return SSSD_EINVAL;
