@@ -197,6 +197,7 @@ typedef struct {
     size_t ws_bytes;
 } sssd_kv8_pages;
 
+/* The calls take pools of up to 2^30 pages. */
 int sssd_kv8_pages_sizes(const sssd_kv8_config *cfg, size_t *ws_bytes);
 
 /*

@@ -16,6 +16,7 @@ namespace {
 
 constexpr int PT = 1024;   // threads of the workgroup that decides
 constexpr int PER = 4;     // neighbouring pages of a thread in a pass over the pool
+constexpr int MOST_PAGES = 1 << 30;   // places behind the last one are numbers, too
 
 // One per workspace.  `fault` and `delta` (behind it, a word per page) are zero before and after every call.
 struct PagesHead {
@@ -527,7 +528,7 @@ int check_pages(const sssd_kv8 *kv, const sssd_kv8_pages *p, Sizes8 &S, PagesArg
     if (rc) return rc;
     PagesSizes z;
     if (!pages_sizes(kv->cfg, S, z) || !p->workspace || (uintptr_t)p->workspace % ALIGN) return SSSD_EINVAL;
-    if (p->ws_bytes < z.bytes) return SSSD_ECAPACITY;
+    if (p->ws_bytes < z.bytes || S.n_pages > MOST_PAGES) return SSSD_ECAPACITY;
     a = PagesArgs{};
     a.g = geom(kv, S);
     a.slots = kv->cfg.max_batch;

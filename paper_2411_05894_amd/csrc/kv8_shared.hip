@@ -538,7 +538,7 @@ int sssd_kv8_attention_shared(const sssd_kv8 *kv, int32_t layer, int32_t B, int3
     a.part_o = (float *)workspace;
     a.part_ml = reinterpret_cast<f32x4 *>(a.part_o + (size_t)(p.segments + a.plan.share) * c.n_kv_heads * a.rows_all * c.head_dim);
     // workgroups of 256 threads
-    if (((int64_t)c.n_kv_heads * p.share + 7) / 8 * 8 * p.tiles > MOST_THREADS / 256 || ((int64_t)B * c.n_kv_heads + 7) / 8 * 8 * a.plan.share * a.plan.passes > MOST_THREADS / 256)
+    if (((int64_t)c.n_kv_heads * p.share + 7) / 8 * 8 * p.tiles + ((int64_t)B * c.n_kv_heads + 7) / 8 * 8 * a.plan.share * a.plan.passes > MOST_THREADS / 256)
         return SSSD_ECAPACITY;
     const int rt = (tiles + a.plan.passes - 1) / a.plan.passes;
     hipStream_t s = (hipStream_t)stream;

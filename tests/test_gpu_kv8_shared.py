@@ -182,6 +182,48 @@ def test_a_row_that_is_no_number_spoils_itself_alone():
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("sequences", [1, 2, 9, 40])
+def test_scores_of_every_magnitude(dtype, sequences):
+    """Neighbouring keys are a sixteenth of the largest apart, so with scores of 2^11 and more only the largest count, and these are equal: the mean of their values, wherever they
+    lie -- in the prefix, behind it, in both."""
+    d, prefix, own, n = 64, 160, 33, 2
+    for where in ("prefix", "own", "both"):
+        batch = Batch("e4m3", 4, 2, d, [(max(sequences, 2), prefix)], [own], n, alone=1 if sequences == 1 else 0, seed=11)
+        cache, B = batch.cache, batch.B
+        g = torch.Generator(device=DEV).manual_seed(12)
+        k = torch.zeros(B, prefix + own + n, 2, d, device=DEV)
+        steps = torch.randint(0, 8, (prefix + own + n,), generator=g, device=DEV).float()
+        top = {"prefix": [3, 77], "own": [prefix + 2, prefix + 30], "both": [5, prefix + 4]}[where]
+        steps[::32] = 8.0                                     # every block has the same scale
+        steps[top] = 9.0
+        k[..., 0] = (steps / 16.0 + 0.375)[None, :, None]
+        v = torch.randn(B, prefix + own + n, 2, d, generator=g, device=DEV)
+        v[:, :prefix] = v[:1, :prefix]
+        for first, end, lens in ((0, prefix, [0] * B), (prefix, prefix + own + n, batch.lens)):
+            at = [0] if first == 0 else list(range(B))
+            for b in at:
+                if first and batch.lens[b] < prefix:          # the one that shares nothing
+                    continue
+                cache.sssd_kv8_append(0, k[b:b + 1, first:end].contiguous(), v[b:b + 1, first:end].contiguous(), ints([first]), first=b)
+        kk, vv = (torch.zeros_like(k) for _ in range(2))
+        cache.sssd_kv8_read(0, None, ints([a + n for a in batch.lens]), kk, vv)
+        for size in (1e3, 1e6, 1e20, 1e34):
+            q = torch.zeros(B, n, 4, d, device=DEV)
+            q[..., 0] = torch.tensor([size, -size * 0.5, size * 3, size * 0.25], device=DEV)
+            q = q.to(dtype)
+            out = torch.full_like(q, 5.5)
+            batch.run(q, out)
+            for b in range(B):
+                if batch.lens[b] < prefix:
+                    continue
+                total = batch.lens[b] + n
+                want, mass, _ = attend(q[b], kk[b, :total].double(), vv[b, :total].double(), batch.lens[b])
+                bound = mass * 2.0 ** -20 + (want.abs() * 2.0 ** -8 + mass * 2.0 ** -10 if dtype == torch.bfloat16 else 0)
+                bad = (out[b].double() - want).abs() > bound
+                assert not bad.any(), (where, size, b, float(((out[b].double() - want).abs() / bound).max()))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_layouts(dtype):
     """Queries in the middle of a QKV product, outputs heads first, unaligned ones."""
     batch = Batch("int8", 8, 2, 64, [(6, 500), (2, 40)], [7, 90], 3, 1, layers=3)

@@ -59,7 +59,8 @@ def test_page_calls_refuse(call):
                 dict(kv=cache(block_table=None)), dict(kv=cache(block_table=PAGES_AT + 4)), dict(kv=cache(cache=None)), dict(kv=cache(cache=FAKE + 16)), dict(kv=cache(status=None)),
                 dict(kv=cache(flags=1))):
         assert call(**{**ok, **bad}) == SSSD_EINVAL, bad
-    for bad in (dict(kv=cache(cache_bytes=1)), dict(book=pages(ws_bytes=size_of() - 1))):
+    many = dict(n_pages=2 ** 30 + 1)
+    for bad in (dict(kv=cache(cache_bytes=1)), dict(book=pages(ws_bytes=size_of() - 1)), dict(kv=cache(**many), book=pages(ws_bytes=size_of(**many)))):
         assert call(**{**ok, **bad}) == SSSD_ECAPACITY, bad
 
 
