@@ -5,6 +5,7 @@ PyTorch fallback: a missing library is an ImportError."""
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import Dict, List, Optional, Sequence
 
@@ -346,26 +347,40 @@ def sssd_op_sample_wide(logits: torch.Tensor, sampling: SamplingParams, uniforms
     return out
 
 
+LOGIT_TYPES = {torch.float32: 0, torch.bfloat16: 1}
+
+
+@functools.lru_cache(maxsize=256)
+def sssd_op_logprobs_scratch_bytes(kind: int, rows: int, vocab: int, m: int, n_top: int) -> int:
+    return lib().sssd_op_logprobs_scratch_bytes(kind, rows, vocab, m, n_top)
+
+
 def sssd_op_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, n_top: int = 0, temperature: float = 1.0):
     """logits [rows][vocab], float32 or bfloat16, any distance between rows; tokens int32 [rows][m] or None -> (logprobs [rows][m], ranks [rows][m],
     entropy [rows], top_ids [rows][n_top], top_logprobs [rows][n_top]).  Outputs and scratch are allocated here."""
     rows, vocab = logits.shape
-    device = logits.device
-    kind = {torch.float32: 0, torch.bfloat16: 1}.get(logits.dtype)
-    assert kind is not None and device.type == "cuda" and (logits.stride(1) == 1 or vocab == 1), "float32 or bfloat16 rows on a GPU"
+    stride, place, device = logits.stride(), logits.device, logits.get_device()
+    kind = LOGIT_TYPES.get(logits.dtype)
+    assert kind is not None and device >= 0 and (stride[1] == 1 or vocab == 1), "float32 or bfloat16 rows on a GPU"
     m = 0
     if tokens is not None:
-        assert tokens.dtype == torch.int32 and tokens.dim() == 2 and tokens.shape[0] == rows and tokens.device == device and tokens.is_contiguous()
+        assert tokens.dtype is torch.int32 and tokens.dim() == 2 and tokens.shape[0] == rows and tokens.get_device() == device and tokens.is_contiguous()
         m = tokens.shape[1]
-    with torch.cuda.device(device):
-        logprobs, entropy = torch.empty(rows, m, device=device), torch.empty(rows, device=device)
-        top_logprobs = torch.empty(rows, n_top, device=device)
-        ranks, top_ids = (torch.empty(rows, k, dtype=torch.int32, device=device) for k in (m, n_top))
-        nbytes = lib().sssd_op_logprobs_scratch_bytes(kind, rows, vocab, m, n_top)
-        scratch = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=device)
-        _check(lib().sssd_op_logprobs(logits.data_ptr(), kind, rows, vocab, logits.stride(0), temperature, _ptr(tokens), m, _ptr(logprobs), _ptr(ranks),
-                                      _ptr(entropy), n_top, _ptr(top_ids), _ptr(top_logprobs), _ptr(scratch), nbytes, _stream()), "sssd_op_logprobs")
-    return logprobs, ranks, entropy, top_ids, top_logprobs
+    if torch._C._cuda_getDevice() != device:
+        with torch.cuda.device(device):
+            return sssd_op_logprobs(logits, tokens, n_top, temperature)
+    f32, i32 = torch.float32, torch.int32
+    logprobs, ranks = torch.empty((rows, m), dtype=f32, device=place), torch.empty((rows, m), dtype=i32, device=place)
+    entropy = torch.empty(rows, dtype=f32, device=place)
+    ids, top = torch.empty((rows, n_top), dtype=i32, device=place), torch.empty((rows, n_top), dtype=f32, device=place)
+    nbytes = sssd_op_logprobs_scratch_bytes(kind, rows, vocab, m, n_top)
+    scratch = torch.empty(nbytes, dtype=torch.uint8, device=place) if nbytes else None
+    code = lib().sssd_op_logprobs(logits.data_ptr(), kind, rows, vocab, stride[0], temperature, tokens.data_ptr() if m else None, m, logprobs.data_ptr(), ranks.data_ptr(),
+                                  entropy.data_ptr(), n_top, ids.data_ptr(), top.data_ptr(), scratch.data_ptr() if nbytes else None, nbytes,
+                                  torch._C._cuda_getCurrentRawStream(device))
+    if code:
+        _check(code, "sssd_op_logprobs")
+    return logprobs, ranks, entropy, ids, top
 
 
 def sssd_op_gemm_small_step_rows() -> int:
