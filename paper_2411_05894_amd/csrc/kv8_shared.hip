@@ -323,83 +323,118 @@ template <int HD, int FMT, int RT, int PARTS> __device__ __forceinline__ void pr
     }
 }
 
-// A wave per row of the batch.
-template <int HD> __global__ __launch_bounds__(256) void kv8_shared_merge_kernel(Kv8SharedArgs a)
+// The partial results of ROWS rows r0 .. (below r_end) of a (sequence, kv head), by one wave: lanes 16s .. 16s+15 take segments s, s+4, ... with HD/16 channels each, U of them in one
+// round of independent loads.  MANY: in several rounds.
+template <int HD, int ROWS, int U, bool MANY> __device__ __forceinline__ void join_rows(const Kv8SharedArgs &a, int b, int kvh, int r0, int r_end, int n_pre, int n_seg, int lane)
 {
-    constexpr int E = HD / 16, U = 4;
-    const int R = a.n * a.gq, nkv = a.g.nkv, lane = threadIdx.x & 63;
+    constexpr int E = HD / 16;
+    const int sg = lane >> 4, cl = lane & 15, each = a.n * a.gq;
+    auto slot = [&](int s, int i) { return shared_slot(a, s < n_pre ? s : a.prefix_segments + s - n_pre, kvh, b * each + min(r0 + i, r_end - 1)); };
+    float m_all[ROWS], v_all[ROWS], den[ROWS], num[ROWS][E];   // v_all: the unit of the sums, that of the segment with the largest
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        m_all[i] = v_all[i] = NONE;
+        den[i] = 0.f;
+        if (MANY)
+            for (int s = lane; s < n_seg; s += 64) {
+                const f32x4 x = a.part_ml[slot(s, i)];
+                m_all[i] = fmaxf(m_all[i], x[0]);
+                v_all[i] = fmaxf(v_all[i], x[2]);
+            }
+#pragma unroll
+        for (int e = 0; e < E; ++e) num[i][e] = 0.f;
+    }
+    for (int base = 0; base < (MANY ? n_seg : 1); base += 4 * U) {
+        f32x4 ml[ROWS][U], pv[ROWS][U][E / 4];
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i)
+#pragma unroll
+            for (int u = 0; u < U; ++u) {   // past the last segment: that one again, not added
+                const size_t at = slot(min(base + 4 * u + sg, n_seg - 1), i);
+                ml[i][u] = a.part_ml[at];
+#pragma unroll
+                for (int e = 0; e < E; e += 4) pv[i][u][e / 4] = *reinterpret_cast<const f32x4 *>(a.part_o + at * HD + cl * E + e);
+            }
+        if (base == 0) {
+#pragma unroll
+            for (int i = 0; i < ROWS; ++i) {
+                if (!MANY) {
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        m_all[i] = fmaxf(m_all[i], ml[i][u][0]);
+                        v_all[i] = fmaxf(v_all[i], ml[i][u][2]);
+                    }
+                    m_all[i] = rows_max(m_all[i]);
+                    v_all[i] = rows_max(v_all[i]);
+                } else {
+#pragma unroll
+                    for (int x = 32; x > 0; x >>= 1) {
+                        m_all[i] = fmaxf(m_all[i], __shfl_xor(m_all[i], x));
+                        v_all[i] = fmaxf(v_all[i], __shfl_xor(v_all[i], x));
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i)
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const bool on = base + 4 * u + sg < n_seg;
+                const float w = on ? __builtin_amdgcn_exp2f(ml[i][u][0] - m_all[i]) : 0.f, wv = __builtin_ldexpf(w, (int)(ml[i][u][2] - v_all[i]));
+                den[i] = on ? __builtin_fmaf(w, ml[i][u][1], den[i]) : den[i];
+#pragma unroll
+                for (int e = 0; e < E; ++e) num[i][e] = on ? __builtin_fmaf(wv, pv[i][u][e / 4][e % 4], num[i][e]) : num[i][e];
+            }
+    }
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        den[i] = rows_sum(den[i]);
+        const float inv = den[i] != 0.f ? 1.f / den[i] : 0.f;
+        if (r0 + i >= r_end) continue;
+        const RowOut o(r0 + i, a.gq, kvh);
+        char *to = a.out.at(b, o.j, o.head);
+#pragma unroll
+        for (int e = 0; e < E; e += 4) {
+            f32x4 y;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) y[x] = __builtin_ldexpf(rows_sum(num[i][e + x]) * inv, (int)v_all[i] - 127);
+            if (sg == e / 4) store4(a.out, to, cl * E + e, y);
+        }
+    }
+}
+
+// ROWS rows of a (sequence, kv head) to a wave: four where there are rows enough to fill the chip all the same.  us, four / one: 32 sequences of 4 rows of 70B, five segments, 6.2 / 10.3.
+template <int HD, int ROWS> __global__ __launch_bounds__(256) void kv8_shared_merge_kernel(Kv8SharedArgs a)
+{
+    const int each = a.n * a.gq, chunks = (each + ROWS - 1) / ROWS, nkv = a.g.nkv, lane = threadIdx.x & 63;
     const uint32_t task = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
-    const uint32_t head_of = task / (uint32_t)R;
-    const int r = (int)(task - head_of * R), b = (int)(head_of / (uint32_t)nkv), kvh = (int)(head_of - (uint32_t)b * nkv);
+    const uint32_t head_of = task / (uint32_t)chunks;
+    const int r0 = (int)(task - head_of * chunks) * ROWS, b = (int)(head_of / (uint32_t)nkv), kvh = (int)(head_of - (uint32_t)b * nkv);
     if (b >= a.B) return;
     int len, count;
     bool ok = kv8_rows(a.lens, a.counts, b, a.n, a.g.max_seq, len, count), sane;
     const Group g = group_of(a, b, lane, sane);
     ok = ok && len >= g.blocks * KV8_BLOCK;
-    const int sg = lane >> 4, cl = lane & 15;
-    const RowOut o(r, a.gq, kvh);
-    char *to = a.out.at(b, o.j, o.head);
     if (!ok) {
-#pragma unroll
-        for (int e = 0; e < E; e += 4)
-            if (sg == e / 4) store4(a.out, to, cl * E + e, f32x4{0.f, 0.f, 0.f, 0.f});
+        for (int i = lane; i < ROWS * (HD / 4); i += 64) {
+            const int r = r0 + i / (HD / 4);
+            const RowOut o(r, a.gq, kvh);
+            if (r < each) store4(a.out, a.out.at(b, o.j, o.head), i % (HD / 4) * 4, f32x4{0.f, 0.f, 0.f, 0.f});
+        }
         return;
     }
-    if (r >= count * a.gq) return;
+    const int r_end = count * a.gq;
+    if (r0 >= r_end) return;
     const int n_pre = g.blocks ? prefix_cut(a, g.blocks).n : 0;
     const int n_seg = n_pre + cut_of(((len + count + 31) >> 5) - g.blocks, a.plan.share).n;
-    const int row = b * R + r;
-    auto slot = [&](int s) { return shared_slot(a, s < n_pre ? s : a.prefix_segments + s - n_pre, kvh, row); };
-    float m_all = NONE, v_all = NONE, den = 0.f, num[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) num[e] = 0.f;
-    const bool many = n_seg > 4 * U;
-    if (many)
-        for (int s = lane; s < n_seg; s += 64) {
-            const f32x4 x = a.part_ml[slot(s)];
-            m_all = fmaxf(m_all, x[0]);
-            v_all = fmaxf(v_all, x[2]);
+    if (n_seg <= 4) join_rows<HD, ROWS, 1, false>(a, b, kvh, r0, r_end, n_pre, n_seg, lane);
+    else if (n_seg <= 8) join_rows<HD, ROWS, 2, false>(a, b, kvh, r0, r_end, n_pre, n_seg, lane);
+    else
+        for (int r = r0; r < min(r0 + ROWS, r_end); ++r) {
+            if (n_seg <= 16) join_rows<HD, 1, 4, false>(a, b, kvh, r, r + 1, n_pre, n_seg, lane);
+            else if (n_seg <= 32) join_rows<HD, 1, 8, false>(a, b, kvh, r, r + 1, n_pre, n_seg, lane);
+            else join_rows<HD, 1, 8, true>(a, b, kvh, r, r + 1, n_pre, n_seg, lane);
         }
-    for (int base = 0; base < n_seg; base += 4 * U) {
-        f32x4 ml[U], pv[U][E / 4];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {   // past the last segment: that one again, not added
-            const size_t at = slot(min(base + 4 * u + sg, n_seg - 1));
-            ml[u] = a.part_ml[at];
-#pragma unroll
-            for (int e = 0; e < E; e += 4) pv[u][e / 4] = *reinterpret_cast<const f32x4 *>(a.part_o + at * HD + cl * E + e);
-        }
-        if (base == 0) {
-            if (!many)
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    m_all = fmaxf(m_all, ml[u][0]);
-                    v_all = fmaxf(v_all, ml[u][2]);
-                }
-#pragma unroll
-            for (int x = 32; x > 0; x >>= 1) {
-                m_all = fmaxf(m_all, __shfl_xor(m_all, x));
-                v_all = fmaxf(v_all, __shfl_xor(v_all, x));
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const bool on = base + 4 * u + sg < n_seg;
-            const float w = on ? __builtin_amdgcn_exp2f(ml[u][0] - m_all) : 0.f, wv = __builtin_ldexpf(w, (int)(ml[u][2] - v_all));
-            den = on ? __builtin_fmaf(w, ml[u][1], den) : den;
-#pragma unroll
-            for (int e = 0; e < E; ++e) num[e] = on ? __builtin_fmaf(wv, pv[u][e / 4][e % 4], num[e]) : num[e];
-        }
-    }
-    den = rows_sum(den);
-    const float inv = den != 0.f ? 1.f / den : 0.f;
-#pragma unroll
-    for (int e = 0; e < E; e += 4) {
-        f32x4 y;
-#pragma unroll
-        for (int x = 0; x < 4; ++x) y[x] = __builtin_ldexpf(rows_sum(num[e + x]) * inv, (int)v_all - 127);
-        if (sg == e / 4) store4(a.out, to, cl * E + e, y);
-    }
 }
 
 // Both kinds of workgroups in one launch, those of prefixes first: they take longest, and the others fill in behind them.  RTP: row tiles of a wave of a prefix; FEW: its waves
@@ -442,7 +477,9 @@ template <int HD, int FMT, int PARTS> hipError_t launch_shared(Kv8SharedArgs a, 
 #undef KV8_SHARED
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kv8_shared_merge_kernel<HD>, dim3(((uint32_t)a.rows_all * a.g.nkv + 3) / 4), dim3(256), 0, s, a);
+    const uint32_t each = a.n * a.gq, heads = (uint32_t)a.B * a.g.nkv;
+    if ((uint64_t)heads * each >= 8192) hipLaunchKernelGGL((kv8_shared_merge_kernel<HD, 4>), dim3((heads * ((each + 3) / 4) + 3) / 4), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((kv8_shared_merge_kernel<HD, 1>), dim3((heads * each + 3) / 4), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 template <int HD> hipError_t launch_format(const Kv8SharedArgs &a, int fmt, int rt_prefix, int rt, hipStream_t s)
@@ -477,7 +514,7 @@ Kv8SharedPlan kv8_shared_plan(int B, int n, int gq, int nkv, int blocks, int gro
     double best = 0;
     p.share = 1;
     for (int64_t s = 1; s <= 64 && s * units <= KV8_GROUPS && (s - 1) * sub * 4 < blocks; ++s) {
-        const double cost = std::ceil((double)blocks / (s * sub)) * (s * units <= 256 ? 0.65 : 0.975) + s * sub * (double)rows * nkv * 2.64e-4;
+        const double cost = std::ceil((double)blocks / (s * sub)) * (s * units <= 256 ? 0.65 : 0.975) + s * sub * ((double)rows * nkv * 2.64e-4 + 0.04);
         if (s == 1 || cost < best) {
             best = cost;
             p.share = (int)s;
