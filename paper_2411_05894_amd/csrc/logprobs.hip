@@ -153,10 +153,15 @@ template <bool BF16, bool WHOLE> __global__ __launch_bounds__(LT) __attribute__(
     const uint32_t empty = BF16 ? 0xFF80FF80u : 0xFF800000u;   // -infinity
     u32x4 raw[V];
     auto request = [&](int first) {   // vectors from there on
+        if (first + V * LT <= vecs) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) raw[i] = from[first + i * LT + (int)threadIdx.x];
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             raw[i] = u32x4{empty, empty, empty, empty};
-            if (first + i * LT + (int)threadIdx.x < vecs) raw[i] = from[first + i * LT + threadIdx.x];
+            if (first + i * LT + (int)threadIdx.x < vecs) raw[i] = from[first + i * LT + (int)threadIdx.x];
         }
     };
     request(0);
@@ -223,7 +228,8 @@ template <bool BF16, bool WHOLE> __global__ __launch_bounds__(LT) __attribute__(
 #pragma unroll
             for (int i = 0; i < N; ++i) top = fmaxf(top, z[i]);
         }
-        const float here = bits_f32((uint32_t)__builtin_amdgcn_readfirstlane((int)f32_bits(wave_max(top))));
+        const bool holds = __any(top >= most);   // hardly any chunk but the first
+        const float here = holds ? bits_f32((uint32_t)__builtin_amdgcn_readfirstlane((int)f32_bits(wave_max(top)))) : most;
         if (here > most) {
             if (equal) {   // those that were the largest join the others
                 const float x = (most - ref) * a.k, e = __builtin_amdgcn_exp2f(x) * (float)equal;
@@ -257,8 +263,8 @@ template <bool BF16, bool WHOLE> __global__ __launch_bounds__(LT) __attribute__(
                 if (decltype(counting)::value) before0 += lanes_of(z[i] > (first + i / PER * LT * PER + G <= token0 ? below0 : v0));
             }
         };
-        const bool counts = here >= v0 && v0 > -INFINITY;
-        if (here == most && most > -INFINITY) {
+        const bool counts = v0 > -INFINITY && __any(top >= v0);
+        if (holds && most > -INFINITY) {
             if (counts) sums(std::true_type(), std::true_type());
             else sums(std::true_type(), std::false_type());
         } else {
@@ -277,7 +283,7 @@ template <bool BF16, bool WHOLE> __global__ __launch_bounds__(LT) __attribute__(
                     const float o = ordered(z[i]);
                     n += lanes_of(id_of(i) < end && (o > v || id_of(i) < token));
                 }
-            } else if (here >= v) {
+            } else if (__any(top >= v)) {
                 if (j > 0) {
                     const float below = next_below(v);
 #pragma unroll
@@ -308,7 +314,7 @@ template <bool BF16, bool WHOLE> __global__ __launch_bounds__(LT) __attribute__(
                 }
             }
         }
-        if (here >= least)
+        if (__any(top >= least))
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 if (!__any(z[i] >= least || least == -INFINITY)) continue;
@@ -323,7 +329,7 @@ template <bool BF16, bool WHOLE> __global__ __launch_bounds__(LT) __attribute__(
                 if (take) list[listed + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0))] = key;
                 listed += (int)__popcll(who);
             }
-        if (listed > n_top / 2 + 48) cut();   // so that the next chunks have fewer to list
+        if (listed > n_top + n_top / 4) cut();   // so that the next chunks have fewer to list
     };
     {
         // the ends are chunks of one logit a lane: before and behind the others
