@@ -252,11 +252,14 @@ struct Kv8SharedArgs : Kv8AttnArgs {   // of a batch whose sequences share prefi
     int prefix_share;      // workgroups on a prefix at most
     int prefix_groups;     // workgroups of a launch that are on prefixes
     int prefix_segments;   // segments of a prefix at most: prefix_share * 4 / wave_rows
+    int prefix_once;       // as many while compute units have one workgroup each; 0: they have more
+    float prefix_cost;     // us that a segment more takes, blocks apart
     int rows_all;          // B * n * gq
 };
 Kv8Plan kv8_plan(int B, int n, int gq, int nkv, int blocks, bool f32);   // blocks: of a sequence at most
 struct Kv8SharedPlan {
-    int rt, wave_rows, tiles, share, segments;   // row tiles of a wave; the others as in Kv8SharedArgs
+    int rt, wave_rows, tiles, share, segments, once;   // row tiles of a wave; the others as in Kv8SharedArgs
+    float cost;
 };
 Kv8SharedPlan kv8_shared_plan(int B, int n, int gq, int nkv, int blocks, int groups, bool f32);   // blocks: of a sequence at most
 size_t kv8_shared_ws(int B, int n, int gq, int nkv, int d);

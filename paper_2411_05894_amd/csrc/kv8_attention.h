@@ -257,7 +257,7 @@ __device__ __forceinline__ bool group_round(const Kv8SharedArgs &a, int round, i
     const int i = round * 64 + lane, at = min(i, a.groups - 1);
     const int from = a.starts[at], to = a.starts[at + 1], shared = a.shared[at];
     const bool ok = from >= 0 && to >= from && to <= a.B && shared >= 0 && shared <= a.g.max_seq;
-    g = Group{from, i < a.groups ? to - from : 0, shared >> 5};
+    g = Group{from, ok && i < a.groups ? to - from : 0, shared >> 5};
     if (g.n < 2 || g.blocks == 0) g = Group{from, 0, 0};   // a sequence alone shares with nobody
     return !__any(!ok);
 }
@@ -284,39 +284,68 @@ __device__ __forceinline__ Group group_of(const Kv8SharedArgs &a, int b, int lan
     }
     return ok ? mine : Group{b, 1, 0};
 }
-// The group that tile `tile` of all groups' rows, `rows` to a tile, belongs to; tile: within the group then.  n = 0: none.
-__device__ __forceinline__ Group group_of_tile(const Kv8SharedArgs &a, int &tile, int rows, int lane)
+// The segments of a shared prefix of some blocks: as many as cost least of the two numbers that are best with one workgroup to a compute unit and with two, a block taking PREFIX_BLOCK us
+// there and half as much again here; at least four blocks each.  The kernels that make and join them have the same answer, with nothing contracted.
+constexpr float PREFIX_BLOCK = 0.65f, PREFIX_BLOCK_TWO = 0.975f;
+__device__ __forceinline__ Cut prefix_cut(const Kv8SharedArgs &a, int blocks)
 {
-    Group mine{0, 0, 0};
-    int before = 0, at = tile;
+#pragma clang fp contract(off)
+    auto up = [](int x, int y) { return (int)(((unsigned)x + (unsigned)y - 1u) / (unsigned)y); };
+    auto each_of = [&](int most, float block) {   // blocks of a segment
+        const int best = (int)__builtin_ceilf(__builtin_amdgcn_sqrtf((float)blocks * (a.prefix_cost / block)));
+        return max(max(up(blocks, most), best), 4);
+    };
+    int each = each_of(a.prefix_segments, PREFIX_BLOCK_TWO), n = up(blocks, each);
+    if (a.prefix_once > 0) {
+        const int one = each_of(a.prefix_once, PREFIX_BLOCK), n_one = up(blocks, one);
+        if (n <= a.prefix_once || (float)one * PREFIX_BLOCK + (float)n_one * a.prefix_cost <= (float)each * PREFIX_BLOCK_TWO + (float)n * a.prefix_cost) {
+            each = one;
+            n = n_one;
+        }
+    }
+    return Cut{each, n};
+}
+
+// What a workgroup on a prefix has: tile `tile` of the group's rows, `rows` to a tile, and its number `pair` among the kv heads of the first segments, the second, ...
+struct PrefixTask {
+    Group g;   // n = 0: nothing
+    Cut cut;
+    int tile, pair;
+};
+// The group's workgroups lie next to each other, tile by tile in whole eights, those of one pair on one die: they read the same blocks.  Workgroups that find nothing come last: in between,
+// some compute units had three of those that do, and others one.  sub: segments of a workgroup
+__device__ __forceinline__ PrefixTask prefix_task(const Kv8SharedArgs &a, uint32_t bid, int rows, int sub, int lane)
+{
+    PrefixTask mine{{0, 0, 0}, {0, 0}, 0, 0};
+    const int slot = (int)(bid >> 3);
+    int before = 0;
     bool ok = true;
     for (int r = 0; r * 64 < a.groups; ++r) {
         Group g;
         ok = group_round(a, r, lane, g) && ok;
+        const Cut cut = prefix_cut(a, max(g.blocks, 1));
         const int tiles = (int)(((unsigned)g.n * (unsigned)(a.n * a.gq) + (unsigned)rows - 1u) / (unsigned)rows);
-        int upto = tiles;
+        const int eights = ((cut.n + sub - 1) / sub * a.g.nkv + 7) >> 3, slots = tiles * eights;
+        int upto = slots;
 #pragma unroll
         for (int x = 1; x < 64; x <<= 1) {
             const int y = __shfl_up(upto, x);
             if (lane >= x) upto += y;
         }
         const int end = before + upto;
-        const uint64_t has = __ballot(tile < end && tile >= end - tiles);
+        const uint64_t has = __ballot(slot < end && slot >= end - slots);
         if (has) {
             const int l = __ffsll((long long)has) - 1;
-            mine = Group{__builtin_amdgcn_readlane(g.first, l), __builtin_amdgcn_readlane(g.n, l), __builtin_amdgcn_readlane(g.blocks, l)};
-            at = tile - __builtin_amdgcn_readlane(end - tiles, l);
+            const int at = slot - __builtin_amdgcn_readlane(end - slots, l), per = __builtin_amdgcn_readlane(eights, l);
+            mine.g = Group{__builtin_amdgcn_readlane(g.first, l), __builtin_amdgcn_readlane(g.n, l), __builtin_amdgcn_readlane(g.blocks, l)};
+            mine.cut = Cut{__builtin_amdgcn_readlane(cut.each, l), __builtin_amdgcn_readlane(cut.n, l)};
+            mine.tile = at / per;
+            mine.pair = (at - mine.tile * per) * 8 + (int)(bid & 7);
         }
         before += __builtin_amdgcn_readlane(upto, 63);
     }
-    tile = at;
-    return ok ? mine : Group{0, 0, 0};
-}
-// The segments of a shared prefix, at least four blocks each.
-__device__ __forceinline__ Cut prefix_cut(const Kv8SharedArgs &a, int blocks)
-{
-    const int each = max((int)(((unsigned)blocks + (unsigned)a.prefix_segments - 1u) / (unsigned)a.prefix_segments), 4);
-    return Cut{each, (int)(((unsigned)blocks + (unsigned)each - 1u) / (unsigned)each)};
+    if (!ok) mine.g.n = 0;
+    return mine;
 }
 // Where the partial result of a row of the batch lies: prefixes' segments first.
 __device__ __forceinline__ size_t shared_slot(const Kv8SharedArgs &a, int segment, int kvh, int row) { return ((size_t)segment * a.g.nkv + kvh) * a.rows_all + row; }
@@ -356,21 +385,20 @@ __device__ __forceinline__ void attend_group(const Kv8Args<MODE> &a, AttnShared<
     const int q = lane >> 4, c = lane & 15;
     int pass, segment, b, kvh;
     int skip = 0, n_rows = 0;   // blocks that are another workgroup's; rows of a group
+    Cut prefix{1, 1};
     if constexpr (PRE) {
-        // workgroups of one (kv head, segment) on one die: they read the same blocks; tiles that no group has come last
-        const uint32_t slot = bid >> 3, pairs = ((uint32_t)nkv * a.prefix_share + 7) >> 3, x = slot / pairs, pair = (slot - x * pairs) * 8 + (bid & 7);
-        int tile = (int)x;
-        segment = (int)(pair / (uint32_t)nkv);
-        kvh = (int)pair - segment * nkv;
-        if (segment >= a.prefix_share) return;
         const int slabs = a.wave_rows, slab = wave & (slabs - 1);
-        const Group g = group_of_tile(a, tile, slabs * RT * 16, lane);
-        if (g.n == 0) return;
-        b = g.first;
-        skip = g.blocks;
-        n_rows = g.n * a.n * a.gq;
-        segment = segment * (NW / slabs) + wave / slabs;
-        pass = tile * slabs + slab;
+        const PrefixTask task = prefix_task(a, bid, slabs * RT * 16, NW / slabs, lane);
+        segment = (int)((uint32_t)task.pair / (uint32_t)nkv);
+        kvh = task.pair - segment * nkv;
+        segment = segment * (NW / slabs);
+        if (task.g.n == 0 || segment >= task.cut.n) return;
+        segment += wave / slabs;
+        b = task.g.first;
+        skip = task.g.blocks;
+        n_rows = task.g.n * a.n * a.gq;
+        pass = task.tile * slabs + slab;
+        prefix = task.cut;
     } else {
         const uint32_t slot = bid >> 3, x = slot / (uint32_t)passes, row = x / (uint32_t)share;
         pass = (int)(slot - x * passes);
@@ -442,7 +470,7 @@ __device__ __forceinline__ void attend_group(const Kv8Args<MODE> &a, AttnShared<
     if constexpr (MODE == KV8_BEHIND) span = Span{0, skip, span.n - skip};
     if constexpr (PRE) span = Span{0, 0, skip};
     Cut cut = cut_of(span.n, share);
-    if constexpr (PRE) cut = prefix_cut(a, span.n);
+    if constexpr (PRE) cut = prefix;
     if (!PRE && segment >= cut.n) return;
     // blocks of a wave: first + off, and every STEP-th behind it
     constexpr int STEP = PRE ? 1 : NW;

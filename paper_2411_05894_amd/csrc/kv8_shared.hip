@@ -3,9 +3,15 @@
 // Mathematics.  softmax over prefix and own rows is joined from partial results (m, l, o) as in kv8_attention.h: a prefix has one per row and segment, the rows
 // behind it (the sequence's own ones and the new ones) one per segment of theirs; with M the largest m, l = sum 2^(m - M) l, o likewise, out = o / l.
 //
-// Split.  The rows of all sequences of a group, side by side, are the queries of its prefix, and all see all of it: no masks.  A wave takes up to three tiles of
-// 16 of them over its segment's blocks; four waves of a workgroup have different rows and read the same blocks, from the first one's cache lines, or, where a group has few
-// rows, different segments.  What lies behind the prefix goes as sequences do alone, and a last launch joins both.
+// Split.  The rows of all sequences of a group, side by side, are the queries of its prefix, and all see all of it: no masks.  A wave takes one or two tiles of
+// 16 of them over its segment's blocks; four waves of a workgroup have different rows and share the blocks' operands in LDS or, where a group has few rows, are on different segments,
+// as a sequence's alone.  What lies behind the prefix goes as sequences do alone, in the same launch, and a last one joins both.
+//
+// What bounds it.  us, kernels of this / of the call for sequences alone: 64 sequences of one row on 32768 positions (8B, bf16) 62 + 10 / 301, 35 GFLOP, of which a
+// large product takes 26; two prompts of 4096 and 8192 with 32 rows of 70B on each 52 + 10 / 68; 20 sequences of one row on 4096 14.5 + 4.3 / 20.6; 4 on 2048 8.3 + 4.3 / 9.0;
+// eight of 9 rows on 2048 20.7 + 5.2 / 20.4; 32 on 512 12.8 + 4.1 / 8.4.  With many rows, matrix instructions are under way for 55 % of the loop's time, exponentials, conversions and what is
+// read of LDS for the rest; around it 5 to 6 us until the first operands are there, and the partial results, 35 MB out and in for the 64 sequences.  Few rows and short
+// prefixes: that start and the second launch, 4 us at least.
 #include "kv8_attention.h"
 #include "kv8_host.h"
 
@@ -14,8 +20,9 @@
 
 namespace {
 
-// Many rows: four waves of a workgroup with up to three row tiles each on the same blocks.  A block's codes are requested two blocks ahead, a quarter by each wave,
-// turned into float16 operands once for all four and handed round in LDS (two blocks of room, one barrier a block); queries stay in registers.
+// Many rows: four waves of a workgroup with one or two row tiles each on the same blocks.  Codes are requested two pairs of blocks ahead, a quarter by each wave,
+// turned into float16 operands once for all four and handed round in LDS (two pairs of room, one barrier a pair); queries stay in registers.  Three tiles do not fit the registers
+// of two waves on a SIMD (92 us instead of 62 for the 64 sequences), nor do two of float32 queries, which are twice the operands.
 //
 // V's scales: the unit of the sums is the largest of the segment, known before the first block.  Where all of them lie within V_SPAN octaves, codes are converted in that unit, which
 // float16 holds exactly (down to 2^-21 for 8-bit floats, 2^-12 for integers); else blocks are multiplied as they are, with probabilities relative to the
@@ -32,17 +39,12 @@ template <int HD, int FMT, int RT, int PARTS> __device__ __forceinline__ void pr
     auto &ring = sh.ring;
     const int nkv = a.g.nkv;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, q = lane >> 4, c = lane & 15;
-    // Workgroups of one (kv head, segment) on one die: they read the same blocks.  Tiles that no group has come last: in between, workgroups that end at once
-    // had some compute units get three of those that do not, and others one.
-    const uint32_t slot = bid >> 3, pairs = ((uint32_t)nkv * a.prefix_share + 7) >> 3, x0 = slot / pairs, pair = (slot - x0 * pairs) * 8 + (bid & 7);
-    int tile = (int)x0;
-    const int segment = (int)(pair / (uint32_t)nkv), kvh = (int)pair - segment * nkv;
-    if (segment >= a.prefix_share) return;
-    const Group g = group_of_tile(a, tile, 4 * RT * 16, lane);
-    if (g.n == 0) return;
+    const PrefixTask task = prefix_task(a, bid, 4 * RT * 16, 1, lane);
+    const Group g = task.g;
+    const Cut cut = task.cut;
+    const int tile = task.tile, segment = (int)((uint32_t)task.pair / (uint32_t)nkv), kvh = task.pair - segment * nkv;
+    if (g.n == 0 || segment >= cut.n) return;
     const int each = a.n * a.gq, rows = g.n * each, row0 = (tile * 4 + wave) * RT * 16;
-    const Cut cut = prefix_cut(a, g.blocks);
-    if (segment >= cut.n) return;
     const int first = segment * cut.each, n_it = min(cut.each, g.blocks - first);
     const bool mine = row0 < rows;
 
@@ -403,7 +405,8 @@ template <int HD, int ROWS, int U, bool MANY> __device__ __forceinline__ void jo
     }
 }
 
-// ROWS rows of a (sequence, kv head) to a wave: four where there are rows enough to fill the chip all the same.  us, four / one: 32 sequences of 4 rows of 70B, five segments, 6.2 / 10.3.
+// ROWS rows of a (sequence, kv head) to a wave: four where there are rows enough to fill the chip all the same.  us, four / one: 32 sequences of
+// 4 rows of 70B, five segments, 8.9 / 10.3.
 template <int HD, int ROWS> __global__ __launch_bounds__(256) void kv8_shared_merge_kernel(Kv8SharedArgs a)
 {
     const int each = a.n * a.gq, chunks = (each + ROWS - 1) / ROWS, nkv = a.g.nkv, lane = threadIdx.x & 63;
@@ -490,11 +493,11 @@ template <int HD> hipError_t launch_format(const Kv8SharedArgs &a, int fmt, int 
 
 }  // namespace
 
-// Row tiles of a wave, and how many workgroups go over a prefix, for groups that are all alike.  Few rows: a workgroup's waves are on different segments.  Else, with s workgroups to
+// Row tiles of a wave, and how many workgroups go over a prefix at most, for groups that are all alike and prefixes as long as they can be; shorter ones take fewer (prefix_cut).  Few rows: a workgroup's waves are on different segments.  Else, with s workgroups to
 // a row tile and prefix, about
 //     blocks / s * (0.65 us, or half as much again where compute units have two of them) + s * rows * nkv * 264 us, for 528 bytes of partial results a row, out and in, at 4 TB/s
-// us, by that / as many as the chip holds: best of eight with 9 rows on 2048 positions 31 / 37, two prompts of 70B 61 / 64, 32 sequences of 4 rows on 2000 of 70B 41 / 49, 64 of one on
-// 32768 and 16 of 9 on 4096 the same.  More workgroups than find something to do hold those that lie behind them up by some 3 us.
+// and 0.04 us a segment for what the joining of it takes.  us, by that / as many as the chip holds: best of eight with 9 rows on 2048 positions 31 / 37, 32 sequences of 4 rows on 2000
+// of 70B 41 / 49, two prompts of 70B 64 / 64, 64 of one on 32768 and 16 of 9 on 4096 the same.  More workgroups than find something to do hold those that lie behind them up by some 3 us.
 Kv8SharedPlan kv8_shared_plan(int B, int n, int gq, int nkv, int blocks, int groups, bool f32)
 {
     Kv8SharedPlan p{};
@@ -511,16 +514,19 @@ Kv8SharedPlan kv8_shared_plan(int B, int n, int gq, int nkv, int blocks, int gro
     p.tiles = (int)((rows + per - 1) / per + std::max(groups, 1) - 1);
     const int64_t units = (each + per - 1) / per * (groups > 0 ? groups : 1) * nkv;
     const int sub = 4 / p.wave_rows;   // segments of a workgroup
+    const double segment_cost = (double)rows * nkv * 2.64e-4 + 0.04;
     double best = 0;
     p.share = 1;
     for (int64_t s = 1; s <= 64 && s * units <= KV8_GROUPS && (s - 1) * sub * 4 < blocks; ++s) {
-        const double cost = std::ceil((double)blocks / (s * sub)) * (s * units <= 256 ? 0.65 : 0.975) + s * sub * ((double)rows * nkv * 2.64e-4 + 0.04);
+        const double cost = std::ceil((double)blocks / (s * sub)) * (s * units <= 256 ? 0.65 : 0.975) + s * sub * segment_cost;
         if (s == 1 || cost < best) {
             best = cost;
             p.share = (int)s;
         }
     }
     p.segments = p.share * sub;
+    p.once = (int)std::min<int64_t>(p.share, 256 / units) * sub;
+    p.cost = (float)segment_cost;
     return p;
 }
 
@@ -571,6 +577,8 @@ int sssd_kv8_attention_shared(const sssd_kv8 *kv, int32_t layer, int32_t B, int3
     const Kv8SharedPlan p = kv8_shared_plan(B, n, a.gq, c.n_kv_heads, S.blocks_per_seq, groups, !a.q.bf16);
     a.groups = groups; a.starts = starts; a.shared = shared;
     a.tiles = p.tiles; a.wave_rows = p.wave_rows; a.prefix_share = p.share; a.prefix_segments = p.segments;
+    a.prefix_once = p.once;
+    a.prefix_cost = p.cost;
     a.rows_all = B * n * a.gq;
     a.part_o = (float *)workspace;
     a.part_ml = reinterpret_cast<f32x4 *>(a.part_o + (size_t)(p.segments + a.plan.share) * c.n_kv_heads * a.rows_all * c.head_dim);
