@@ -174,7 +174,7 @@ int sssd_kv8_commit_tree(const sssd_kv8 *kv, int32_t B, int32_t n, int32_t *lens
  *   starts      device int32 [groups + 1], ascending from >= 0 to <= B
  *   shared      device int32 [groups], 0 .. max_seq
  *   workspace   device, 256-byte aligned, any contents, at least what sssd_kv8_shared_sizes asks for this B and n (a larger B or n asks
- *               for more); calls that share it must be ordered.  kv's own workspace is not used
+ *               for more); calls that share it must be ordered, as those of one kv, whose own workspace is used too
  * starts or shared out of range raise the status, and nothing is shared in that call.  A sequence shorter than its group's shared blocks is rejected
  * like the others (sssd_kv8_attention).  Pages outside the pool among a prefix's blocks raise the status and spoil the rows of the group.
  */

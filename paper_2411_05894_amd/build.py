@@ -10,7 +10,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsssd_verify.so")
 DRIVER = os.path.join(HERE, "step_driver")
 SOURCES = ["api.hip", "attention.hip", "elementwise.hip", "stream_gemm.hip", "sampling.hip", "kv8_api.hip", "kv8_store.hip", "kv8_attention.hip", "kv8_shared.hip",
-           "kv8_pages.hip", "logprobs.hip", "drafter.cpp"]
+           "kv8_apart.hip", "kv8_pages.hip", "logprobs.hip", "drafter.cpp"]
 import shlex
 FLAGS = shlex.split(os.environ.get("SSSD_EXTRA_HIPCC_FLAGS", "")) + ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wextra",
          # packed-fp32 VALU forms are kept off on the test machines

@@ -260,8 +260,10 @@ Kv8Plan kv8_plan(int B, int n, int gq, int nkv, int blocks, bool f32);   // bloc
 struct Kv8SharedPlan {
     int rt, wave_rows, tiles, share, segments, once;   // row tiles of a wave; the others as in Kv8SharedArgs
     float cost;
+    double us;             // what a call takes, about, for prefixes as long as they can be
 };
 Kv8SharedPlan kv8_shared_plan(int B, int n, int gq, int nkv, int blocks, int groups, bool f32);   // blocks: of a sequence at most
 size_t kv8_shared_ws(int B, int n, int gq, int nkv, int d);
 size_t kv8_attention_ws(int d);   // bytes behind the workspace that any call's partial results take
+hipError_t launch_kv8_apart(Kv8SharedArgs a, int fmt, int d, void *ws, hipStream_t s);
 hipError_t launch_kv8_attention(Kv8AttnArgs a, int fmt, int d, void *ws, hipStream_t s);

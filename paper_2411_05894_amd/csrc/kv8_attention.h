@@ -350,8 +350,9 @@ __device__ __forceinline__ PrefixTask prefix_task(const Kv8SharedArgs &a, uint32
 // Where the partial result of a row of the batch lies: prefixes' segments first.
 __device__ __forceinline__ size_t shared_slot(const Kv8SharedArgs &a, int segment, int kvh, int row) { return ((size_t)segment * a.g.nkv + kvh) * a.rows_all + row; }
 
-// What a workgroup goes over: the blocks of a sequence, a sequence's blocks behind what its group shares, or blocks that a group shares.
-enum Kv8Mode : int { KV8_ALONE, KV8_BEHIND, KV8_PREFIX };
+// What a workgroup goes over: the blocks of a sequence, the same with those that its group shares read through the table of the first, a sequence's blocks behind what its group shares, or
+// blocks that a group shares.
+enum Kv8Mode : int { KV8_ALONE, KV8_APART, KV8_BEHIND, KV8_PREFIX };
 template <int MODE> using Kv8Args = std::conditional_t<MODE == KV8_ALONE, Kv8AttnArgs, Kv8SharedArgs>;
 
 // PARTS: the query operand is float16 (1: bf16 queries) or float16 hi + lo (2: float32 queries), and so are the probabilities.
@@ -442,9 +443,12 @@ __device__ __forceinline__ void attend_group(const Kv8Args<MODE> &a, AttnShared<
     }
     int up = lane - 1;
     if (!PRE && a.parents && lane < a.n) up = a.parents[(size_t)b * a.n + lane];
-    if constexpr (MODE == KV8_BEHIND) {
+    int front = b;   // the sequence whose table has the first `skip` blocks
+    if constexpr (MODE == KV8_BEHIND || MODE == KV8_APART) {
         bool sane;
-        skip = group_of(a, b, lane, sane).blocks;
+        const Group g = group_of(a, b, lane, sane);
+        skip = g.blocks;
+        front = g.first;
         if (!sane && bid == 0 && threadIdx.x == 0) atomicOr(a.status, KV8_RANGE);
         if (len < skip * KV8_BLOCK) ok = false;   // shorter than what it is said to share
     }
@@ -486,7 +490,7 @@ __device__ __forceinline__ void attend_group(const Kv8Args<MODE> &a, AttnShared<
     auto look = [&](int chunk) {
         const int i = min(first + off + STEP * (64 * chunk + lane), span.n - 1);
         Ahead x;
-        const int entry = kv8_entry(a.g, b, span.block(i));
+        const int entry = kv8_entry(a.g, MODE == KV8_APART && span.block(i) < skip ? front : b, span.block(i));
         const int page = min(max(entry, 0), a.g.n_pages - 1);
         if (entry != page && kvh == 0 && pass == 0) atomicOr(a.status, KV8_RANGE);
         x.record = page * nkv + kvh;
@@ -842,7 +846,7 @@ __device__ __forceinline__ void attend_group(const Kv8Args<MODE> &a, AttnShared<
                 for (int x = 0; x < QT; ++x) y[x] += (i ? part(wave, w, t, x) : own[t][x]) * fv;
             }
             if (row >= rows) continue;
-            if (MODE == KV8_ALONE && cut.n == 1) {
+            if ((MODE == KV8_ALONE || MODE == KV8_APART) && cut.n == 1) {
                 const RowOut ro(row, a.gq, kvh);
                 const float inv = l_all != 0.f ? 1.f / l_all : 0.f;   // a row that sees nothing: 0
                 char *to = a.out.at(b, ro.j, ro.head);
@@ -862,7 +866,7 @@ __device__ __forceinline__ void attend_group(const Kv8Args<MODE> &a, AttnShared<
             }
         }
     }
-    if (MODE != KV8_ALONE || cut.n == 1 || !a.hand.words) return;
+    if (MODE == KV8_BEHIND || cut.n == 1 || !a.hand.words) return;
     const int group = (b * nkv + kvh) * passes + pass;
     HandWay way = hand_wait(a.hand, group, cut.n, hand_arrive(a.hand, group), &way_s);
     if (way == HAND_TURN_IN) way = hand_turn_in(a.hand, group, cut.n, &way_s);
@@ -886,13 +890,6 @@ __device__ __forceinline__ void attend_group(const Kv8Args<MODE> &a, AttnShared<
     }
     if (way != HAND_SHARE) left = hand_leave(a.hand, group);
     hand_clear(a.hand, group, cut.n, left);
-}
-
-template <int HD, int FMT, int RT, int PARTS, int NW>
-__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void kv8_attn_kernel(Kv8AttnArgs a)
-{
-    __shared__ AttnShared<HD, RT, PARTS, NW, KV8_ALONE> sh;
-    attend_group<HD, FMT, RT, PARTS, NW, KV8_ALONE>(a, sh, blockIdx.x);
 }
 
 }  // namespace

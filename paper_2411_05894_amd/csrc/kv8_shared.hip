@@ -5,7 +5,8 @@
 //
 // Split.  The rows of all sequences of a group, side by side, are the queries of its prefix, and all see all of it: no masks.  A wave takes one or two tiles of
 // 16 of them over its segment's blocks; four waves of a workgroup have different rows and share the blocks' operands in LDS or, where a group has few rows, are on different segments,
-// as a sequence's alone.  What lies behind the prefix goes as sequences do alone, in the same launch, and a last one joins both.
+// as a sequence's alone.  What lies behind the prefix goes as sequences do alone, in the same launch, and a last one joins both.  Where that would take longer than every sequence by itself
+// (apart_us), they go by themselves, the shared blocks read through the first one's table (kv8_apart.hip).
 //
 // What bounds it.  us, kernels of this / of the call for sequences alone: 64 sequences of one row on 32768 positions (8B, bf16) 62 + 10 / 301, 35 GFLOP, of which a
 // large product takes 26; two prompts of 4096 and 8192 with 32 rows of 70B on each 52 + 10 / 68; 20 sequences of one row on 4096 14.5 + 4.3 / 20.6; 4 on 2048 8.3 + 4.3 / 9.0;
@@ -524,10 +525,21 @@ Kv8SharedPlan kv8_shared_plan(int B, int n, int gq, int nkv, int blocks, int gro
             p.share = (int)s;
         }
     }
+    p.us = 18 + best;
     p.segments = p.share * sub;
     p.once = (int)std::min<int64_t>(p.share, 256 / units) * sub;
     p.cost = (float)segment_cost;
     return p;
+}
+
+// The same of a call whose sequences go by themselves: a block takes a workgroup so much, by row tiles, and a fifth more where sequences are cut into segments.  For f32 and bf16, prefixes of 512 to 32768 positions, groups of 4 to 32
+// sequences, 1 to 32 rows of 8B and 70B, whichever of both is said to be the lesser took 0.5 % longer than whichever was, all going by themselves 9.6 % longer, none 22 %.
+// us, by themselves / sharing: 32 of 9 rows of 8B bf16 512 18.9 / 33.4, 2048 34.9 / 45.4, 8192 90.9 / 74.1, 32768 311 / 196, f32 21.3 / 35.5, 39.7 / 51.4, 102 / 111, 355 / 368; 8 of one row
+// 16.8 / 19.1, 17.1 / 19.9, 30.8 / 23.8, 83.7 / 36.3.  Like the plans it goes by how long sequences can be.
+static double apart_us(int64_t heads, int tiles, int blocks, bool f32, const Kv8Plan &p)
+{
+    static const double block[2][KV8_MAX_TILES + 1] = {{0, 0.20, 0.24, 0.29}, {0, 0.22, 0.24, 0.33}};
+    return 13 + (double)blocks / p.share * block[f32][(tiles + p.passes - 1) / p.passes] * std::max(1.0, heads * p.passes * p.share / 256.0) * (p.share > 1 ? 1.2 : 1.0);
 }
 
 // For every number of groups: a prefix's results are at most those of KV8_GROUPS workgroups of 4 * KV8_MAX_TILES row tiles or, where there are more workgroups than that, four a
@@ -559,10 +571,12 @@ int sssd_kv8_attention_shared(const sssd_kv8 *kv, int32_t layer, int32_t B, int3
     int rc = check_cache(kv, layer, S);
     if (rc) return rc;
     const sssd_kv8_config &c = kv->cfg;
-    if (!lens || B <= 0 || n <= 0 || groups < 0 || (groups > 0 && (!starts || !shared)) || !workspace || (uintptr_t)workspace % ALIGN) return SSSD_EINVAL;
+    if (!lens || B <= 0 || n <= 0 || groups < 0 || (groups > 0 && (!starts || !shared)) || !workspace || (uintptr_t)workspace % ALIGN || !kv->workspace ||
+        (uintptr_t)kv->workspace % ALIGN)
+        return SSSD_EINVAL;
     size_t need = 0;
     if ((rc = sssd_kv8_shared_sizes(&c, B, n, &need))) return rc;
-    if (groups > B || ws_bytes < need) return SSSD_ECAPACITY;
+    if (groups > B || ws_bytes < need || kv->ws_bytes < S.ws_bytes) return SSSD_ECAPACITY;
     Kv8SharedArgs a{};
     if ((rc = make_rows(q, B, n, c.n_q_heads, a.q)) || (rc = make_rows(out, B, n, c.n_q_heads, a.out))) return rc;
     if (a.q.bf16 != a.out.bf16) return SSSD_EINVAL;
@@ -576,6 +590,12 @@ int sssd_kv8_attention_shared(const sssd_kv8 *kv, int32_t layer, int32_t B, int3
     a.rows_pad = tiles * 16;
     const Kv8SharedPlan p = kv8_shared_plan(B, n, a.gq, c.n_kv_heads, S.blocks_per_seq, groups, !a.q.bf16);
     a.groups = groups; a.starts = starts; a.shared = shared;
+    hipStream_t s = (hipStream_t)stream;
+    if ((groups == 0 || apart_us((int64_t)B * c.n_kv_heads, tiles, S.blocks_per_seq, !a.q.bf16, a.plan) <= p.us) && (int64_t)B * c.n_q_heads <= MOST_THREADS / (32 * 256)) {
+        a.hand.polls = kv->flags & SSSD_NO_WAIT ? 0 : HAND_POLLS;
+        HIP_TRY(launch_kv8_apart(a, c.format, c.head_dim, kv->workspace, s));
+        return SSSD_OK;
+    }
     a.tiles = p.tiles; a.wave_rows = p.wave_rows; a.prefix_share = p.share; a.prefix_segments = p.segments;
     a.prefix_once = p.once;
     a.prefix_cost = p.cost;
@@ -586,7 +606,6 @@ int sssd_kv8_attention_shared(const sssd_kv8 *kv, int32_t layer, int32_t B, int3
     if (((int64_t)c.n_kv_heads * p.share + 7) / 8 * 8 * p.tiles + ((int64_t)B * c.n_kv_heads + 7) / 8 * 8 * a.plan.share * a.plan.passes > MOST_THREADS / 256)
         return SSSD_ECAPACITY;
     const int rt = (tiles + a.plan.passes - 1) / a.plan.passes;
-    hipStream_t s = (hipStream_t)stream;
     HIP_TRY(c.head_dim == 128 ? launch_format<128>(a, c.format, p.rt, rt, s) : launch_format<64>(a, c.format, p.rt, rt, s));
     return SSSD_OK;
 }

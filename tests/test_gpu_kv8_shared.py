@@ -13,6 +13,14 @@ from paper_2411_05894_amd import kv8
 from paper_2411_05894_amd.binding import SSSD_ENOSPACE, SSSD_OK, SssdError
 
 DEV = "cuda:0"
+LONGER = 0      # positions that a sequence could have beyond what the batch needs
+
+
+@pytest.fixture(autouse=True, params=["as long as they are", "room for more"])
+def room(request):
+    """How long sequences can be decides whether short prefixes are read for all rows of a group at once or by each sequence: both have to be right."""
+    global LONGER
+    LONGER = 0 if request.param == "as long as they are" else 200000
 
 
 def ints(v):
@@ -36,8 +44,8 @@ class Batch:
         self.own = [own[b % len(own)] for b in range(B)]
         self.lens = [a + b for a, b in zip(front, self.own)]
         self.counts = counts or [n] * B
-        max_seq = max(self.lens) + n + extra
-        per = (max_seq + 31) // 32
+        longest = max(self.lens) + n + extra
+        max_seq = longest + LONGER
         pages = sum((p + 31) // 32 for _, p in groups) + sum((a + n + 31) // 32 + 1 for a in self.own) + 3
         self.cache = kv8.Kv8Cache(layers, nq, nkv, d, B, max_seq, fmt, n_pages=pages, device=DEV)
         self.book = kv8.Kv8Pages(self.cache)
@@ -69,7 +77,7 @@ class Batch:
         assert self.cache.sssd_kv8_sync() == SSSD_OK
         self.starts, self.shared = starts, [p for _, p in groups]
         self.q = torch.randn(B, n, nq, d, generator=g, device=DEV)
-        held = [torch.zeros(B, max_seq, nkv, d, device=DEV) for _ in range(2)]
+        held = [torch.zeros(B, longest, nkv, d, device=DEV) for _ in range(2)]
         self.cache.sssd_kv8_read(self.layer, None, ints([a + c for a, c in zip(self.lens, self.counts)]), *held)
         self.held = held
         self.workspace = self.cache.sssd_kv8_shared_workspace(B, n)

@@ -23,6 +23,14 @@ def test_registers_of_the_shared_attention(tmp_path):
         assert registers <= 256 and scratch <= allowed, (k, registers, spilled, scratch)
 
 
+def test_registers_of_sequences_by_themselves(tmp_path):
+    """As those of a batch that shares nothing: two waves a SIMD, nothing in scratch memory."""
+    found = {k: v for k, v in kernels("kv8_apart", tmp_path).items() if "kv8_attn_kernel" in k}
+    assert len(found) == 2 * 2 * 2 * 3 + 2 * 2 * 2
+    for k, (registers, spilled, scratch) in found.items():
+        assert registers <= 256 and spilled == 0 and scratch == 0, (k, registers, spilled, scratch)
+
+
 def test_registers_of_log_probabilities(tmp_path):
     """Six workgroups of four waves on a compute unit: 1536 rows at once."""
     found = {k: v for k, v in kernels("logprobs", tmp_path).items() if "logprob_kernel" in k}
@@ -44,7 +52,7 @@ def test_host_code_is_clean_under_asan_and_ubsan():
     out = os.path.join(OUT, "more")
     os.makedirs(out, exist_ok=True)
     jobs = [(HIP + ["-c", os.path.join(CSRC, src)], os.path.join(out, src + ".o"))
-            for src in ("kv8_shared.hip", "kv8_attention.hip", "kv8_store.hip", "kv8_api.hip", "kv8_pages.hip", "logprobs.hip")]
+            for src in ("kv8_shared.hip", "kv8_apart.hip", "kv8_attention.hip", "kv8_store.hip", "kv8_api.hip", "kv8_pages.hip", "logprobs.hip")]
     jobs.append((HIP + ["-c", os.path.join(ROOT, "tests", "sanitize", "more_san.hip")], os.path.join(out, "more_san.o")))
     with ThreadPoolExecutor(max_workers=4) as ex:
         objs = list(ex.map(_compile, jobs))
