@@ -8,7 +8,9 @@
  * (the last accepted token and n-1 drafts, a chain or a tree):
  *   sssd_kv8_append     rotate the new K rows, quantise K and V into the cache, rotate the queries
  *   sssd_kv8_attention  every new row's attention over the cached rows it sees
- * and after acceptance, once for all layers, sssd_kv8_commit_tree.
+ * and after acceptance, once for all layers, sssd_kv8_commit_tree.  Where sequences continue one another (several answers
+ * to a prompt, many users behind a system prompt), sssd_kv8_fork makes them, sssd_kv8_reserve gives the next rows room of
+ * their own, sssd_kv8_attention_shared reads what they share once, and sssd_kv8_compact closes a pool's holes.
  *
  * Stored values.  Positions are kept in blocks of 32, a page each (of one sequence, all kv heads).  A
  * block's K of one kv head, and its V, have one scale each, a power of two: with A the largest finite
@@ -167,7 +169,7 @@ int sssd_kv8_commit_tree(const sssd_kv8 *kv, int32_t B, int32_t n, int32_t *lens
 /* ----------------------------------------------------------------- prefixes that sequences share -- */
 /*
  * sssd_kv8_attention for a batch whose sequences share prefixes: the same rows and results (but for the order of sums), without a window,
- * each prefix read once for all rows of its group.  Sequences of a group lie next to each other: group g is the slots starts[g] ..
+ * each prefix read once for all rows of its group, or by each sequence where that is the faster way for sequences of up to max_seq positions.  Sequences of a group lie next to each other: group g is the slots starts[g] ..
  * starts[g+1]-1 below B, and the first shared[g] positions of all of them are the same rows.  They are read, in whole blocks
  * (shared[g] / 32 of them), through the block table's row of the group's first sequence, whose other state plays no part.
  *   groups      0 .. B; sequences in no group, groups of one and empty groups share nothing

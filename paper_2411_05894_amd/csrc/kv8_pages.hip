@@ -7,8 +7,8 @@
 // A call is all or nothing.  It is planned first (fork_plan_kernel adds the differences up beside the references, reserve_kernel and compact_kernel look
 // everything over), one workgroup decides, and only then are table, references and pages written.
 //
-// What bounds it: the pages that are copied, in all layers, at the rate of a copy (1100 pages of 64 KiB in 7 layers, 1.05 GB out and in, 203 us of a kernel, 5.2 TB/s); without many, the
-// launches and the one workgroup's round trips.  us of kernels: 64 slots of 70B forked from three prompts, 3.6 + 4.2 for the plan and the decision, 6.3 for copies and table; room for 9 rows
+// What bounds it: the pages that are copied, in all layers, at the rate of a copy (1001 pages of 64 KiB in 8 layers, 1.05 GB out and in, 201 us of a kernel, 5.2 TB/s); without many, the
+// launches and the one workgroup's round trips.  us of kernels: 64 slots forked from four prompts, 3.5 + 4.5 for the plan and the decision, 9.6 for table and 31 pages in 16 layers; room for 9 rows
 // of 16 sequences 7.9, for prompts of up to 4001 17, and 3.4 to 5.1 for the copies behind it.  One workgroup decides since the others would wait for each other's counts: a launch
 // apiece is what that would cost, and a pool's references are read by one in rounds of 4096.
 #include "kv8_host.h"

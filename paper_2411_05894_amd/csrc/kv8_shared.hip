@@ -8,10 +8,10 @@
 // as a sequence's alone.  What lies behind the prefix goes as sequences do alone, in the same launch, and a last one joins both.  Where that would take longer than every sequence by itself
 // (apart_us), they go by themselves, the shared blocks read through the first one's table (kv8_apart.hip).
 //
-// What bounds it.  us, kernels of this / of the call for sequences alone: 64 sequences of one row on 32768 positions (8B, bf16) 62 + 10 / 301, 35 GFLOP, of which a
-// large product takes 26; two prompts of 4096 and 8192 with 32 rows of 70B on each 52 + 10 / 68; 20 sequences of one row on 4096 14.5 + 4.3 / 20.6; 4 on 2048 8.3 + 4.3 / 9.0;
-// eight of 9 rows on 2048 20.7 + 5.2 / 20.4; 32 on 512 12.8 + 4.1 / 8.4.  With many rows, matrix instructions are under way for 55 % of the loop's time, exponentials, conversions and what is
-// read of LDS for the rest; around it 5 to 6 us until the first operands are there, and the partial results, 35 MB out and in for the 64 sequences.  Few rows and short
+// What bounds it.  us, kernels of this / of the call for sequences alone: 64 sequences of one row on 32768 positions (8B, bf16) 62 + 10 / 301, 35 GFLOP, for which a
+// large product takes 26; 70B, 17 sequences of 5 rows on 4000 positions and 9 on 2000 48 + 8 / 68; 20 sequences of one row of 8B on 4096 14.5 + 4.3 / 20.6; 4 on 2048 8.3 + 4.3 / 9.0;
+// eight of 9 rows on 2048 20.7 + 5.2 / 20.4; 32 of one on 512 12.8 + 4.1 / 8.4.  With many rows, matrix instructions are under way for 55 % of the loop's time (30 % of the
+// kernel's), exponentials, conversions and what is read of LDS for the rest; around it 5 to 6 us until the first operands are there, and the partial results, 35 MB out and in for the 64 sequences.  Few rows and short
 // prefixes: that start and the second launch, 4 us at least.
 #include "kv8_attention.h"
 #include "kv8_host.h"

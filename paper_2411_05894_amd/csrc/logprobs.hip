@@ -9,7 +9,7 @@
 // changes it), how many come before each given token, and a list of its most probable tokens: what is above the last of n in a list that was full, at first above the n-th largest of its lanes'
 // largest logits.  Parts leave all that in memory, and a second launch joins them.  The order of sums is fixed.
 //
-// What bounds it: nine instructions a logit, an exponential among them, and in their shadow the reading.  us: 1501 rows of 128256, one token with its rank and one alternative,
+// What bounds it: fourteen instructions a logit, an exponential among them, and in their shadow the reading.  us: 1501 rows of 128256, one token with its rank and one alternative,
 // bf16 104 (3.7 TB/s), float32 148 (5.2 TB/s, as fast as a copy); bf16 without the token 91, without the alternative 93, without both 78; 20 alternatives 144.  9 rows: 8.6 and 6.3 for the joining,
 // both round trips behind one another.
 #include "../../include/sssd_ops.h"
