@@ -10,7 +10,7 @@ pytestmark = pytest.mark.gpu
 
 from kv8_reference import attend
 from paper_2411_05894_amd import kv8
-from paper_2411_05894_amd.binding import SSSD_ENOSPACE, SSSD_OK, SssdError
+from paper_2411_05894_amd.binding import SSSD_ENOSPACE, SSSD_NO_WAIT, SSSD_OK, SssdError
 
 DEV = "cuda:0"
 LONGER = 0      # positions that a sequence could have beyond what the batch needs
@@ -298,6 +298,21 @@ def test_workspaces():
         batch.run(batch.q, torch.empty_like(batch.q))
     batch.workspace = torch.full((batch.cache.sssd_kv8_shared_workspace(4, 3).numel() // 4,), float("nan"), device=DEV)      # any contents
     batch.check(torch.float32)
+
+
+@pytest.mark.parametrize("n", [1, 9])
+def test_segments_joined_without_waiting(n):
+    """The same bits, whoever joins a sequence's segments; and what the call leaves behind in the cache's own workspace serves plain attention."""
+    batch = Batch("e4m3", 32, 8, 128, [(4, 2000), (3, 640)], [30, 200], n, 1)
+    a = batch.check(torch.float32)
+    batch.cache.args.flags = SSSD_NO_WAIT
+    b = batch.check(torch.float32)
+    batch.cache.args.flags = 0
+    assert torch.equal(a, b) and torch.equal(a, batch.check(torch.float32))
+    plain = torch.full_like(a, 5.5)
+    batch.cache.sssd_kv8_attention(0, batch.q, ints(batch.lens), plain)
+    for i in range(batch.B):
+        batch.compare(i, batch.q, plain)
 
 
 def test_replays_and_streams():
