@@ -9,7 +9,7 @@
 //
 // What bounds it: the pages that are copied, in all layers, at the rate of a copy (1001 pages of 64 KiB in 8 layers, 1.05 GB out and in, 201 us of a kernel, 5.2 TB/s); without many, the
 // launches and the one workgroup's round trips.  us of kernels: 64 slots forked from four prompts, 3.5 + 4.5 for the plan and the decision, 9.6 for table and 31 pages in 16 layers; room for 9 rows
-// of 16 sequences 7.9, for prompts of up to 4001 17, and 3.4 to 5.1 for the copies behind it.  One workgroup decides since the others would wait for each other's counts: a launch
+// of 16 sequences 7.9, for prompts of up to 4001 12, and 3.4 to 5.1 for the copies behind it.  One workgroup decides since the others would wait for each other's counts: a launch
 // apiece is what that would cost, and a pool's references are read by one in rounds of 4096.
 #include "kv8_host.h"
 
@@ -271,8 +271,9 @@ __global__ __launch_bounds__(256) void fork_write_kernel(PagesArgs a, CopyArgs c
 }
 
 // ---------------------------------------------------------------------------------------------------------- reserve ----
-// One workgroup: the blocks that the call's rows touch, slot by slot, a thread each, in as many rounds as they take.  One round is the rule (a step's rows): then what a thread has
-// read stays with it.
+// One workgroup: the blocks that the call's rows touch, slot by slot, a thread each, in as many rounds as they take.  What a thread has read stays with it for up to KEEP rounds
+// (1885 blocks of prompts 12 us of kernel, 17 when only one round is kept).
+constexpr int KEEP = 3;
 struct Asked {
     bool on, bad, live;   // live: rows that live are in the block
     int slot, blk, page, refs;
@@ -305,7 +306,7 @@ __global__ __launch_bounds__(PT) void reserve_kernel(PagesArgs a)
         __syncthreads();
         return total;
     };
-    auto block = [&](int base, int k, int total) {
+    auto entry = [&](int base, int k, int total) {
         Asked x{k < total, false, false, 0, 0, -1, 0};
         if (!x.on) return x;
         int lo = 0, hi = PT - 1;   // the last sequence that begins at or before k: it has blocks
@@ -318,23 +319,39 @@ __global__ __launch_bounds__(PT) void reserve_kernel(PagesArgs a)
         x.blk = (len_s[lo] >> 5) + k - off_s[lo];
         x.live = (int64_t)x.blk * 32 < len_s[lo];
         x.page = a.table[place(x.slot, x.blk)];
+        return x;
+    };
+    auto counted = [&](Asked &x) {
         x.bad = x.page < -1 || x.page >= a.g.n_pages;
         x.refs = x.bad || x.page < 0 ? 0 : a.refs[x.page];
         x.bad = x.bad || (x.page >= 0 && x.refs <= 0);
-        return x;
     };
     int total = a.B <= PT ? sequences(0) : 0;
-    const bool one = a.B <= PT && total <= PT;
-    const Asked mine = block(0, threadIdx.x, one ? total : 0);
+    const bool kept = a.B <= PT && total <= KEEP * PT;
+    Asked mine[KEEP];
+#pragma unroll
+    for (int r = 0; r < KEEP; ++r) {
+        mine[r] = Asked{false, false, false, 0, 0, -1, 0};
+        if (kept && r * PT < total) mine[r] = entry(0, r * PT + (int)threadIdx.x, total);
+    }
+#pragma unroll
+    for (int r = 0; r < KEEP; ++r)
+        if (kept && r * PT < total) counted(mine[r]);
     // f(what is asked) for all blocks in order, the same number of times in every thread
     auto all = [&](auto f) {
-        if (one) {
-            f(mine);
+        if (kept) {
+#pragma unroll
+            for (int r = 0; r < KEEP; ++r)
+                if (r * PT < total) f(mine[r]);
             return;
         }
         for (int base = 0; base < a.B; base += PT) {
             if (a.B > PT) total = sequences(base);
-            for (int r = 0; r < total; r += PT) f(block(base, r + threadIdx.x, total));
+            for (int r = 0; r < total; r += PT) {
+                Asked x = entry(base, r + threadIdx.x, total);
+                counted(x);
+                f(x);
+            }
             __syncthreads();
         }
     };

@@ -327,3 +327,55 @@ def test_no_call_allocates():
         pool.book.sssd_kv8_compact()
     torch.cuda.synchronize()
     assert torch.cuda.mem_get_info()[0] == free
+
+
+@pytest.mark.parametrize("slots,max_seq", [(4, 200), (4, 40000), (1024, 128), (1024, 129), (1025, 96)])
+def test_forks_of_few_and_many_entries(slots, max_seq):
+    """Few slots and as many as the deciding workgroup has threads, or more, rows of one block and of more than a workgroup's run; and what is refused."""
+    rng = random.Random(slots + max_seq)
+    pool = Pool(slots, max_seq, 3 * slots + 40, layers=1, nkv=1)
+    lens = [rng.randint(0, min(max_seq, 70)) for _ in range(slots)]
+    lens[0], lens[1] = 70, 33
+    pool.reserve(70, [0] * slots, lens)
+    pool.lens = list(lens)
+    pool.d_lens.copy_(ints(lens))
+    origins = [rng.choice([-1, b, rng.randrange(slots)]) for b in range(slots)]
+    origins[-1] = origins[2] = 1
+    assert pool.fork(origins) is not None
+    assert pool.fork([b if rng.random() < 0.8 else rng.randrange(slots) for b in range(slots)]) is not None
+    state = pool.table, pool.refs, pool.lens
+    live = next(b for b in range(slots) if pool.lens[b] > 32)
+    for row, block, value in ((live, 0, -2 ** 31), (live, 1, -1), (live, 0, 2 ** 31 - 1), (slots - 1, pool.per - 1, -2 ** 31), (0, pool.per - 1, -2)):
+        spoiled = [list(r) for r in state[0]]
+        spoiled[row][block] = value
+        pool.set(spoiled, state[1], state[2])
+        assert pool.fork([live if b == 0 else b for b in range(slots)]) is None, (row, block, value)
+    for row, origin in ((0, slots), (slots - 1, -2), (1, 2 ** 31 - 1), (2, -2 ** 31)):
+        pool.set(*state)
+        assert pool.fork([origin if b == row else b for b in range(slots)]) is None, (row, origin)
+    for length in (-1, -2 ** 31, max_seq + 1, 2 ** 31 - 1):
+        pool.set(state[0], state[1], [length if b == live else n for b, n in enumerate(state[2])])
+        assert pool.fork(list(range(slots))) is None, length
+    pool.set(*state)
+    assert pool.fork(list(range(slots))[::-1]) is not None
+
+
+@pytest.mark.parametrize("blocks", [1, 1023, 1024, 1025, 2048, 2049, 3071, 3072, 3073, 4200])
+def test_reserves_of_many_blocks(blocks):
+    """As many blocks as a round of the workgroup has threads, as it keeps, and more; some of them shared, some in place already."""
+    slots = 5
+    each = (blocks + slots - 1) // slots
+    pool = Pool(slots, 32 * each + 64, blocks + 40, layers=1, nkv=1)
+    counts = [32 * min(each, max(0, blocks - b * each)) for b in range(slots)]
+    pool.reserve(9, [0], [9])
+    pool.lens[0] = 9
+    pool.d_lens.copy_(ints(pool.lens))
+    assert pool.fork([0] * slots) is not None                     # slots 1 .. 4 have a block of their own for 9 rows
+    pool.lens = [min(n, c) // 2 for n, c in zip(pool.lens, counts)]
+    assert sum(ref.blocks(a + c) - a // 32 for a, c in zip(pool.lens, counts)) >= blocks
+    assert pool.reserve(32 * each, pool.lens, counts) is not None
+    pool.lens = [a + c for a, c in zip(pool.lens, counts)]
+    pool.d_lens.copy_(ints(pool.lens))
+    assert pool.fork([0, 0] + list(range(2, slots))) is not None
+    pool.lens[:2] = [0, 0]
+    assert pool.reserve(32 * each, [0] * slots, [min(counts[0], 64), counts[0], 0, 5, 0]) is not None
