@@ -99,6 +99,7 @@ int sssd_op_sample_wide(const float *logits, int32_t rows, int32_t vocab, const 
 /*
  * Log-probabilities under softmax(logits / temperature), row by row, in one pass over the logits; natural logarithms, float32.
  *   logits     device [rows][vocab], SSSD_F32 or SSSD_BF16, rows row_stride >= 0 elements apart; vocab <= 2^30
+ *   temperature  1e-38 .. 1e36
  *   tokens     device int32 [rows][n_tokens], n_tokens <= SSSD_LOGPROBS_MAX_TOKENS; NULL for none
  *   logprobs   device out [rows][n_tokens]; -infinity for a token outside 0 .. vocab-1
  *   ranks      device int32 out [rows][n_tokens] or NULL: how many tokens come before it, by logit descending, then id ascending; -1

@@ -9,8 +9,8 @@
 // changes it), how many come before each given token, and a list of its most probable tokens: what is above the last of n in a list that was full, at first above the n-th largest of its lanes'
 // largest logits.  Parts leave all that in memory, and a second launch joins them.  The order of sums is fixed.
 //
-// What bounds it: fourteen instructions a logit, an exponential among them, and in their shadow the reading.  us: 1501 rows of 128256, one token with its rank and one alternative,
-// bf16 104 (3.7 TB/s), float32 148 (5.2 TB/s, as fast as a copy); bf16 without the token 91, without the alternative 93, without both 78; 20 alternatives 144.  9 rows: 8.6 and 6.3 for the joining,
+// What bounds it: thirteen instructions a logit, an exponential among them, and in their shadow the reading.  us: 1501 rows of 128256, one token with its rank and one alternative,
+// bf16 95 (4.0 TB/s; 104 with (z - r) k in two roundings), float32 148 (5.2 TB/s, as fast as a copy); bf16 without the token 84, without the alternative 86, without both 76; 20 alternatives 137.  9 rows: 8.6 and 6.3 for the joining,
 // both round trips behind one another.
 #include "../../include/sssd_ops.h"
 #include "common.h"
@@ -26,6 +26,7 @@ constexpr int MOST_TOKENS = SSSD_LOGPROBS_MAX_TOKENS, MOST_TOP = SSSD_LOGPROBS_M
 static_assert(LIST >= MOST_TOP + 64);
 constexpr int MOST_VOCAB = 1 << 30;         // places behind the last token are numbers, too
 constexpr float FAR = 4.f;                  // octaves of probability that M may be away from r
+constexpr float MOST_OFF = 0x1p20f;         // r k beyond that is rounded by more than a sixteenth of an octave
 
 // Order of tokens: larger logit first, then the lower id; what is no number counts as -infinity.  As one word, larger first: keys of logits ascend with
 // them (-0 is 0), ids are inverted.
@@ -120,7 +121,8 @@ struct Row {   // what comes out of one
         log_s = none ? NAN : log1pf(p.s);
         if (writes && a.entropy) a.entropy[row] = log_s - p.t * 0.69314718056f / (1.f + p.s);
     }
-    __device__ __forceinline__ float logprob(float z) const { return (z - m) * a.inv_t - log_s; }
+    // the difference may be beyond float32's range, the quotient not
+    __device__ __forceinline__ float logprob(float z) const { return __builtin_fmaf(z, 0.5f, -0.5f * m) * (2.f * a.inv_t) - log_s; }
     __device__ __forceinline__ void token(int j, bool there, float z, int before) const
     {
         a.logprobs[row * a.n_tokens + j] = there ? logprob(z) : -INFINITY;
@@ -181,7 +183,11 @@ template <bool BF16, bool WHOLE> __global__ __launch_bounds__(LT) __attribute__(
     const int token0 = n_tokens > 0 ? token_s[0] : 0;
     const float v0 = n_tokens > 0 ? ordered(token_z_s[0]) : INFINITY, below0 = next_below(v0);
 
-    float most = -INFINITY, ref = 0.f, s = 0.f, t = 0.f;   // most: the wave's largest so far; s, t: the lane's
+    // most: the wave's largest so far; s, t: the lane's.  Exponents are (z - ref) k; for bf16, which instructions bound and not the reading, z k + off in one of them, with off = -ref k as
+    // that is rounded, which moves r by as much for all.
+    float most = -INFINITY, ref = 0.f, off = 0.f, s = 0.f, t = 0.f;
+    auto near = [](float off) { return BF16 && fabsf(off) <= MOST_OFF; };
+    auto exponent = [&](float z) { return near(off) ? __builtin_fmaf(z, a.k, off) : (z - ref) * a.k; };
     int equal = 0, before0 = 0, listed = 0;
     float least = -INFINITY;    // what is below it is not among the wave's n_top
     uint64_t least_key = 0;
@@ -234,11 +240,11 @@ template <bool BF16, bool WHOLE> __global__ __launch_bounds__(LT) __attribute__(
         const float here = holds ? bits_f32((uint32_t)__builtin_amdgcn_readfirstlane((int)f32_bits(wave_max(top)))) : most;
         if (here > most) {
             if (equal) {   // those that were the largest join the others
-                const float x = (most - ref) * a.k, e = __builtin_amdgcn_exp2f(x) * (float)equal;
+                const float x = exponent(most), e = __builtin_amdgcn_exp2f(x) * (float)equal;
                 s += lane == 0 ? e : 0.f;
                 t += lane == 0 ? e * x : 0.f;
             }
-            const float d = (ref - here) * a.k;
+            const float next = -here * a.k, d = near(off) && near(next) ? next - off : (ref - here) * a.k;
             if (!equal || !(d >= -FAR)) {
                 const float f = __builtin_amdgcn_exp2f(d);
                 if (equal) {
@@ -246,14 +252,15 @@ template <bool BF16, bool WHOLE> __global__ __launch_bounds__(LT) __attribute__(
                     s *= f;
                 }
                 ref = here;
+                off = next;
             }
             most = here;
             equal = 0;
         }
-        auto sums = [&](auto holding, auto counting) {
+        auto sums = [&](auto holding, auto counting, auto one) {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const float x = (z[i] - ref) * a.k;
+                const float x = decltype(one)::value ? __builtin_fmaf(z[i], a.k, off) : (z[i] - ref) * a.k;
                 float e = __builtin_amdgcn_exp2f(x);
                 if (decltype(holding)::value) {
                     const bool is = z[i] == most;
@@ -266,13 +273,13 @@ template <bool BF16, bool WHOLE> __global__ __launch_bounds__(LT) __attribute__(
             }
         };
         const bool counts = v0 > -INFINITY && __any(top >= v0);
-        if (holds && most > -INFINITY) {
-            if (counts) sums(std::true_type(), std::true_type());
-            else sums(std::true_type(), std::false_type());
-        } else {
-            if (counts) sums(std::false_type(), std::true_type());
-            else sums(std::false_type(), std::false_type());
-        }
+        auto both = [&](auto holding, auto one) {
+            if (counts) sums(holding, std::true_type(), one);
+            else sums(holding, std::false_type(), one);
+        };
+        if (BF16 && !near(off)) both(std::true_type(), std::false_type());
+        else if (holds && most > -INFINITY) both(std::true_type(), std::integral_constant<bool, BF16>());
+        else both(std::false_type(), std::integral_constant<bool, BF16>());
         // Tokens that come before the given ones: larger logits, and of equal ones those of lower ids -- what is larger than the next number below.
         auto id_of = [&](int i) { return first + i / PER * LT * PER + i % PER; };
         for (int j = 0; j < n_tokens; ++j) {
@@ -350,7 +357,7 @@ template <bool BF16, bool WHOLE> __global__ __launch_bounds__(LT) __attribute__(
     }
     if (n_top > 0) cut();
     // relative to the wave's largest
-    const float x = (most - ref) * a.k, f = equal ? __builtin_amdgcn_exp2f(-x) : 1.f;
+    const float x = exponent(most), f = equal ? __builtin_amdgcn_exp2f(-x) : 1.f;
     t = wave_add(t);
     s = wave_add(s);
     if (equal) {
@@ -545,7 +552,8 @@ int sssd_op_logprobs(const void *logits, int32_t type, int32_t rows, int32_t voc
     const bool bf16 = type == SSSD_BF16;
     if ((uintptr_t)logits % (bf16 ? 2 : 4) || (rows > 1 && row_stride < 0)) return SSSD_EINVAL;
     const float k = 1.4426950408889634f / temperature;
-    if (!(temperature > 0.f) || !(k > 0.f) || !(k <= 3.0e38f)) return SSSD_EINVAL;
+    // where a difference of logits is beyond float32's range, times k it is beyond that of exponents
+    if (!(temperature > 0.f) || !(k >= 1e-36f) || !(k <= 1.5e38f)) return SSSD_EINVAL;
     const LogPlan p = log_plan(rows, vocab);
     const LogScratch z = log_scratch(rows, p, n_tokens, n_top);
     if (z.bytes && (!scratch || (uintptr_t)scratch % 16)) return SSSD_EINVAL;

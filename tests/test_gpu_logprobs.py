@@ -185,3 +185,17 @@ def test_replays_and_another_stream():
         eager = sv.sssd_op_logprobs(z, t, 5)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, eager))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,vocab", [(7, 9001), (1100, 9001)])
+def test_logits_far_from_zero(dtype, rows, vocab):
+    """Rows about one large number, and rows that climb or fall from one to another, so that exponents are taken in either way within a row."""
+    g = torch.Generator(device=DEV).manual_seed(rows)
+    tokens = torch.randint(0, vocab, (rows, 3), generator=g, device=DEV)
+    up = torch.arange(vocab, device=DEV) / vocab
+    starts = torch.tensor([-1e6, 1e6, 100.0, -7e5, 7.3e5, -3e7, -2e38], device=DEV).repeat(rows // 7 + 1)[:rows, None]
+    ends = torch.tensor([1e6, -1e6, -1e4, -7e5, 7.2e5, 1e3, 2e38], device=DEV).repeat(rows // 7 + 1)[:rows, None]
+    z = (starts * (1 - up) + ends * up + torch.randn(rows, vocab, generator=g, device=DEV) * 3).to(dtype)
+    for temperature in (1.0, 1e-3, 1e4, 1e-20):
+        check(z, tokens, 5, temperature)

@@ -118,7 +118,7 @@ def logprobs(logits=FAKE, type=0, rows=2, vocab=100, stride=100, temperature=1.0
 
 def test_logprobs_refuse():
     for bad in (dict(logits=None), dict(type=2), dict(rows=0), dict(vocab=0), dict(stride=-1), dict(temperature=0.0), dict(temperature=-1.0), dict(temperature=float("nan")),
-                dict(temperature=float("inf")), dict(temperature=1e-39), dict(tokens=None), dict(lp=None), dict(m=-1), dict(top=-1), dict(top=101), dict(ids=None), dict(top_lp=None),
+                dict(temperature=float("inf")), dict(temperature=1e-39), dict(temperature=2e36), dict(temperature=9e-39), dict(tokens=None), dict(lp=None), dict(m=-1), dict(top=-1), dict(top=101), dict(ids=None), dict(top_lp=None),
                 dict(vocab=5000, scratch=None), dict(vocab=5000, scratch=FAKE + 8), dict(logits=FAKE + 2), dict(logits=FAKE + 1, type=1)):
         assert logprobs(**bad) == SSSD_EINVAL, bad
     for bad in (dict(m=33), dict(top=65), dict(vocab=5000, scratch_bytes=16), dict(vocab=2 ** 30 + 1), dict(rows=2 ** 31 - 1, vocab=128256, stride=128256)):
