@@ -273,7 +273,7 @@ __global__ __launch_bounds__(256) void fork_write_kernel(PagesArgs a, CopyArgs c
 // ---------------------------------------------------------------------------------------------------------- reserve ----
 // One workgroup: the blocks that the call's rows touch, slot by slot, a thread each, in as many rounds as they take.  What a thread has read stays with it for up to KEEP rounds
 // (1885 blocks of prompts 12 us of kernel, 17 when only one round is kept).
-constexpr int KEEP = 3;
+constexpr int KEEP = 4;
 struct Asked {
     bool on, bad, live;   // live: rows that live are in the block
     int slot, blk, page, refs;

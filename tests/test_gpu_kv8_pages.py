@@ -360,7 +360,7 @@ def test_forks_of_few_and_many_entries(slots, max_seq):
     assert pool.fork(list(range(slots))[::-1]) is not None
 
 
-@pytest.mark.parametrize("blocks", [1, 1023, 1024, 1025, 2048, 2049, 3071, 3072, 3073, 4200])
+@pytest.mark.parametrize("blocks", [1, 1023, 1024, 1025, 2048, 2049, 3500, 4095, 4096, 4097, 5300])
 def test_reserves_of_many_blocks(blocks):
     """As many blocks as a round of the workgroup has threads, as it keeps, and more; some of them shared, some in place already."""
     slots = 5
