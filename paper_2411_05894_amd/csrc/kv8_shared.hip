@@ -532,14 +532,16 @@ Kv8SharedPlan kv8_shared_plan(int B, int n, int gq, int nkv, int blocks, int gro
     return p;
 }
 
-// The same of a call whose sequences go by themselves: a block takes a workgroup so much, by row tiles, and a fifth more where sequences are cut into segments.  For f32 and bf16, prefixes of 512 to 32768 positions, groups of 4 to 32
-// sequences, 1 to 32 rows of 8B and 70B, whichever of both is said to be the lesser took 0.5 % longer than whichever was, all going by themselves 9.6 % longer, none 22 %.
-// us, by themselves / sharing: 32 of 9 rows of 8B bf16 512 18.9 / 33.4, 2048 34.9 / 45.4, 8192 90.9 / 74.1, 32768 311 / 196, f32 21.3 / 35.5, 39.7 / 51.4, 102 / 111, 355 / 368; 8 of one row
-// 16.8 / 19.1, 17.1 / 19.9, 30.8 / 23.8, 83.7 / 36.3.  Like the plans it goes by how long sequences can be.
+// The same of a call whose sequences go by themselves: a block takes a workgroup so much, by row tiles, more where sequences are cut into segments, and with bf16 less where compute units have two
+// workgroups.  For f32 and bf16, prefixes of 512 to 32768 positions, groups of 4 to 32 sequences, 1 to 32 rows of 8B and 70B, whichever of both is said to be the lesser took 0.2 % longer
+// than whichever was, all going by themselves 9.6 % longer, none 22 %.  us, by themselves / sharing: 32 of 9 rows of 8B bf16 512 18.9 / 33.4, 2048 34.9 / 45.4, 8192 90.9 / 74.1, 32768 311 / 196,
+// f32 21.3 / 35.5, 39.7 / 51.4, 102 / 111, 355 / 368; 8 of one row 16.8 / 19.1, 17.1 / 19.9, 30.8 / 23.8, 83.7 / 36.3.  Like the plans it goes by how long sequences can be.
 static double apart_us(int64_t heads, int tiles, int blocks, bool f32, const Kv8Plan &p)
 {
-    static const double block[2][KV8_MAX_TILES + 1] = {{0, 0.20, 0.24, 0.29}, {0, 0.22, 0.24, 0.33}};
-    return 13 + (double)blocks / p.share * block[f32][(tiles + p.passes - 1) / p.passes] * std::max(1.0, heads * p.passes * p.share / 256.0) * (p.share > 1 ? 1.2 : 1.0);
+    static const double block[2][2][KV8_MAX_TILES + 1] = {{{0, 0.20, 0.24, 0.29}, {0, 0.22, 0.24, 0.33}}, {{0, 0.275, 0.28, 0.28}, {0, 0.28, 0.29, 0.35}}};   // whole, cut
+    const double rounds = (double)heads * p.passes * p.share / 256;
+    const double us = blocks * block[p.share > 1 && rounds <= 1][f32][(tiles + p.passes - 1) / p.passes] / p.share;
+    return 13 + us * (rounds <= 1 ? 1 : f32 ? rounds : 0.75 * rounds);
 }
 
 // For every number of groups: a prefix's results are at most those of KV8_GROUPS workgroups of 4 * KV8_MAX_TILES row tiles or, where there are more workgroups than that, four a
