@@ -608,172 +608,176 @@ __device__ __forceinline__ void attend_group(const Kv8Args<MODE> &a, AttnShared<
     bool huge = false;   // some row's reference has been HUGE_SCORE
     const int all_from = a.window > 0 ? len + count - a.window : 0;   // every row sees the old positions from here on
 
-    for (int i = 0; i < n_it; ++i) {
-        if (i >> 6 != chunk) {
-            chunk = i >> 6;
+    // Chunks are a loop of their own: where the loop over blocks changes them, pages and scales move between registers on the way round, and every block begins with a wait for all
+    // that is under way, its own V among it (8B, 4 sequences of 32768 bf16 captured 63 us, so 55).
+    for (int i0 = 0; i0 < n_it; i0 += 64) {
+        if (i0 > 0) {
+            chunk = i0 >> 6;
             now = next;
             next = look(chunk + 1);
         }
-        const int t0 = span.block(first + off + STEP * i) * 32;
-        const float k_scale = bits_f32((uint32_t)__builtin_amdgcn_readlane((int)f32_bits(now.scale.x), i & 63));
-        int v_e = __builtin_amdgcn_readlane((int)f32_bits(now.scale.y), i & 63) >> 23 & 255;
-        int ql = lane;
-        if (RT * PARTS > 2) asm volatile("" : "+v"(ql));   // the query operands are read again for every block: hoisted, they would not fit the registers
-        f32x4 s[RT][2];   // s[t][u][r]: position t0 + 16u + 4q + r for query row c of tile t
+        for (int i = i0, end = min(i0 + 64, n_it); i < end; ++i) {
+            const int t0 = span.block(first + off + STEP * i) * 32;
+            const float k_scale = bits_f32((uint32_t)__builtin_amdgcn_readlane((int)f32_bits(now.scale.x), i & 63));
+            int v_e = __builtin_amdgcn_readlane((int)f32_bits(now.scale.y), i & 63) >> 23 & 255;
+            int ql = lane;
+            if (RT * PARTS > 2) asm volatile("" : "+v"(ql));   // the query operands are read again for every block: hoisted, they would not fit the registers
+            f32x4 s[RT][2];   // s[t][u][r]: position t0 + 16u + 4q + r for query row c of tile t
 #pragma unroll
-        for (int t = 0; t < RT; ++t) s[t][0] = s[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-        // The operands of a step (32 channels, hi or lo) are read a step ahead: LDS answers after some hundred cycles, and one wave alone has
-        // nothing else to do meanwhile.
-        u32x4 qq[2][RT];
-        auto fetch = [&](int x) {
+            for (int t = 0; t < RT; ++t) s[t][0] = s[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+            // The operands of a step (32 channels, hi or lo) are read a step ahead: LDS answers after some hundred cycles, and one wave alone has
+            // nothing else to do meanwhile.
+            u32x4 qq[2][RT];
+            auto fetch = [&](int x) {
 #pragma unroll
-            for (int t = 0; t < RT; ++t) qq[x & 1][t] = q_lds[(t * KS * PARTS + x) * 64 + ql];
-        };
-        half8_t kk[2];
-        fetch(0);
+                for (int t = 0; t < RT; ++t) qq[x & 1][t] = q_lds[(t * KS * PARTS + x) * 64 + ql];
+            };
+            half8_t kk[2];
+            fetch(0);
 #pragma unroll
-        for (int x = 0; x < KS * PARTS; ++x) {
-            if (x + 1 < KS * PARTS) fetch(x + 1);
-            if (x % PARTS == 0) {
-                const int ks = x / PARTS;
+            for (int x = 0; x < KS * PARTS; ++x) {
+                if (x + 1 < KS * PARTS) fetch(x + 1);
+                if (x % PARTS == 0) {
+                    const int ks = x / PARTS;
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const u32x4 &w = k[u * (KS / 2) + ks % (KS / 2)];
-                    kk[u] = ks < KS / 2 ? codes_half8<FMT>(w[0], w[1], 1.f) : codes_half8<FMT>(w[2], w[3], 1.f);
+                    for (int u = 0; u < 2; ++u) {
+                        const u32x4 &w = k[u * (KS / 2) + ks % (KS / 2)];
+                        kk[u] = ks < KS / 2 ? codes_half8<FMT>(w[0], w[1], 1.f) : codes_half8<FMT>(w[2], w[3], 1.f);
+                    }
                 }
+#pragma unroll
+                for (int t = 0; t < RT; ++t)
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) s[t][u] = mfma16(kk[u], __builtin_bit_cast(half8_t, qq[x & 1][t]), s[t][u]);
+                if (RT * PARTS > 2) __builtin_amdgcn_sched_barrier(0);
             }
-#pragma unroll
-            for (int t = 0; t < RT; ++t)
-#pragma unroll
-                for (int u = 0; u < 2; ++u) s[t][u] = mfma16(kk[u], __builtin_bit_cast(half8_t, qq[x & 1][t]), s[t][u]);
-            if (RT * PARTS > 2) __builtin_amdgcn_sched_barrier(0);
-        }
-        load_k(i + 1);
-        const bool whole = PRE || (t0 + 32 <= len && (t0 >= all_from || t0 + 32 <= a.sinks));   // all rows see all of the block
-        float sc[RT], mx[RT];   // mx: of the lane's own eight positions
-        bool grow = huge;
-#pragma unroll
-        for (int t = 0; t < RT; ++t) {
-            sc[t] = __builtin_amdgcn_fmed3f(row_scale[t] * k_scale, 0x1p-126f, 0x1p127f);   // neither 0 nor infinite: times -INFINITY or 0
-            if (!whole) {
-                const uint32_t mine = visible(t0, len, low_s[t * 16 + c], a.sinks, word_s[t * 16 + c]) >> (4 * q);
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) s[t][u][r] = mine & (1u << (16 * u + r)) ? s[t][u][r] : -INFINITY;
-            }
-            mx[t] = max3(max3(s[t][0][0], s[t][0][1], s[t][0][2]), max3(s[t][0][3], s[t][1][0], s[t][1][1]), max3(s[t][1][2], s[t][1][3], s[t][1][3]));
-            grow = grow || above(mx[t], sc[t], m_run[t]) > REF_MOST;
-        }
-        if (__any(grow)) {
+            load_k(i + 1);
+            const bool whole = PRE || (t0 + 32 <= len && (t0 >= all_from || t0 + 32 <= a.sinks));   // all rows see all of the block
+            float sc[RT], mx[RT];   // mx: of the lane's own eight positions
+            bool grow = huge;
 #pragma unroll
             for (int t = 0; t < RT; ++t) {
-                const float m = rows_max(mx[t]);
-                const float m_new = above(m, sc[t], m_run[t]) > REF_MOST ? above(m, sc[t], REF_BELOW) : m_run[t], alpha = __builtin_amdgcn_exp2f(m_run[t] - m_new);
-                m_run[t] = m_new;
-                huge = huge || __any(fabsf(m_new) >= HUGE_SCORE && m_new != NONE);
-                l_run[t] *= alpha;
+                sc[t] = __builtin_amdgcn_fmed3f(row_scale[t] * k_scale, 0x1p-126f, 0x1p127f);   // neither 0 nor infinite: times -INFINITY or 0
+                if (!whole) {
+                    const uint32_t mine = visible(t0, len, low_s[t * 16 + c], a.sinks, word_s[t * 16 + c]) >> (4 * q);
 #pragma unroll
-                for (int dt = 0; dt < DT; ++dt) o[t][dt] *= alpha;
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) s[t][u][r] = mine & (1u << (16 * u + r)) ? s[t][u][r] : -INFINITY;
+                }
+                mx[t] = max3(max3(s[t][0][0], s[t][0][1], s[t][0][2]), max3(s[t][0][3], s[t][1][0], s[t][1][1]), max3(s[t][1][2], s[t][1][3], s[t][1][3]));
+                grow = grow || above(mx[t], sc[t], m_run[t]) > REF_MOST;
             }
-            if (huge)
+            if (__any(grow)) {
 #pragma unroll
                 for (int t = 0; t < RT; ++t) {
-                    const bool mine = fabsf(m_run[t]) >= HUGE_SCORE;   // by the row alone: the others change none of its bits
+                    const float m = rows_max(mx[t]);
+                    const float m_new = above(m, sc[t], m_run[t]) > REF_MOST ? above(m, sc[t], REF_BELOW) : m_run[t], alpha = __builtin_amdgcn_exp2f(m_run[t] - m_new);
+                    m_run[t] = m_new;
+                    huge = huge || __any(fabsf(m_new) >= HUGE_SCORE && m_new != NONE);
+                    l_run[t] *= alpha;
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) s[t][u] = mine ? s[t][u] * sc[t] : s[t][u];
-                    sc[t] = mine ? 1.f : sc[t];
+                    for (int dt = 0; dt < DT; ++dt) o[t][dt] *= alpha;
                 }
-        }
-        u32x4 pk[RT][PARTS];
-        auto weigh = [&](int t, float ref) {
+                if (huge)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e >> 1][2 * (e & 1)], sc[t], -ref));
-                const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e >> 1][2 * (e & 1) + 1], sc[t], -ref));
-                uint32_t hi, lo;
-                if (PARTS == 2) {
-                    split_half2(p0, p1, hi, lo);
-                    pk[t][PARTS - 1][e] = lo;
-                } else {
-                    hi = pack_half2(p0, p1);
-                }
-                pk[t][0][e] = hi;
+                    for (int t = 0; t < RT; ++t) {
+                        const bool mine = fabsf(m_run[t]) >= HUGE_SCORE;   // by the row alone: the others change none of its bits
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) s[t][u] = mine ? s[t][u] * sc[t] : s[t][u];
+                        sc[t] = mine ? 1.f : sc[t];
+                    }
             }
-        };
-        auto codes = [&](int dt, float ratio) {
-            const u32x4 &w = v[dt >> 1];
-            return dt & 1 ? codes_half8<FMT>(w[2], w[3], ratio) : codes_half8<FMT>(w[0], w[1], ratio);
-        };
-        auto times = [&](const half8_t &x, int t, f32x4 sum) {
+            u32x4 pk[RT][PARTS];
+            auto weigh = [&](int t, float ref) {
 #pragma unroll
-            for (int part = 0; part < PARTS; ++part) sum = mfma16(x, __builtin_bit_cast(half8_t, pk[t][part]), sum);
-            return sum;
-        };
-        // The sums are in units of 2^(v_ref - 127), a V scale: they move to a larger one only when a block's outgrows it, and not for a block of zeros, whose
-        // scale says nothing.
-        const int low_was = v_low;
-        v_low = min(v_low, v_e);
-        if (__builtin_expect((uint32_t)(v_e - v_from) > v_span, false)) {
-            uint32_t any = 0;
-#pragma unroll
-            for (int x = 0; x < VR; ++x)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) any |= FMT == SSSD_KV8_E4M3 ? v[x][e] & 0x7F7F7F7Fu : v[x][e] ^ 0x80808080u;
-            const bool some = __any(any != 0), far = some && v_ref >= 0;
-            if (some) {
-                const float down = bits_f32((uint32_t)max(v_ref - v_e + 127, 0) << 23);
-                if (v_e > v_ref) {
-#pragma unroll
-                    for (int t = 0; t < RT; ++t)
-#pragma unroll
-                        for (int dt = 0; dt < DT; ++dt) o[t][dt] *= down;
+                for (int e = 0; e < 4; ++e) {
+                    const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e >> 1][2 * (e & 1)], sc[t], -ref));
+                    const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e >> 1][2 * (e & 1) + 1], sc[t], -ref));
+                    uint32_t hi, lo;
+                    if (PARTS == 2) {
+                        split_half2(p0, p1, hi, lo);
+                        pk[t][PARTS - 1][e] = lo;
+                    } else {
+                        hi = pack_half2(p0, p1);
+                    }
+                    pk[t][0][e] = hi;
                 }
-                v_ref = max(v_ref, v_e);
-                const int top = min(v_ref + V_ABOVE, v_low + V_ABOVE + V_BELOW);
-                v_from = top < v_ref - V_BELOW ? 512 : v_ref - V_BELOW;   // 512: beyond all
-                v_span = (uint32_t)(top - v_from) & 31u;
+            };
+            auto codes = [&](int dt, float ratio) {
+                const u32x4 &w = v[dt >> 1];
+                return dt & 1 ? codes_half8<FMT>(w[2], w[3], ratio) : codes_half8<FMT>(w[0], w[1], ratio);
+            };
+            auto times = [&](const half8_t &x, int t, f32x4 sum) {
+#pragma unroll
+                for (int part = 0; part < PARTS; ++part) sum = mfma16(x, __builtin_bit_cast(half8_t, pk[t][part]), sum);
+                return sum;
+            };
+            // The sums are in units of 2^(v_ref - 127), a V scale: they move to a larger one only when a block's outgrows it, and not for a block of zeros, whose
+            // scale says nothing.
+            const int low_was = v_low;
+            v_low = min(v_low, v_e);
+            if (__builtin_expect((uint32_t)(v_e - v_from) > v_span, false)) {
+                uint32_t any = 0;
+#pragma unroll
+                for (int x = 0; x < VR; ++x)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) any |= FMT == SSSD_KV8_E4M3 ? v[x][e] & 0x7F7F7F7Fu : v[x][e] ^ 0x80808080u;
+                const bool some = __any(any != 0), far = some && v_ref >= 0;
+                if (some) {
+                    const float down = bits_f32((uint32_t)max(v_ref - v_e + 127, 0) << 23);
+                    if (v_e > v_ref) {
+#pragma unroll
+                        for (int t = 0; t < RT; ++t)
+#pragma unroll
+                            for (int dt = 0; dt < DT; ++dt) o[t][dt] *= down;
+                    }
+                    v_ref = max(v_ref, v_e);
+                    const int top = min(v_ref + V_ABOVE, v_low + V_ABOVE + V_BELOW);
+                    v_from = top < v_ref - V_BELOW ? 512 : v_ref - V_BELOW;   // 512: beyond all
+                    v_span = (uint32_t)(top - v_from) & 31u;
+                }
+                if (far) {
+                    const f32x4 none = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY}, zero = f32x4{0.f, 0.f, 0.f, 0.f};
+                    const float down = bits_f32((uint32_t)max(v_e - v_ref + 127, 0) << 23);
+                    float back[RT];   // from the block's reference and scale to the row's reference and the unit
+#pragma unroll
+                    for (int t = 0; t < RT; ++t) {
+                        const float m = rows_max(max3(max3(s[t][0][0], s[t][0][1], s[t][0][2]), max3(s[t][0][3], s[t][1][0], s[t][1][1]), max3(s[t][1][2], s[t][1][3], s[t][1][3])));
+                        const float ref = fmaxf(above(m, sc[t], REF_BELOW), m_run[t] - REF_FAR);
+                        weigh(t, ref);
+                        s[t][0] = s[t][1] = none;   // then there is nothing left of the block
+                        back[t] = __builtin_amdgcn_exp2f(ref - m_run[t]);
+                        l_run[t] += times(ones, t, zero) * back[t];
+                        back[t] *= down;
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt) {
+                        const half8_t vv = codes(dt, 1.f);
+#pragma unroll
+                        for (int t = 0; t < RT; ++t) o[t][dt] += times(vv, t, zero) * back[t];
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
+                if (!some) v_low = low_was;
+                v_e = v_ref;
+#pragma unroll
+                for (int x = 0; x < VR; ++x) asm volatile("" : "+v"(v[x]));   // its codes as halves are not kept for what follows: 32 registers
             }
-            if (far) {
-                const f32x4 none = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY}, zero = f32x4{0.f, 0.f, 0.f, 0.f};
-                const float down = bits_f32((uint32_t)max(v_e - v_ref + 127, 0) << 23);
-                float back[RT];   // from the block's reference and scale to the row's reference and the unit
+            const float ratio = bits_f32((uint32_t)(v_e - v_ref + 127) << 23);   // 2^-V_BELOW .. 2^V_ABOVE
 #pragma unroll
-                for (int t = 0; t < RT; ++t) {
-                    const float m = rows_max(max3(max3(s[t][0][0], s[t][0][1], s[t][0][2]), max3(s[t][0][3], s[t][1][0], s[t][1][1]), max3(s[t][1][2], s[t][1][3], s[t][1][3])));
-                    const float ref = fmaxf(above(m, sc[t], REF_BELOW), m_run[t] - REF_FAR);
-                    weigh(t, ref);
-                    s[t][0] = s[t][1] = none;   // then there is nothing left of the block
-                    back[t] = __builtin_amdgcn_exp2f(ref - m_run[t]);
-                    l_run[t] += times(ones, t, zero) * back[t];
-                    back[t] *= down;
-                    __builtin_amdgcn_sched_barrier(0);
-                }
+            for (int t = 0; t < RT; ++t) weigh(t, m_run[t]);
 #pragma unroll
-                for (int dt = 0; dt < DT; ++dt) {
-                    const half8_t vv = codes(dt, 1.f);
+            for (int t = 0; t < RT; ++t) l_run[t] = times(ones, t, l_run[t]);
 #pragma unroll
-                    for (int t = 0; t < RT; ++t) o[t][dt] += times(vv, t, zero) * back[t];
-                    __builtin_amdgcn_sched_barrier(0);
-                }
+            for (int dt = 0; dt < DT; ++dt) {
+                const half8_t vv = codes(dt, ratio);
+#pragma unroll
+                for (int t = 0; t < RT; ++t) o[t][dt] = times(vv, t, o[t][dt]);
             }
-            if (!some) v_low = low_was;
-            v_e = v_ref;
-#pragma unroll
-            for (int x = 0; x < VR; ++x) asm volatile("" : "+v"(v[x]));   // its codes as halves are not kept for what follows: 32 registers
+            load_v(i + 1);
         }
-        const float ratio = bits_f32((uint32_t)(v_e - v_ref + 127) << 23);   // 2^-V_BELOW .. 2^V_ABOVE
-#pragma unroll
-        for (int t = 0; t < RT; ++t) weigh(t, m_run[t]);
-#pragma unroll
-        for (int t = 0; t < RT; ++t) l_run[t] = times(ones, t, l_run[t]);
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-            const half8_t vv = codes(dt, ratio);
-#pragma unroll
-            for (int t = 0; t < RT; ++t) o[t][dt] = times(vv, t, o[t][dt]);
-        }
-        load_v(i + 1);
     }
 
     if constexpr (PRE) {
