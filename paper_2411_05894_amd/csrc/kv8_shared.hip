@@ -496,7 +496,7 @@ template <int HD> hipError_t launch_format(const Kv8SharedArgs &a, int fmt, int 
 
 // Row tiles of a wave, and how many workgroups go over a prefix at most, for groups that are all alike and prefixes as long as they can be; shorter ones take fewer (prefix_cut).  Few rows: a workgroup's waves are on different segments.  Else, with s workgroups to
 // a row tile and prefix, about
-//     blocks / s * (0.65 us, or half as much again where compute units have two of them) + s * rows * nkv * 264 us, for 528 bytes of partial results a row, out and in, at 4 TB/s
+//     blocks / s * (0.65 us, or half as much again where compute units have two of them, in as many rounds as they come in) + s * rows * nkv * 264 ps, for 528 bytes of partial results a row, out and in, at 4 TB/s
 // and 0.04 us a segment for what the joining of it takes.  us, by that / as many as the chip holds: best of eight with 9 rows on 2048 positions 31 / 37, 32 sequences of 4 rows on 2000
 // of 70B 41 / 49, two prompts of 70B 64 / 64, 64 of one on 32768 and 16 of 9 on 4096 the same.  More workgroups than find something to do hold those that lie behind them up by some 3 us.
 Kv8SharedPlan kv8_shared_plan(int B, int n, int gq, int nkv, int blocks, int groups, bool f32)
@@ -513,13 +513,14 @@ Kv8SharedPlan kv8_shared_plan(int B, int n, int gq, int nkv, int blocks, int gro
     }
     const int64_t per = p.wave_rows * p.rt * 16;
     p.tiles = (int)((rows + per - 1) / per + std::max(groups, 1) - 1);
-    const int64_t units = (each + per - 1) / per * (groups > 0 ? groups : 1) * nkv;
+    const int64_t tiles_all = (each + per - 1) / per * (groups > 0 ? groups : 1), units = tiles_all * nkv;
     const int sub = 4 / p.wave_rows;   // segments of a workgroup
     const double segment_cost = (double)rows * nkv * 2.64e-4 + 0.04;
+    auto on_die = [&](int64_t s) { return tiles_all * ((s * nkv + 7) / 8); };   // workgroups on a die at most, of 32 compute units
     double best = 0;
     p.share = 1;
-    for (int64_t s = 1; s <= 64 && s * units <= KV8_GROUPS && (s - 1) * sub * 4 < blocks; ++s) {
-        const double cost = std::ceil((double)blocks / (s * sub)) * (s * units <= 256 ? 0.65 : 0.975) + s * sub * segment_cost;
+    for (int64_t s = 1; s == 1 || (s <= 64 && s * units <= KV8_GROUPS && (s - 1) * sub * 4 < blocks); ++s) {
+        const double cost = std::ceil((double)blocks / (s * sub)) * (on_die(s) <= 32 ? 0.65 : 0.975 * ((on_die(s) + 63) / 64)) + s * sub * segment_cost;
         if (s == 1 || cost < best) {
             best = cost;
             p.share = (int)s;
@@ -527,21 +528,26 @@ Kv8SharedPlan kv8_shared_plan(int B, int n, int gq, int nkv, int blocks, int gro
     }
     p.us = 18 + best;
     p.segments = p.share * sub;
-    p.once = (int)std::min<int64_t>(p.share, 256 / units) * sub;
+    p.once = 0;
+    for (int s = p.share; s > 0 && !p.once; --s)
+        if (on_die(s) <= 32) p.once = s * sub;
     p.cost = (float)segment_cost;
     return p;
 }
 
-// The same of a call whose sequences go by themselves: a block takes a workgroup so much, by row tiles, more where sequences are cut into segments, and with bf16 less where compute units have two
-// workgroups.  For f32 and bf16, prefixes of 512 to 32768 positions, groups of 4 to 32 sequences, 1 to 32 rows of 8B and 70B, whichever of both is said to be the lesser took 0.2 % longer
-// than whichever was, all going by themselves 9.6 % longer, none 22 %.  us, by themselves / sharing: 32 of 9 rows of 8B bf16 512 18.9 / 33.4, 2048 34.9 / 45.4, 8192 90.9 / 74.1, 32768 311 / 196,
-// f32 21.3 / 35.5, 39.7 / 51.4, 102 / 111, 355 / 368; 8 of one row 16.8 / 19.1, 17.1 / 19.9, 30.8 / 23.8, 83.7 / 36.3.  Like the plans it goes by how long sequences can be.
-static double apart_us(int64_t heads, int tiles, int blocks, bool f32, const Kv8Plan &p)
+// The same of a call whose sequences go by themselves: a block takes a workgroup so much by row tiles, and more where compute units have several workgroups; or what it takes to get it there, the less
+// the more of a group's sequences, and passes of theirs, read the same one at the same time.  Of 384 batches of 4 to 64 sequences in up to eight groups, with 1 to 32 rows, of 8B, 70B and other numbers of heads, on
+// 512 to 32768 positions, and of 152 others in up to 128 groups, whichever is said to be the lesser took 0.3 and 0.8 % longer than whichever was, all going by themselves 14 and 20 %, none 30 and 21 %; it takes one
+// kv head with many rows to be joined faster than it is (24 of 9 rows of 32 heads, bf16, 16384: by themselves 88, joined 160).  us, by themselves / joined, ten in a row in a graph: 32 of 9 rows of 8B bf16
+// 512 15.1 / 29.8, 2048 28.6 / 41.7, 8192 80.4 / 70.5, 32768 264 / 192, f32 18.0 / 31.8, 34.9 / 47.8, 97.8 / 108, 351 / 365; 8 of one row bf16 9.4 / 14.9, 12.4 / 15.7, 27.1 / 19.3, 84.0 / 28.7.  Like the plans it
+// goes by how long sequences can be.
+static double apart_us(int B, int groups, int nkv, int tiles, int blocks, bool f32, const Kv8Plan &p)
 {
-    static const double block[2][2][KV8_MAX_TILES + 1] = {{{0, 0.20, 0.24, 0.29}, {0, 0.22, 0.24, 0.33}}, {{0, 0.275, 0.28, 0.28}, {0, 0.28, 0.29, 0.35}}};   // whole, cut
-    const double rounds = (double)heads * p.passes * p.share / 256;
-    const double us = blocks * block[p.share > 1 && rounds <= 1][f32][(tiles + p.passes - 1) / p.passes] / p.share;
-    return 13 + us * (rounds <= 1 ? 1 : f32 ? rounds : 0.75 * rounds);
+    static const double block[2][KV8_MAX_TILES + 1] = {{0, 0.142, 0.20, 0.25}, {0, 0.178, 0.243, 0.326}};
+    const int rt = (tiles + p.passes - 1) / p.passes;
+    const double rounds = (double)B * nkv * p.passes * p.share / 256, same = (double)B / std::max(groups, 1) * p.passes;
+    const double longer = rounds <= 1 ? 1 : std::ceil(rounds) * (!f32 ? 0.77 : rt == 1 ? 0.83 : 1);
+    return 13 + blocks * std::max(block[f32][rt] * longer, 0.30 * std::min(1.0, 8 / same) * std::max(1.0, rounds)) / p.share;
 }
 
 // For every number of groups: a prefix's results are at most those of KV8_GROUPS workgroups of 4 * KV8_MAX_TILES row tiles or, where there are more workgroups than that, four a
@@ -593,7 +599,7 @@ int sssd_kv8_attention_shared(const sssd_kv8 *kv, int32_t layer, int32_t B, int3
     const Kv8SharedPlan p = kv8_shared_plan(B, n, a.gq, c.n_kv_heads, S.blocks_per_seq, groups, !a.q.bf16);
     a.groups = groups; a.starts = starts; a.shared = shared;
     hipStream_t s = (hipStream_t)stream;
-    if ((groups == 0 || apart_us((int64_t)B * c.n_kv_heads, tiles, S.blocks_per_seq, !a.q.bf16, a.plan) <= p.us) && (int64_t)B * c.n_q_heads <= MOST_THREADS / (32 * 256)) {
+    if ((groups == 0 || apart_us(B, groups, c.n_kv_heads, tiles, S.blocks_per_seq, !a.q.bf16, a.plan) <= p.us) && (int64_t)B * c.n_q_heads <= MOST_THREADS / (32 * 256)) {
         a.hand.polls = kv->flags & SSSD_NO_WAIT ? 0 : HAND_POLLS;
         HIP_TRY(launch_kv8_apart(a, c.format, c.head_dim, kv->workspace, s));
         return SSSD_OK;

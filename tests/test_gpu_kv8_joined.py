@@ -208,3 +208,11 @@ def test_a_step_replays_while_sequences_come_and_go(dtype, kind, n):
                     bound = bound + mass * 2.0 ** -11 + (want.abs() + bound) * torch.finfo(torch.bfloat16).eps / 2
                 assert ((out[b].double() - want).abs() <= bound).all(), (turn, b)
         lens += counts
+
+
+def test_sequences_by_themselves(no_room):
+    """Short prefixes, and batches whose rows fill the chip as they are: nothing to join, the workspace is left alone.  The last has more workgroups than the chip holds at once."""
+    for heads, groups, own, n in (((8, 2, 64), [(6, 500)], [7, 90], 3), ((4, 2, 64), [(4, 512)], [33], 1), ((64, 8, 128), [(64, 320)], [3], 9)):
+        batch = Batch("e4m3", *heads, groups, own, n)
+        out, went = way(batch, lambda: batch.check(torch.float32))
+        assert went == "apart", (heads, groups, n)
