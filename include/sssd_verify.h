@@ -69,11 +69,11 @@ typedef struct {
     const void *const *attn_norm, *const *mlp_norm;
 } sssd_weights;
 
-/* Flags of sssd_verify_init. */
 /* Types of elements in device memory, where a call takes several. */
 #define SSSD_F32 0
 #define SSSD_BF16 1
 
+/* Flags of sssd_verify_init. */
 #define SSSD_PACK_IN_PLACE 1u /* reorder each weight matrix inside the caller's own buffer
                                  (needs hidden, n_q*d and ffn to be multiples of 32);
                                  the caller's matrices are then in the library's private

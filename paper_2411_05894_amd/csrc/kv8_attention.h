@@ -261,13 +261,6 @@ __device__ __forceinline__ bool group_round(const Kv8SharedArgs &a, int round, i
     if (g.n < 2 || g.blocks == 0) g = Group{from, 0, 0};   // a sequence alone shares with nobody
     return !__any(!ok);
 }
-__device__ __forceinline__ bool groups_ok(const Kv8SharedArgs &a, int lane)
-{
-    bool ok = true;
-    Group g;
-    for (int r = 0; r * 64 < a.groups; ++r) ok = group_round(a, r, lane, g) && ok;
-    return ok;
-}
 // What sequence b shares.
 __device__ __forceinline__ Group group_of(const Kv8SharedArgs &a, int b, int lane, bool &ok)
 {
@@ -360,7 +353,7 @@ template <int MODE> using Kv8Pass = std::conditional_t<MODE == KV8_ALONE, const 
 
 // PARTS: the query operand is float16 (1: bf16 queries) or float16 hi + lo (2: float32 queries), and so are the probabilities.
 // grid: workgroups of one (sequence, kv head) have block indexes of one residue modulo 8: its segments, and their passes next to each other.
-// KV8_PREFIX: a wave has row tiles of its own (wave_rows of a workgroup's waves), the others of a tile are on other segments; its partial results are its own.
+// KV8_PREFIX: the waves of a workgroup have the same row tiles and are on segments next to each other; a wave's partial results are its own.
 template <int HD, int RT, int PARTS, int NW, int MODE> struct AttnShared {   // LDS of a workgroup
     static constexpr int KS = HD / 32, DT = HD / 16, QT = DT / NW, TR = NW == 4 ? RT : RT <= 2 ? RT : 2;
     static constexpr int QREC = RT * KS * PARTS * 64, RRED = NW * (NW - 1) * TR * QT * 64, QSETS = MODE == KV8_PREFIX ? NW : 1;
@@ -391,17 +384,16 @@ __device__ __forceinline__ void attend_group(Kv8Pass<MODE> a, AttnShared<HD, RT,
     int skip = 0, n_rows = 0;   // blocks that are another workgroup's; rows of a group
     Cut prefix{1, 1};
     if constexpr (PRE) {
-        const int slabs = a.wave_rows, slab = wave & (slabs - 1);
-        const PrefixTask task = prefix_task(a, bid, slabs * RT * 16, NW / slabs, lane);
+        const PrefixTask task = prefix_task(a, bid, RT * 16, NW, lane);
         segment = (int)((uint32_t)task.pair / (uint32_t)nkv);
         kvh = task.pair - segment * nkv;
-        segment = segment * (NW / slabs);
+        segment *= NW;
         if (task.g.n == 0 || segment >= task.cut.n) return;
-        segment += wave / slabs;
+        segment += wave;
         b = task.g.first;
         skip = task.g.blocks;
         n_rows = task.g.n * a.n * a.gq;
-        pass = task.tile * slabs + slab;
+        pass = task.tile;
         prefix = task.cut;
     } else {
         const uint32_t slot = bid >> 3, x = slot / (uint32_t)passes, row = x / (uint32_t)share;
