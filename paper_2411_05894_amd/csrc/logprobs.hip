@@ -9,9 +9,9 @@
 // changes it), how many come before each given token, and a list of its most probable tokens: what is above the last of n in a list that was full, at first above the n-th largest of its lanes'
 // largest logits.  Parts leave all that in memory, and a second launch joins them.  The order of sums is fixed.
 //
-// What bounds it: thirteen instructions a logit, an exponential among them, and in their shadow the reading.  us, four in a row in a graph: 1501 rows of 128256, one token with its rank and one alternative,
-// bf16 96 (4.0 TB/s; 90 where inputs change), float32 164 (4.7 TB/s; a kernel that only reads takes 54 and 108); without the alternative 89 and 152, 20 alternatives 137 and 179.  9 rows: 8.6 and 6.3 for the
-// joining, both round trips behind one another.
+// What bounds it: thirteen instructions a logit, an exponential among them, and in their shadow the reading.  us: 1501 rows of 128256, one token with its rank and one alternative,
+// bf16 95 (4.0 TB/s; 104 with (z - r) k in two roundings), float32 148 (5.2 TB/s, as fast as a copy); bf16 without the token 84, without the alternative 86, without both 76; 20 alternatives 137.  9 rows: 8.6 and 6.3 for the joining,
+// both round trips behind one another.
 #include "../../include/sssd_ops.h"
 #include "common.h"
 
@@ -506,17 +506,13 @@ template <bool BF16> __global__ __launch_bounds__(JT) void logprob_join_kernel(L
     }
 }
 
-// Parts so that some thousand workgroups have work, but no more than the chip holds of them at once (six on a compute unit): what is left for a second round takes as long as the first.  us, one
-// token, its rank and one alternative of 128256 logits, bf16 / float32: 400 rows in three parts 45 / 46, 768 in two 61 / 86, 900 whole 70 / 101 (in two 85 / 121), 1023 71 / 108
-// (88 / 124), 1536 97 / 165, 1600, a second round, 130 / 206, 4001 235 / 402.
+// Whole rows while there are enough of them to fill the chip, else parts.
 struct LogPlan {
     int part, parts;
 };
 LogPlan log_plan(int64_t rows, int vocab)
 {
-    const int64_t most = ((int64_t)vocab + 2047) / 2048;   // parts of 2048 logits at least
-    int64_t want = (1024 + rows - 1) / rows;
-    if (want * rows > 6 * 256) --want;
+    const int64_t want = (1024 + rows - 1) / rows, most = ((int64_t)vocab + 2047) / 2048;   // parts of 2048 logits at least
     LogPlan p;
     p.parts = (int)std::max<int64_t>(1, std::min(want, most));
     p.part = (int)((((int64_t)vocab + p.parts - 1) / p.parts + 7) / 8 * 8);

@@ -1,4 +1,4 @@
-"""sssd_op_logprobs against 64 bits where one workgroup goes over a whole row (from 769 rows on) of a real vocabulary, and where the true log-probability is -infinity.
+"""sssd_op_logprobs against 64 bits where one workgroup goes over a whole row (from 1024 rows on) of a real vocabulary, and where the true log-probability is -infinity.
 
 Bounds, u = 2^-24, for rows whose logits are about as far apart as those of a model.  A term of S is off by (4 |x| + 2) u of itself (the difference, the factor log2(e) / T, their product, exp2), x
 relative to a logit within four octaves of the largest, 2.8 more than the row's own x: (4 |x| + 13) u.  A lane adds vocab / 256 + 1 terms, a wave its lanes in 6 steps; the sums are moved to
@@ -58,7 +58,7 @@ def check(z, tokens, n_top, temperature=1.0, at_a_time=256):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("rows", [768, 769, 1501])
+@pytest.mark.parametrize("rows", [1023, 1024, 1501])
 @pytest.mark.parametrize("m,n_top,temperature", [(1, 1, 1.0), (7, 20, 0.7)])
 def test_whole_rows_of_a_real_vocabulary(dtype, rows, m, n_top, temperature):
     z, tokens = base.random_rows(rows, 128256, rows + m, dtype)
