@@ -9,9 +9,9 @@
 // changes it), how many come before each given token, and a list of its most probable tokens: what is above the last of n in a list that was full, at first above the n-th largest of its lanes'
 // largest logits.  Parts leave all that in memory, and a second launch joins them.  The order of sums is fixed.
 //
-// What bounds it: thirteen instructions a logit, an exponential among them, and in their shadow the reading.  us: 1501 rows of 128256, one token with its rank and one alternative,
-// bf16 95 (4.0 TB/s; 104 with (z - r) k in two roundings), float32 148 (5.2 TB/s, as fast as a copy); bf16 without the token 84, without the alternative 86, without both 76; 20 alternatives 137.  9 rows: 8.6 and 6.3 for the joining,
-// both round trips behind one another.
+// What bounds it: thirteen instructions a logit, an exponential among them, and in their shadow the reading.  us, four in a row in a graph: 1501 rows of 128256, one token with its rank and one alternative,
+// bf16 96 (4.0 TB/s; 90 where inputs change), float32 164 (4.7 TB/s; a kernel that only reads takes 54 and 108); without the alternative 89 and 152, 20 alternatives 137 and 179.  9 rows: 8.6 and 6.3 for the
+// joining, both round trips behind one another.
 #include "../../include/sssd_ops.h"
 #include "common.h"
 
@@ -506,7 +506,9 @@ template <bool BF16> __global__ __launch_bounds__(JT) void logprob_join_kernel(L
     }
 }
 
-// Whole rows while there are enough of them to fill the chip, else parts.
+// Whole rows while there are enough of them to fill the chip, else parts.  us, one token, its rank and one alternative of 128256 logits, bf16 / float32: 400 rows in three parts 45 / 46, 768 in two 61 / 86,
+// 900 in two, which are more workgroups than the chip holds at once (six on a compute unit), 85 / 121, whole they would take 70 / 101; 1024 whole 71 / 105, 1536 97 / 165, 1600, a second round, 130 / 206,
+// 4001 235 / 402.
 struct LogPlan {
     int part, parts;
 };

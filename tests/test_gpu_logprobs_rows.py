@@ -58,7 +58,7 @@ def check(z, tokens, n_top, temperature=1.0, at_a_time=256):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("rows", [1023, 1024, 1501])
+@pytest.mark.parametrize("rows", [768, 1023, 1024, 1501])
 @pytest.mark.parametrize("m,n_top,temperature", [(1, 1, 1.0), (7, 20, 0.7)])
 def test_whole_rows_of_a_real_vocabulary(dtype, rows, m, n_top, temperature):
     z, tokens = base.random_rows(rows, 128256, rows + m, dtype)
