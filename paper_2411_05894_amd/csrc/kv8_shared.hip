@@ -8,11 +8,11 @@
 // as a sequence's alone.  What lies behind the prefix goes as sequences do alone, in the same launch, and a last one joins both.  Where that would take longer than every sequence by itself
 // (apart_us), they go by themselves, the shared blocks read through the first one's table (kv8_apart.hip).
 //
-// What bounds it.  us, kernels of this / of the call for sequences alone: 64 sequences of one row on 32768 positions (8B, bf16) 62 + 10 / 301, 35 GFLOP, for which a
-// large product takes 26; 70B, 17 sequences of 5 rows on 4000 positions and 9 on 2000 48 + 8 / 68; 20 sequences of one row of 8B on 4096 14.5 + 4.3 / 20.6; 4 on 2048 8.3 + 4.3 / 9.0;
-// eight of 9 rows on 2048 20.7 + 5.2 / 20.4; 32 of one on 512 12.8 + 4.1 / 8.4.  With many rows, matrix instructions are under way for 55 % of the loop's time (30 % of the
+// What bounds it.  us, kernels of this / of the call for sequences alone: 64 sequences of one row on 32768 positions (8B, bf16) 61 + 10 / 232, 35 GFLOP, for which a
+// large product takes 26; 20 sequences of one row of 8B on 4096 16.3 + 5.0 / 20.3; 4 on 2048 9.9 + 4.7 / 9.0; eight of 9 rows, float32, on 2048 20.8 + 5.3 / 20.6; 32 of one on 512 13.4 + 4.1 / 8.4; eight of one
+// on 32768 21 + 9.3 / 84.  With many rows, matrix instructions are under way for 55 % of the loop's time (30 % of the
 // kernel's), exponentials, conversions and what is read of LDS for the rest; around it 5 to 6 us until the first operands are there, and the partial results, 35 MB out and in for the 64 sequences.  Few rows and short
-// prefixes: that start and the second launch, 4 us at least.
+// prefixes: that start and the second launch, 4 us at least, and partial results of every wave.
 #include "kv8_attention.h"
 #include "kv8_host.h"
 
@@ -538,12 +538,12 @@ Kv8SharedPlan kv8_shared_plan(int B, int n, int gq, int nkv, int blocks, int gro
 // The same of a call whose sequences go by themselves: a block takes a workgroup so much by row tiles, and more where compute units have several workgroups; or what it takes to get it there, the less
 // the more of a group's sequences, and passes of theirs, read the same one at the same time.  Of 384 batches of 4 to 64 sequences in up to eight groups, with 1 to 32 rows, of 8B, 70B and other numbers of heads, on
 // 512 to 32768 positions, and of 152 others in up to 128 groups, whichever is said to be the lesser took 0.3 and 0.8 % longer than whichever was, all going by themselves 14 and 20 %, none 30 and 21 %; it takes one
-// kv head with many rows to be joined faster than it is (24 of 9 rows of 32 heads, bf16, 16384: by themselves 88, joined 160).  us, by themselves / joined, ten in a row in a graph: 32 of 9 rows of 8B bf16
+// kv head with many rows to be joined faster than it is (24 of 9 rows of 32 heads, bf16, 16384: by themselves 88, joined 160).  us, by themselves / joined, five in a row in a graph: 32 of 9 rows of 8B bf16
 // 512 15.1 / 29.8, 2048 28.6 / 41.7, 8192 80.4 / 70.5, 32768 264 / 192, f32 18.0 / 31.8, 34.9 / 47.8, 97.8 / 108, 351 / 365; 8 of one row bf16 9.4 / 14.9, 12.4 / 15.7, 27.1 / 19.3, 84.0 / 28.7.  Like the plans it
 // goes by how long sequences can be.
 static double apart_us(int B, int groups, int nkv, int tiles, int blocks, bool f32, const Kv8Plan &p)
 {
-    static const double block[2][KV8_MAX_TILES + 1] = {{0, 0.142, 0.20, 0.25}, {0, 0.178, 0.243, 0.326}};
+    static const double block[2][KV8_MAX_TILES + 1] = {{0, 0.142, 0.20, 0.29}, {0, 0.178, 0.243, 0.326}};
     const int rt = (tiles + p.passes - 1) / p.passes;
     const double rounds = (double)B * nkv * p.passes * p.share / 256, same = (double)B / std::max(groups, 1) * p.passes;
     const double longer = rounds <= 1 ? 1 : std::ceil(rounds) * (!f32 ? 0.77 : rt == 1 ? 0.83 : 1);
