@@ -604,7 +604,7 @@ __device__ __forceinline__ void attend_group(Kv8Pass<MODE> a, AttnShared<HD, RT,
     const int all_from = a.window > 0 ? len + count - a.window : 0;   // every row sees the old positions from here on
 
     // Chunks are a loop of their own: where the loop over blocks changes them, pages and scales move between registers on the way round, and every block begins with a wait for all
-    // that is under way, its own V among it (8B, 4 sequences of 32768 bf16 captured 63 us, so 55).
+    // that is under way, its own V among it (8B, 4 sequences of 32768 bf16 captured 63 us instead of 55).
     for (int i0 = 0; i0 < n_it; i0 += 64) {
         if (i0 > 0) {
             chunk = i0 >> 6;
